@@ -82,6 +82,9 @@ typedef enum nmdlm_status {
 /* bits of the device status word of a block step (nmdlm_step_io.status) */
 #define NMDLM_STATUS_TOKEN_CLAMPED 0x1  /* a token id outside [0, V] was read as
                                            the nearest of 0 and V (the mask id) */
+/* bits of the device status word of nmdlm_page_plan */
+#define NMDLM_STATUS_PAGES_SHORT 0x2    /* the ring had too few pages for a request */
+#define NMDLM_STATUS_BAD_REQUEST 0x4    /* lengths outside the bounds of the plan   */
 
 /*
  * Statistics of one spike product, written by the device (int64 so the
@@ -501,6 +504,149 @@ nmdlm_status nmdlm_block_step(const nmdlm_model* model, nmdlm_step_io* io,
  * several sequences). */
 size_t nmdlm_block_step_workspace_size(const nmdlm_model* model, int M,
                                        unsigned flags);
+
+/* ------------------------------------------------------------------------
+ * Paged caches — requests of different lengths that share one pool of pages.
+ *
+ * A page holds the keys and values of NMDLM_PAGE = 64 consecutive positions of
+ * one request (one word of the value cache).  A layer's pool:
+ *   k_pages    device [pool][H][T][64][dh/64] words, 16-byte aligned: bit c%64
+ *              of word c/64 is key channel c of the head at that position
+ *   v_pages    device [pool][H][T][dh] words, 16-byte aligned: bit j is value
+ *              channel c of the page's position j
+ *   key_counts device [pool][H][T][dh] bytes, 16-byte aligned: in how many of
+ *              the page's keys channel c spikes (what nmdlm_page_select scores
+ *              by)
+ * The layers of a model share the page numbers: one plan serves all of them.
+ *
+ * A plan covers n_seq requests, each with `held` pages (logical page p, its
+ * positions 64p .. 64p+63, is pool page table[s][p]) and, in one step, new
+ * rows that follow its context.  Packed rows are the new rows of all
+ * requests one after the other: spikes [T][max_rows][H*dh/64], rows
+ * [cu_rows[s], cu_rows[s+1]) being request s's.  Rows past the last
+ * request's are not read as queries, keys or values, and nothing is written
+ * for them.
+ *
+ * The plan is device memory of the caller.  The table, held, ring and
+ * ring_state arrays live from step to step; initially held = 0, ring = the page numbers 0 .. pool-1
+ * in any order and ring_state = {0, pool}.  The others are outputs of
+ * nmdlm_page_plan.  Page numbers outside the pool are never followed: keys of
+ * such a page count as absent and rows of it are not stored.
+ * ------------------------------------------------------------------------ */
+#define NMDLM_PAGE 64
+#define NMDLM_MAX_REQUESTS 65536
+#define NMDLM_MAX_PLAN_ROWS 524288   /* 2^19 packed rows                        */
+#define NMDLM_MAX_PAGES 131072       /* pages of a request: NMDLM_MAX_KEYS / 64 */
+#define NMDLM_MAX_POOL 33554432      /* pages of a pool (2^25)                  */
+
+typedef struct nmdlm_pages {
+  int n_seq;            /* requests, 1 .. NMDLM_MAX_REQUESTS                    */
+  int max_rows;         /* packed rows, 1 .. NMDLM_MAX_PLAN_ROWS                */
+  int max_pages;        /* width of the table, 1 .. NMDLM_MAX_PAGES             */
+  int pool;             /* pages of the pool, 1 .. NMDLM_MAX_POOL               */
+  int32_t* table;       /* device [n_seq][max_pages]                            */
+  int32_t* held;        /* device [n_seq]: pages that request s holds           */
+  int32_t* ring;        /* device [pool]: free pages, from ring_state[0] on,
+                           wrapping at pool                                     */
+  int32_t* ring_state;  /* device [2]: index of the first free page, their number */
+  int32_t* cu_rows;     /* device [n_seq + 1]: first packed row of each request */
+  int64_t* slot;        /* device [max_rows]: 64 * page + position within it, or
+                           -1 for a row that has no page                        */
+  int32_t* pos;         /* device [max_rows]: position of the row in its request
+                           (0 for a row without a request)                      */
+  void* index;          /* device, 16-byte aligned: work lists of the calls below */
+  size_t index_bytes;   /* >= nmdlm_page_index_bytes(n_seq, max_rows)           */
+} nmdlm_pages;
+
+size_t nmdlm_page_index_bytes(int n_seq, int max_rows);
+
+/* ------------------------------------------------------------------------
+ * nmdlm_page_plan — block tables, slots and work lists of a step from the
+ * requests' lengths.  Request s holds ctx[s] positions and brings new_rows[s]:
+ *   new_rows > 0   rows for positions ctx .. ctx+new_rows-1.  The pages up to
+ *                  ceil((ctx+new_rows)/64) that it does not hold are taken from
+ *                  the ring, in the order of the requests
+ *   new_rows = 0   idle: keeps its pages
+ *   new_rows = -1  ended: its pages go behind the ring's last, held becomes 0
+ *                  (free to be taken from the next call on)
+ * A call with the same lengths again takes no further page, so the plan can
+ * be made once a block and used by all of its steps.
+ *
+ * From the first request on whose pages the ring does not have, every
+ * request that needs a page is refused (NMDLM_STATUS_PAGES_SHORT); one with
+ * ctx < 0 or ctx > 64 held, new_rows < -1, ctx+new_rows > 64 max_pages, held
+ * outside [0, max_pages] or rows past max_rows is refused as well
+ * (NMDLM_STATUS_BAD_REQUEST).  A refused request takes no page; its rows (none
+ * when new_rows > max_rows) have slot -1 and the calls below skip them.
+ *
+ *   ctx, new_rows  device int32 [n_seq]
+ *   status         device int32 or NULL: bits are ORed in
+ * Errors: NMDLM_ERR_INVALID_ARG for a missing or misaligned pointer or a size
+ * below 1, NMDLM_ERR_UNSUPPORTED beyond the limits above,
+ * NMDLM_ERR_WORKSPACE for an index that is too small.
+ * ------------------------------------------------------------------------ */
+nmdlm_status nmdlm_page_plan(const nmdlm_pages* pages, const int32_t* ctx,
+                             const int32_t* new_rows, int32_t* status, void* stream);
+
+/* ------------------------------------------------------------------------
+ * nmdlm_page_store — keys and values of the packed rows into their pages,
+ * after nmdlm_page_plan.  key_counts of a page that takes rows are counted
+ * again over its positions up to the last stored one (keys past it, of an
+ * earlier holder of the page, are not counted).  Bits of other positions keep
+ * their values.
+ *
+ *   k, v        device spikes [T][max_rows][H*dh/64], 16-byte aligned
+ *   k_pages, v_pages, key_counts   see above
+ *   T, H, dh    1 <= T <= 8, dh 64 or 128, T*max_rows <= 2^19, H*dh <= 65536
+ * ------------------------------------------------------------------------ */
+nmdlm_status nmdlm_page_store(const nmdlm_pages* pages, const uint64_t* k,
+                              const uint64_t* v, int T, int H, int dh,
+                              uint64_t* k_pages, uint64_t* v_pages,
+                              uint8_t* key_counts, void* stream);
+
+/* ------------------------------------------------------------------------
+ * nmdlm_page_select — for each packed row and head, the context pages that
+ * matter most to it.  Page p of the ctx/64 full context pages scores
+ *     S = sum_t sum_c Q[t,row,c] * key_counts[page][head][t][c],
+ * the sum over the page's keys and the timesteps of the attention scores
+ * popcount(Q AND K).  The n_sel pages of the largest S are selected (ties: the
+ * lower p; all when there are no more), and every page from ctx/64 on: the
+ * rest of the context and the new rows themselves.  The integers are exact.
+ *
+ *   q      device spikes [T][max_rows][H*dh/64], 16-byte aligned
+ *   n_sel  >= 0
+ *   sel    device [max_rows][H][ceil(max_pages/64)] words: bit p%64 of word
+ *          p/64 is set when logical page p is selected; rows without a page
+ *          keep their words
+ *   ws     workspace of nmdlm_page_select_workspace_size() bytes
+ * ------------------------------------------------------------------------ */
+nmdlm_status nmdlm_page_select(const nmdlm_pages* pages, const uint64_t* q, int T,
+                               int H, int dh, const uint8_t* key_counts, int n_sel,
+                               uint64_t* sel, void* ws, size_t ws_bytes, void* stream);
+size_t nmdlm_page_select_workspace_size(const nmdlm_pages* pages, int T, int H, int dh);
+
+/* ------------------------------------------------------------------------
+ * nmdlm_bbm_attn_paged — nmdlm_bbm_attn (its formulas, weights and neuron) of
+ * the packed rows: row i of request s over the keys of its ctx+new_rows
+ * positions, in its pages.  The rows' own keys and values must be stored
+ * (nmdlm_page_store).  With sel, a row of a head sees only the keys of the
+ * pages whose bit is set (0 where none is: a = 0).
+ *
+ *   q, T, H, dh, k_pages, v_pages   see above
+ *   lut_att  device uint8 [256]
+ *   sel      device [max_rows][H][ceil(max_pages/64)] words or NULL (all pages)
+ *   a_out    device int32 [T][max_rows][H*dh] or NULL
+ *   theta_a  threshold (> 0) when s_out is given
+ *   s_out    device spikes [T][max_rows][H*dh/64] or NULL (at least one output);
+ *            rows without a page keep what a_out and s_out hold
+ *   ws       workspace of nmdlm_bbm_attn_paged_workspace_size() bytes
+ * ------------------------------------------------------------------------ */
+nmdlm_status nmdlm_bbm_attn_paged(const nmdlm_pages* pages, const uint64_t* q, int T,
+                                  int H, int dh, const uint64_t* k_pages,
+                                  const uint64_t* v_pages, const uint8_t* lut_att,
+                                  const uint64_t* sel, int32_t* a_out, int32_t theta_a,
+                                  uint64_t* s_out, void* ws, size_t ws_bytes, void* stream);
+size_t nmdlm_bbm_attn_paged_workspace_size(const nmdlm_pages* pages, int T, int H, int dh);
 
 /* Clears a workspace region with a fill kernel on the stream (use once on a
  * new workspace). */

@@ -557,3 +557,111 @@ def bitwise_value(s: np.ndarray) -> np.ndarray:
     train codes (Eq. (8)), and the sum Eq. (11) scales by V_th."""
     s = np.asarray(s, dtype=np.int64)
     return sum((1 << t) * s[t] for t in range(s.shape[0]))
+
+
+# ----------------------------------------------------------------------------
+# Paged caches: requests of different lengths over one pool of 64-position pages
+# ----------------------------------------------------------------------------
+PAGE = 64
+PAGES_SHORT, BAD_REQUEST = 2, 4
+
+
+def page_plan(ctx, new, table, held, ring, ring_state, max_rows: int) -> dict:
+    """One request after the other: an ended one (new = -1) gives its pages
+    back behind the ring's last, one with new rows takes the pages it lacks
+    from the ring's first.  After the first request whose pages are not there
+    every other that needs a page is refused; a request outside the bounds is
+    refused and takes nothing.  Returns the new state and, per packed row, slot
+    and position."""
+    table, held, ring = (np.array(x, dtype=np.int64) for x in (table, held, ring))
+    n, max_pages = table.shape
+    pool = len(ring)
+    head, free = (int(x) for x in ring_state)
+    slot, pos = np.full(max_rows, -1, dtype=np.int64), np.zeros(max_rows, dtype=np.int64)
+    cu, end, status = [0], 0, 0
+    asked = taken = 0
+    back = []
+    ok = []
+    for s in range(n):
+        c, m = int(ctx[s]), int(new[s])
+        end += m if 0 < m <= max_rows else 0
+        first = cu[-1]
+        cu.append(min(end, max_rows))
+        ok.append(False)
+        if not 0 <= held[s] <= max_pages or m < -1:
+            status |= BAD_REQUEST
+            continue
+        if m == -1:
+            back += [int(p) for p in table[s, :held[s]]]
+            held[s] = 0
+            continue
+        if m > max_rows or end > max_rows or c < 0 or c > PAGE * held[s] or c + m > PAGE * max_pages:
+            status |= BAD_REQUEST
+            continue
+        lack = max(0, -(-(c + m) // PAGE) - int(held[s]))
+        asked += lack
+        if lack and asked > free:
+            status |= PAGES_SHORT
+            continue
+        ok[-1] = True
+        for _ in range(lack):
+            table[s, held[s]] = ring[(head + taken) % pool]
+            held[s] += 1
+            taken += 1
+        for i in range(m):
+            page = int(table[s, (c + i) // PAGE])
+            pos[first + i] = c + i
+            if 0 <= page < pool:
+                slot[first + i] = page * PAGE + (c + i) % PAGE
+    for i, p in enumerate(back):
+        ring[(head + free + i) % pool] = p
+    return dict(table=table, held=held, ring=ring, ring_state=[(head + taken) % pool, free - taken + len(back)],
+                cu_rows=np.array(cu), slot=slot, pos=pos, status=status, ok=np.array(ok))
+
+
+def page_store(k, v, slot, k_pages, v_pages, counts) -> None:
+    """k, v: 0/1 [T][rows][H][dh]; k_pages, v_pages: 0/1 [pool][H][T][64][dh];
+    counts [pool][H][T][dh].  Writes each row with a slot; the counts of a page
+    cover its positions up to the last one written."""
+    last = {}
+    for m, sl in enumerate(slot):
+        if sl < 0:
+            continue
+        page, off = divmod(int(sl), PAGE)
+        k_pages[page, :, :, off] = k[:, m].transpose(1, 0, 2)
+        v_pages[page, :, :, off] = v[:, m].transpose(1, 0, 2)
+        last[page] = max(last.get(page, 0), off)
+    for page, off in last.items():
+        counts[page] = k_pages[page, :, :, :off + 1].sum(2)
+
+
+def page_select(Q, counts, n_full: int, n_pages: int, n_sel: int) -> np.ndarray:
+    """Q: 0/1 [T][M][H][dh]; counts [n_pages][H][T][dh] of the request's pages.
+    0/1 [M][H][n_pages]: the n_sel of the first n_full pages with the largest
+    sum_t sum_c Q * count (ties: the lower page), and all from n_full on."""
+    T, M, H, _ = Q.shape
+    sel = np.zeros((M, H, n_pages), dtype=np.uint8)
+    sel[:, :, n_full:] = 1
+    for m in range(M):
+        for h in range(H):
+            score = (counts[:n_full, h].astype(np.int64) * Q[:, m, h].astype(np.int64)).sum((1, 2))
+            for p in np.lexsort((np.arange(n_full), -score))[:n_sel]:
+                sel[m, h, p] = 1
+    return sel
+
+
+def paged_attention(Q, K, V, lut, see) -> np.ndarray:
+    """Currents of one request: Q 0/1 [T][M][H][dh]; K, V 0/1 [H][T][J][dh];
+    see 0/1 [M][H][J] (the keys that a row of a head sees):
+    floor(256 sum_j p V / sum_j p) over the seen keys, p = lut[popcount(Q and K)],
+    0 where the weights sum to 0.  int64 [T][M][H*dh]."""
+    T, M, H, dh = Q.shape
+    lut = np.asarray(lut, dtype=np.int64)
+    a = np.zeros((T, M, H, dh), dtype=np.int64)
+    for t in range(T):
+        for h in range(H):
+            p = lut[_exact_matmul(Q[t, :, h], K[h, t].T)] * see[:, h].astype(np.int64)
+            num, den = _exact_matmul(p, V[h, t]), p.sum(1)
+            live = den > 0
+            a[t, live, h] = 256 * num[live] // den[live, None]
+    return a.reshape(T, M, H * dh)

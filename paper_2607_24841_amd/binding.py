@@ -31,6 +31,13 @@ NMDLM_ATTN_FUSED = 0x4
 NMDLM_MAX_HEAD_M = 4096   # block tokens of a step that runs the head
 NMDLM_MAX_KEYS = 1 << 23   # attention keys C+M per sequence
 NMDLM_STATUS_TOKEN_CLAMPED = 0x1
+NMDLM_STATUS_PAGES_SHORT = 0x2
+NMDLM_STATUS_BAD_REQUEST = 0x4
+NMDLM_PAGE = 64           # positions of a page
+NMDLM_MAX_REQUESTS = 65536
+NMDLM_MAX_PLAN_ROWS = 1 << 19
+NMDLM_MAX_PAGES = 1 << 17   # pages of a request
+NMDLM_MAX_POOL = 1 << 25
 NMDLM_NOALLOC_SCRATCH_BYTES = 16 << 20   # static scratch of nmdlm_qbsm_noalloc per GPU
 NMDLM_MAX_THR_DEN = 1 << 24
 NMDLM_PATH_SHIFT = 20
@@ -51,6 +58,9 @@ EXPORTS = (
     "nmdlm_block_step_workspace_size", "nmdlm_workspace_clear", "nmdlm_status_string",
     "nmdlm_abi_version", "nmdlm_ternary_encode", "nmdlm_qbsm_ternary", "nmdlm_qbsm_ternary_if",
     "nmdlm_qbsm_blocked", "nmdlm_weight_blocked_bytes", "nmdlm_weight_block",
+    "nmdlm_page_index_bytes", "nmdlm_page_plan", "nmdlm_page_store", "nmdlm_page_select",
+    "nmdlm_page_select_workspace_size", "nmdlm_bbm_attn_paged",
+    "nmdlm_bbm_attn_paged_workspace_size",
 )
 
 
@@ -96,6 +106,15 @@ class StepIO(C.Structure):
         ("pred", C.c_void_p), ("conf", C.c_void_p), ("unmasked_pos", C.c_void_p),
         ("stats", C.c_void_p), ("prof_events", C.POINTER(C.c_void_p)), ("n_prof_events", C.c_int),
         ("n_seq", C.c_int), ("status", C.c_void_p),
+    ]
+
+
+class PagesC(C.Structure):
+    _fields_ = [
+        ("n_seq", C.c_int), ("max_rows", C.c_int), ("max_pages", C.c_int), ("pool", C.c_int),
+        ("table", C.c_void_p), ("held", C.c_void_p), ("ring", C.c_void_p),
+        ("ring_state", C.c_void_p), ("cu_rows", C.c_void_p), ("slot", C.c_void_p),
+        ("pos", C.c_void_p), ("index", C.c_void_p), ("index_bytes", C.c_size_t),
     ]
 
 
@@ -148,6 +167,18 @@ def load(path: str = LIB_PATH):
     lib.nmdlm_block_step.argtypes = [C.POINTER(Model), C.POINTER(StepIO), vp, sz, vp]
     lib.nmdlm_block_step_workspace_size.argtypes = [C.POINTER(Model), C.c_int, u]
     lib.nmdlm_block_step_workspace_size.restype = sz
+    pg = C.POINTER(PagesC)
+    lib.nmdlm_page_index_bytes.argtypes = [C.c_int, C.c_int]
+    lib.nmdlm_page_index_bytes.restype = sz
+    lib.nmdlm_page_plan.argtypes = [pg, vp, vp, vp, vp]
+    lib.nmdlm_page_store.argtypes = [pg, vp, vp, C.c_int, C.c_int, C.c_int, vp, vp, vp, vp]
+    lib.nmdlm_page_select.argtypes = [pg, vp, C.c_int, C.c_int, C.c_int, vp, C.c_int, vp, vp, sz, vp]
+    lib.nmdlm_page_select_workspace_size.argtypes = [pg, C.c_int, C.c_int, C.c_int]
+    lib.nmdlm_page_select_workspace_size.restype = sz
+    lib.nmdlm_bbm_attn_paged.argtypes = [pg, vp, C.c_int, C.c_int, C.c_int, vp, vp, vp, vp, vp, i32,
+                                         vp, vp, sz, vp]
+    lib.nmdlm_bbm_attn_paged_workspace_size.argtypes = [pg, C.c_int, C.c_int, C.c_int]
+    lib.nmdlm_bbm_attn_paged_workspace_size.restype = sz
     lib.nmdlm_workspace_clear.argtypes = [vp, sz, vp]
     lib.nmdlm_status_string.argtypes = [C.c_int]
     lib.nmdlm_status_string.restype = C.c_char_p
@@ -302,6 +333,132 @@ def nmdlm_bbm_attn(q, k_cache, vt_cache, cache_cap, T, M, C_, H, dh, lut_att, a_
 
 def nmdlm_bbm_attn_workspace_size(T, M, H, dh) -> int:
     return load().nmdlm_bbm_attn_workspace_size(T, M, H, dh)
+
+
+# ----------------------------------------------------------------------------
+# paged caches
+# ----------------------------------------------------------------------------
+class Pages:
+    """The device memory of a page plan (nmdlm_pages) for n_seq requests, at
+    most max_rows packed rows a step and max_pages pages a request, over pools
+    of `pool` pages.  The state that lives from step to step (table, held,
+    ring, ring_state) is one tensor, `state`; at first every page is free."""
+
+    def __init__(self, n_seq: int, max_rows: int, max_pages: int, pool: int, device="cuda"):
+        nbytes = load().nmdlm_page_index_bytes(n_seq, max_rows)
+        if nbytes == 0 or max_pages < 1 or pool < 1:
+            raise NmdlmError(NMDLM_ERR_INVALID_ARG, "Pages: sizes")
+        self.n_seq, self.max_rows, self.max_pages, self.pool = n_seq, max_rows, max_pages, pool
+        i32 = dict(dtype=torch.int32, device=device)
+        self.state = torch.zeros(n_seq * max_pages + n_seq + pool + 2, **i32)
+        self.device = self.state.device
+        table, self.held, self.ring, self.ring_state = torch.split(
+            self.state, [n_seq * max_pages, n_seq, pool, 2])
+        self.table = table.view(n_seq, max_pages)
+        self.cu_rows = torch.zeros(n_seq + 1, **i32)
+        self.pos = torch.zeros(max_rows, **i32)
+        self.slot = torch.full((max_rows,), -1, dtype=torch.int64, device=device)
+        self.index = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        self.reset()
+        self.c = PagesC(n_seq, max_rows, max_pages, pool, ptr(self.table), ptr(self.held),
+                        ptr(self.ring), ptr(self.ring_state), ptr(self.cu_rows), ptr(self.slot),
+                        ptr(self.pos), ptr(self.index), nbytes)
+
+    def reset(self):
+        """No request holds a page."""
+        self.table.fill_(-1)
+        self.held.zero_()
+        torch.arange(self.pool, out=self.ring)
+        self.set_state(None, None, None, (0, self.pool))
+
+    def set_state(self, table, held, ring, ring_state):
+        """Copies the given parts of the state (None: left as they are)."""
+        for dst, src in ((self.table, table), (self.held, held), (self.ring, ring),
+                         (self.ring_state, ring_state)):
+            if src is not None:
+                dst.copy_(torch.as_tensor(src, dtype=torch.int32).view(dst.shape))
+
+    def pools(self, T: int, H: int, dh: int):
+        """A layer's empty pools: key pages, value pages, key counts."""
+        shape = (self.pool, H, T)
+        return (torch.zeros(*shape, NMDLM_PAGE, dh // 64, dtype=torch.int64, device=self.device),
+                torch.zeros(*shape, dh, dtype=torch.int64, device=self.device),
+                torch.zeros(*shape, dh, dtype=torch.uint8, device=self.device))
+
+    def selection(self, H: int):
+        """An empty selection: words [max_rows][H][ceil(max_pages/64)]."""
+        return torch.zeros(self.max_rows, H, -(-self.max_pages // 64), dtype=torch.int64,
+                           device=self.device)
+
+    def _need(self, what: str, **tensors):
+        """Each (tensor or None, elements, bytes of one): on the plan's device,
+        contiguous, of that element size and large enough."""
+        for name, (t, n, size) in tensors.items():
+            if t is None:
+                continue
+            if (t.device != self.device or not t.is_contiguous() or t.element_size() != size
+                    or t.numel() < n):
+                raise NmdlmError(NMDLM_ERR_INVALID_ARG,
+                                 f"{what}: {name} needs {n} contiguous elements of {size} bytes on "
+                                 f"{self.device}")
+
+    def _rows(self, T, H, dh):
+        return T * self.max_rows * (H * dh // 64), 8
+
+    def _pool(self, T, H, dh):
+        return self.pool * H * T * dh, 8
+
+
+def _on(pages: Pages, fn, what: str, *args, stream=None) -> None:
+    """The call on the plan's device and, by default, its current stream."""
+    with torch.cuda.device(pages.device):
+        st = fn(C.byref(pages.c), *args, stream_handle(stream))
+    check(st, what)
+
+
+def nmdlm_page_plan(pages: Pages, ctx, new_rows, status=None, stream=None) -> None:
+    what = "nmdlm_page_plan"
+    pages._need(what, ctx=(ctx, pages.n_seq, 4), new_rows=(new_rows, pages.n_seq, 4),
+                status=(status, 1, 4))
+    _on(pages, load().nmdlm_page_plan, what, ptr(ctx), ptr(new_rows), ptr(status), stream=stream)
+
+
+def nmdlm_page_store(pages: Pages, k, v, T, H, dh, k_pages, v_pages, key_counts, stream=None) -> None:
+    what = "nmdlm_page_store"
+    rows, pool = pages._rows(T, H, dh), pages._pool(T, H, dh)
+    pages._need(what, k=(k, *rows), v=(v, *rows), k_pages=(k_pages, *pool), v_pages=(v_pages, *pool),
+                key_counts=(key_counts, pool[0], 1))
+    _on(pages, load().nmdlm_page_store, what, ptr(k), ptr(v), T, H, dh, ptr(k_pages), ptr(v_pages),
+        ptr(key_counts), stream=stream)
+
+
+def nmdlm_page_select(pages: Pages, q, T, H, dh, key_counts, n_sel, sel, ws=None, stream=None) -> None:
+    what = "nmdlm_page_select"
+    pages._need(what, q=(q, *pages._rows(T, H, dh)), key_counts=(key_counts, pages._pool(T, H, dh)[0], 1),
+                sel=(sel, pages.max_rows * H * -(-pages.max_pages // 64), 8), ws=(ws, 1, 1))
+    _on(pages, load().nmdlm_page_select, what, ptr(q), T, H, dh, ptr(key_counts), n_sel, ptr(sel), ptr(ws),
+        0 if ws is None else ws.numel(), stream=stream)
+
+
+def nmdlm_page_select_workspace_size(pages: Pages, T, H, dh) -> int:
+    return load().nmdlm_page_select_workspace_size(C.byref(pages.c), T, H, dh)
+
+
+def nmdlm_bbm_attn_paged(pages: Pages, q, T, H, dh, k_pages, v_pages, lut_att, a_out=None, theta_a=0,
+                         s_out=None, sel=None, ws=None, stream=None) -> None:
+    what = "nmdlm_bbm_attn_paged"
+    rows, pool = pages._rows(T, H, dh), pages._pool(T, H, dh)
+    pages._need(what, q=(q, *rows), k_pages=(k_pages, *pool), v_pages=(v_pages, *pool),
+                lut_att=(lut_att, 256, 1), a_out=(a_out, T * pages.max_rows * H * dh, 4),
+                s_out=(s_out, *rows), sel=(sel, pages.max_rows * H * -(-pages.max_pages // 64), 8),
+                ws=(ws, 1, 1))
+    _on(pages, load().nmdlm_bbm_attn_paged, what, ptr(q), T, H, dh, ptr(k_pages), ptr(v_pages),
+        ptr(lut_att), ptr(sel), ptr(a_out), theta_a, ptr(s_out), ptr(ws),
+        0 if ws is None else ws.numel(), stream=stream)
+
+
+def nmdlm_bbm_attn_paged_workspace_size(pages: Pages, T, H, dh) -> int:
+    return load().nmdlm_bbm_attn_paged_workspace_size(C.byref(pages.c), T, H, dh)
 
 
 def nmdlm_block_step(model: "DeviceModel", io: StepIO, ws: torch.Tensor, stream=None) -> None:

@@ -4,6 +4,7 @@
 #include <climits>
 
 #include "common.h"
+#include "pages.h"
 
 namespace nmdlm {
 size_t block_step_ws_size(const nmdlm_model* md, int M, unsigned flags);
@@ -28,6 +29,31 @@ size_t qbsm_ws(int T, int M, int K, int N) {
 bool blocked_ok(const int8_t* Wb, int K, int N) {
   return !Wb || (((reinterpret_cast<uintptr_t>(Wb) & 15) == 0) &&
                  weight_blocked_bytes(K, N) < ((size_t)1 << 31));
+}
+
+// the plan's sizes and pointers
+nmdlm_status pages_ok(const nmdlm_pages* p) {
+  if (!p || p->n_seq < 1 || p->max_rows < 1 || p->max_pages < 1 || p->pool < 1) return NMDLM_ERR_INVALID_ARG;
+  if (p->n_seq > NMDLM_MAX_REQUESTS || p->max_rows > NMDLM_MAX_PLAN_ROWS || p->max_pages > NMDLM_MAX_PAGES ||
+      p->pool > NMDLM_MAX_POOL)
+    return NMDLM_ERR_UNSUPPORTED;
+  for (const void* q : {(const void*)p->table, (const void*)p->held, (const void*)p->ring,
+                        (const void*)p->ring_state, (const void*)p->cu_rows, (const void*)p->pos})
+    if (!q || !aligned(q, 4)) return NMDLM_ERR_INVALID_ARG;
+  if (!p->slot || !aligned(p->slot, 8) || !p->index || !aligned(p->index, 16)) return NMDLM_ERR_INVALID_ARG;
+  PageIndex ix;
+  if (p->index_bytes < page_index_layout(p->n_seq, p->max_rows, nullptr, &ix)) return NMDLM_ERR_WORKSPACE;
+  return NMDLM_OK;
+}
+
+// the plan and the sizes of a call over its pages
+nmdlm_status paged_call_ok(const nmdlm_pages* p, int T, int H, int dh) {
+  const nmdlm_status rc = pages_ok(p);
+  if (rc != NMDLM_OK) return rc;
+  if (T < 1 || H < 1 || dh < 1) return NMDLM_ERR_INVALID_ARG;
+  if (T > NMDLM_MAX_T || (dh != 64 && dh != 128)) return NMDLM_ERR_UNSUPPORTED;
+  if ((int64_t)T * p->max_rows > (1 << 19) || (int64_t)H * dh > NMDLM_MAX_K) return NMDLM_ERR_UNSUPPORTED;
+  return NMDLM_OK;
 }
 
 bool weights_ok(const int8_t* W, int K, int N, int64_t ldw) {
@@ -329,6 +355,67 @@ nmdlm_status nmdlm_bbm_attn(const uint64_t* q, const uint64_t* k_cache, const ui
   const AttnCall c{q, k_cache, vt_cache, cache_cap, T, M, C, H, dh, 1, 0, lut_att, theta_a, a_out,
                    a, s_out, nullptr, false, false};
   return launch_attention(c, static_cast<hipStream_t>(stream));
+}
+
+size_t nmdlm_page_index_bytes(int n_seq, int max_rows) {
+  if (n_seq < 1 || n_seq > NMDLM_MAX_REQUESTS || max_rows < 1 || max_rows > NMDLM_MAX_PLAN_ROWS) return 0;
+  PageIndex ix;
+  return page_index_layout(n_seq, max_rows, nullptr, &ix);
+}
+
+nmdlm_status nmdlm_page_plan(const nmdlm_pages* pg, const int32_t* ctx, const int32_t* new_rows,
+                             int32_t* status, void* stream) {
+  const nmdlm_status rc = pages_ok(pg);
+  if (rc != NMDLM_OK) return rc;
+  if (!ctx || !new_rows) return NMDLM_ERR_INVALID_ARG;
+  return launch_page_plan(*pg, ctx, new_rows, status, static_cast<hipStream_t>(stream));
+}
+
+nmdlm_status nmdlm_page_store(const nmdlm_pages* pg, const uint64_t* k, const uint64_t* v, int T, int H,
+                              int dh, uint64_t* k_pages, uint64_t* v_pages, uint8_t* key_counts,
+                              void* stream) {
+  const nmdlm_status rc = paged_call_ok(pg, T, H, dh);
+  if (rc != NMDLM_OK) return rc;
+  for (const void* p : {(const void*)k, (const void*)v, (const void*)k_pages, (const void*)v_pages,
+                        (const void*)key_counts})
+    if (!p || !aligned(p, 16)) return NMDLM_ERR_INVALID_ARG;
+  return launch_page_store(*pg, k, v, T, H, dh, k_pages, v_pages, key_counts,
+                           static_cast<hipStream_t>(stream));
+}
+
+size_t nmdlm_page_select_workspace_size(const nmdlm_pages* pg, int T, int H, int dh) {
+  return paged_call_ok(pg, T, H, dh) == NMDLM_OK ? page_select_ws(*pg, H) : 0;
+}
+
+nmdlm_status nmdlm_page_select(const nmdlm_pages* pg, const uint64_t* q, int T, int H, int dh,
+                               const uint8_t* key_counts, int n_sel, uint64_t* sel, void* ws,
+                               size_t ws_bytes, void* stream) {
+  const nmdlm_status rc = paged_call_ok(pg, T, H, dh);
+  if (rc != NMDLM_OK) return rc;
+  if (!q || !aligned(q, 16) || !key_counts || !aligned(key_counts, 16) || !sel || n_sel < 0)
+    return NMDLM_ERR_INVALID_ARG;
+  if (!ws || !aligned(ws, 256) || ws_bytes < page_select_ws(*pg, H)) return NMDLM_ERR_WORKSPACE;
+  return launch_page_select(*pg, q, T, H, dh, key_counts, n_sel, sel, ws, static_cast<hipStream_t>(stream));
+}
+
+size_t nmdlm_bbm_attn_paged_workspace_size(const nmdlm_pages* pg, int T, int H, int dh) {
+  return paged_call_ok(pg, T, H, dh) == NMDLM_OK ? paged_attn_ws(*pg, T, H, dh) : 0;
+}
+
+nmdlm_status nmdlm_bbm_attn_paged(const nmdlm_pages* pg, const uint64_t* q, int T, int H, int dh,
+                                  const uint64_t* k_pages, const uint64_t* v_pages,
+                                  const uint8_t* lut_att, const uint64_t* sel, int32_t* a_out,
+                                  int32_t theta_a, uint64_t* s_out, void* ws, size_t ws_bytes,
+                                  void* stream) {
+  const nmdlm_status rc = paged_call_ok(pg, T, H, dh);
+  if (rc != NMDLM_OK) return rc;
+  for (const void* p : {(const void*)q, (const void*)k_pages, (const void*)v_pages})
+    if (!p || !aligned(p, 16)) return NMDLM_ERR_INVALID_ARG;
+  if (!lut_att || (!a_out && !s_out) || (s_out && theta_a <= 0)) return NMDLM_ERR_INVALID_ARG;
+  const size_t need = paged_attn_ws(*pg, T, H, dh);
+  if (need > 0 && (!ws || !aligned(ws, 256) || ws_bytes < need)) return NMDLM_ERR_WORKSPACE;
+  const PagedAttnCall c{q, k_pages, v_pages, T, H, dh, lut_att, sel, a_out, theta_a, s_out, nullptr, ws};
+  return launch_paged_attn(*pg, c, static_cast<hipStream_t>(stream));
 }
 
 size_t nmdlm_block_step_workspace_size(const nmdlm_model* model, int M, unsigned flags) {

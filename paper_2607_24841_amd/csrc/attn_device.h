@@ -334,6 +334,11 @@ struct AttnWave {
       for (int n = 0; n < NT; ++n) v[n] &= vm;
     }
     weigh(v, p);
+    finish(reinterpret_cast<char*>(st), lane, g, c);
+  }
+
+  // The wave's sums over its lane groups; sc: LDS of the wave, 64 bytes a tile.
+  __device__ __forceinline__ void finish(char* sc, int lane, int g, int c) {
 #pragma unroll
     for (int w = 0; w < QG; ++w) {  // over the four lane groups
       den[w] += __shfl_xor(den[w], 16);
@@ -345,7 +350,6 @@ struct AttnWave {
     for (int n = 0; n < NT; ++n) cnt[n] += __shfl_xor(cnt[n], 16);
 #pragma unroll
     for (int n = 0; n < NT; ++n) cnt[n] += __shfl_xor(cnt[n], 32);
-    char* sc = reinterpret_cast<char*>(st);
 #pragma unroll
     for (int n = 0; n < NT; ++n)  // the four lane groups store the same values
       *reinterpret_cast<i32_alias*>(sc + 64 * n + 4 * c) = 128 * cnt[n];

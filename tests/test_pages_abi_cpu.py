@@ -1,0 +1,141 @@
+"""Refusals of the paged calls, before any HIP call (no GPU)."""
+import ctypes as C
+import os
+
+import pytest
+
+torch = pytest.importorskip("torch")
+from paper_2607_24841_amd import binding as B  # noqa: E402
+
+FAKE = 1 << 40
+pytestmark = pytest.mark.skipif(not os.path.exists(B.LIB_PATH), reason="libnmdlm.so not built")
+INVALID, UNSUPPORTED, WORKSPACE = B.NMDLM_ERR_INVALID_ARG, B.NMDLM_ERR_UNSUPPORTED, B.NMDLM_ERR_WORKSPACE
+
+
+def pages(**kw):
+    a = dict(n_seq=3, max_rows=40, max_pages=5, pool=9, table=FAKE, held=FAKE, ring=FAKE, ring_state=FAKE,
+             cu_rows=FAKE, slot=FAKE, pos=FAKE, index=FAKE, index_bytes=1 << 40)
+    a.update(kw)
+    return B.PagesC(*[a[n] for n, _ in B.PagesC._fields_])
+
+
+def plan(p=None, ctx=FAKE, new=FAKE):
+    return B.load().nmdlm_page_plan(C.byref(p if p is not None else pages()), ctx, new, None, None)
+
+
+def store(p=None, **kw):
+    a = dict(k=FAKE, v=FAKE, T=4, H=2, dh=64, kp=FAKE, vp=FAKE, cnt=FAKE)
+    a.update(kw)
+    return B.load().nmdlm_page_store(C.byref(p if p is not None else pages()), *a.values(), None)
+
+
+def select(p=None, **kw):
+    a = dict(q=FAKE, T=4, H=2, dh=64, cnt=FAKE, n_sel=2, sel=FAKE, ws=FAKE, ws_bytes=1 << 40)
+    a.update(kw)
+    return B.load().nmdlm_page_select(C.byref(p if p is not None else pages()), *a.values(), None)
+
+
+def attn(p=None, **kw):
+    a = dict(q=FAKE, T=4, H=2, dh=64, kp=FAKE, vp=FAKE, lut=FAKE, sel=None, a_out=FAKE, theta=100, s_out=FAKE,
+             ws=FAKE, ws_bytes=1 << 40)
+    a.update(kw)
+    return B.load().nmdlm_bbm_attn_paged(C.byref(p if p is not None else pages()), *a.values(), None)
+
+
+CALLS = [plan, store, select, attn]
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_plan_arguments(call):
+    for name in ("n_seq", "max_rows", "max_pages", "pool"):
+        assert call(pages(**{name: 0})) == INVALID, name
+        assert call(pages(**{name: -5})) == INVALID, name
+    for name in ("table", "held", "ring", "ring_state", "cu_rows", "slot", "pos", "index"):
+        assert call(pages(**{name: None})) == INVALID, name
+    assert call(pages(slot=FAKE + 4)) == INVALID
+    assert call(pages(index=FAKE + 8)) == INVALID
+    assert call(pages(table=FAKE + 2)) == INVALID
+    assert call(pages(n_seq=B.NMDLM_MAX_REQUESTS + 1)) == UNSUPPORTED
+    assert call(pages(max_rows=B.NMDLM_MAX_PLAN_ROWS + 1)) == UNSUPPORTED
+    assert call(pages(max_pages=B.NMDLM_MAX_PAGES + 1)) == UNSUPPORTED
+    assert call(pages(pool=B.NMDLM_MAX_POOL + 1)) == UNSUPPORTED
+    need = B.load().nmdlm_page_index_bytes(3, 40)
+    assert call(pages(index_bytes=need - 1)) == WORKSPACE
+
+
+def test_null_plan():
+    assert B.load().nmdlm_page_plan(None, FAKE, FAKE, None, None) == INVALID
+    assert plan(ctx=None) == INVALID
+    assert plan(new=None) == INVALID
+
+
+@pytest.mark.parametrize("call", CALLS[1:])
+def test_sizes(call):
+    for name in ("T", "H", "dh"):
+        assert call(**{name: 0}) == INVALID, name
+    assert call(T=9) == UNSUPPORTED
+    assert call(dh=96) == UNSUPPORTED
+    assert call(H=1025) == UNSUPPORTED                       # H*dh beyond 65536
+    assert call(pages(max_rows=(1 << 17) + 1)) == UNSUPPORTED  # T*max_rows beyond 2^19
+
+
+def test_pointers():
+    for name in ("k", "v", "kp", "vp", "cnt"):
+        assert store(**{name: None}) == INVALID, name
+        assert store(**{name: FAKE + 8}) == INVALID, name
+    for name in ("q", "cnt"):
+        assert select(**{name: None}) == INVALID, name
+        assert select(**{name: FAKE + 8}) == INVALID, name
+    assert select(sel=None) == INVALID
+    assert select(n_sel=-1) == INVALID
+    assert select(ws=None) == WORKSPACE
+    assert select(ws=FAKE + 16) == WORKSPACE
+    assert select(ws_bytes=B.load().nmdlm_page_select_workspace_size(C.byref(pages()), 4, 2, 64) - 1) == WORKSPACE
+    for name in ("q", "kp", "vp"):
+        assert attn(**{name: None}) == INVALID, name
+        assert attn(**{name: FAKE + 8}) == INVALID, name
+    assert attn(lut=None) == INVALID
+    assert attn(a_out=None, s_out=None) == INVALID
+    assert attn(theta=0) == INVALID
+    need = B.load().nmdlm_bbm_attn_paged_workspace_size(C.byref(pages(max_pages=500)), 4, 2, 64)
+    assert need > 0
+    assert attn(pages(max_pages=500), ws_bytes=need - 1) == WORKSPACE
+    assert attn(pages(max_pages=500), ws=None) == WORKSPACE
+
+
+def test_sizes_of_invalid_calls_are_zero():
+    lib = B.load()
+    assert lib.nmdlm_page_index_bytes(0, 4) == 0
+    assert lib.nmdlm_page_index_bytes(4, 0) == 0
+    assert lib.nmdlm_page_index_bytes(B.NMDLM_MAX_REQUESTS + 1, 4) == 0
+    assert lib.nmdlm_page_index_bytes(4, B.NMDLM_MAX_PLAN_ROWS + 1) == 0
+    for f in (lib.nmdlm_page_select_workspace_size, lib.nmdlm_bbm_attn_paged_workspace_size):
+        assert f(C.byref(pages()), 9, 2, 64) == 0
+        assert f(C.byref(pages()), 4, 2, 32) == 0
+        assert f(None, 4, 2, 64) == 0
+
+
+def test_binding_checks_its_tensors():
+    p = B.Pages(2, 10, 3, 7, device="cpu")
+    assert p.ring.tolist() == list(range(7)) and p.ring_state.tolist() == [0, 7] and p.table.shape == (2, 3)
+    k = torch.zeros(4, 10, 2, dtype=torch.int64)
+    kp, vp, cnt = p.pools(4, 2, 64)
+    ok = dict(k=k, v=k, T=4, H=2, dh=64, k_pages=kp, v_pages=vp, key_counts=cnt)
+    for bad in (dict(k=k[:3]), dict(v=k.int()), dict(k_pages=kp[:-1]), dict(v_pages=vp.transpose(1, 2)),
+                dict(key_counts=cnt[1:])):
+        with pytest.raises(B.NmdlmError, match=next(iter(bad))):
+            B.nmdlm_page_store(p, **{**ok, **bad})
+    with pytest.raises(B.NmdlmError, match="ctx"):
+        B.nmdlm_page_plan(p, torch.zeros(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32))
+    with pytest.raises(B.NmdlmError):
+        B.Pages(0, 10, 3, 7, device="cpu")
+
+
+def test_constants_match_the_header():
+    import re
+
+    text = open(os.path.join(os.path.dirname(B.PKG), "include", "nmdlm.h")).read()
+    for name in ("NMDLM_PAGE", "NMDLM_MAX_REQUESTS", "NMDLM_MAX_PLAN_ROWS", "NMDLM_MAX_PAGES",
+                 "NMDLM_MAX_POOL", "NMDLM_STATUS_PAGES_SHORT", "NMDLM_STATUS_BAD_REQUEST"):
+        m = re.search(r"#define\s+%s\s+([0-9xXa-fA-F]+)" % name, text)
+        assert getattr(B, name) == int(m.group(1), 0), name
