@@ -352,6 +352,8 @@ class Pages:
         i32 = dict(dtype=torch.int32, device=device)
         self.state = torch.zeros(n_seq * max_pages + n_seq + pool + 2, **i32)
         self.device = self.state.device
+        self._index = self.state.get_device()   # of the GPU, -1 on the host
+        self.words = -(-max_pages // 64)        # words of a row and head in a selection
         table, self.held, self.ring, self.ring_state = torch.split(
             self.state, [n_seq * max_pages, n_seq, pool, 2])
         self.table = table.view(n_seq, max_pages)
@@ -363,6 +365,7 @@ class Pages:
         self.c = PagesC(n_seq, max_rows, max_pages, pool, ptr(self.table), ptr(self.held),
                         ptr(self.ring), ptr(self.ring_state), ptr(self.cu_rows), ptr(self.slot),
                         ptr(self.pos), ptr(self.index), nbytes)
+        self._ref = C.byref(self.c)
 
     def reset(self):
         """No request holds a page."""
@@ -387,57 +390,59 @@ class Pages:
 
     def selection(self, H: int):
         """An empty selection: words [max_rows][H][ceil(max_pages/64)]."""
-        return torch.zeros(self.max_rows, H, -(-self.max_pages // 64), dtype=torch.int64,
-                           device=self.device)
+        return torch.zeros(self.max_rows, H, self.words, dtype=torch.int64, device=self.device)
 
-    def _need(self, what: str, **tensors):
-        """Each (tensor or None, elements, bytes of one): on the plan's device,
-        contiguous, of that element size and large enough."""
-        for name, (t, n, size) in tensors.items():
-            if t is None:
-                continue
-            if (t.device != self.device or not t.is_contiguous() or t.element_size() != size
-                    or t.numel() < n):
-                raise NmdlmError(NMDLM_ERR_INVALID_ARG,
-                                 f"{what}: {name} needs {n} contiguous elements of {size} bytes on "
-                                 f"{self.device}")
+    def _arg(self, what: str, name: str, t, n: int, size: int) -> int | None:
+        """The address of a tensor (None for None) that has to lie on the plan's
+        device, contiguous, with n or more elements of `size` bytes."""
+        if t is None:
+            return None
+        if (t.numel() < n or t.element_size() != size or t.get_device() != self._index
+                or not t.is_contiguous()):
+            raise NmdlmError(NMDLM_ERR_INVALID_ARG,
+                             f"{what}: {name} needs {n} contiguous elements of {size} bytes on "
+                             f"{self.device}")
+        return t.data_ptr()
 
-    def _rows(self, T, H, dh):
-        return T * self.max_rows * (H * dh // 64), 8
-
-    def _pool(self, T, H, dh):
-        return self.pool * H * T * dh, 8
-
-
-def _on(pages: Pages, fn, what: str, *args, stream=None) -> None:
-    """The call on the plan's device and, by default, its current stream."""
-    with torch.cuda.device(pages.device):
-        st = fn(C.byref(pages.c), *args, stream_handle(stream))
-    check(st, what)
+    def _call(self, fn, what: str, *args, stream=None) -> None:
+        """The call on the plan's device and, by default, its current stream."""
+        if self._index < 0:
+            raise NmdlmError(NMDLM_ERR_INVALID_ARG, f"{what}: the plan is not on a GPU")
+        if stream is not None:
+            stream = stream.cuda_stream
+        else:
+            stream = torch._C._cuda_getCurrentRawStream(self._index)
+        if torch.cuda.current_device() == self._index:
+            st = fn(self._ref, *args, stream)
+        else:
+            with torch.cuda.device(self._index):
+                st = fn(self._ref, *args, stream)
+        if st != NMDLM_OK:
+            check(st, what)
 
 
 def nmdlm_page_plan(pages: Pages, ctx, new_rows, status=None, stream=None) -> None:
-    what = "nmdlm_page_plan"
-    pages._need(what, ctx=(ctx, pages.n_seq, 4), new_rows=(new_rows, pages.n_seq, 4),
-                status=(status, 1, 4))
-    _on(pages, load().nmdlm_page_plan, what, ptr(ctx), ptr(new_rows), ptr(status), stream=stream)
+    what, arg = "nmdlm_page_plan", pages._arg
+    n = pages.n_seq
+    pages._call(load().nmdlm_page_plan, what, arg(what, "ctx", ctx, n, 4),
+                arg(what, "new_rows", new_rows, n, 4), arg(what, "status", status, 1, 4), stream=stream)
 
 
 def nmdlm_page_store(pages: Pages, k, v, T, H, dh, k_pages, v_pages, key_counts, stream=None) -> None:
-    what = "nmdlm_page_store"
-    rows, pool = pages._rows(T, H, dh), pages._pool(T, H, dh)
-    pages._need(what, k=(k, *rows), v=(v, *rows), k_pages=(k_pages, *pool), v_pages=(v_pages, *pool),
-                key_counts=(key_counts, pool[0], 1))
-    _on(pages, load().nmdlm_page_store, what, ptr(k), ptr(v), T, H, dh, ptr(k_pages), ptr(v_pages),
-        ptr(key_counts), stream=stream)
+    what, arg = "nmdlm_page_store", pages._arg
+    rows, pool = T * pages.max_rows * (H * dh // 64), pages.pool * H * T * dh
+    pages._call(load().nmdlm_page_store, what, arg(what, "k", k, rows, 8), arg(what, "v", v, rows, 8), T, H,
+                dh, arg(what, "k_pages", k_pages, pool, 8), arg(what, "v_pages", v_pages, pool, 8),
+                arg(what, "key_counts", key_counts, pool, 1), stream=stream)
 
 
 def nmdlm_page_select(pages: Pages, q, T, H, dh, key_counts, n_sel, sel, ws=None, stream=None) -> None:
-    what = "nmdlm_page_select"
-    pages._need(what, q=(q, *pages._rows(T, H, dh)), key_counts=(key_counts, pages._pool(T, H, dh)[0], 1),
-                sel=(sel, pages.max_rows * H * -(-pages.max_pages // 64), 8), ws=(ws, 1, 1))
-    _on(pages, load().nmdlm_page_select, what, ptr(q), T, H, dh, ptr(key_counts), n_sel, ptr(sel), ptr(ws),
-        0 if ws is None else ws.numel(), stream=stream)
+    what, arg = "nmdlm_page_select", pages._arg
+    pages._call(load().nmdlm_page_select, what,
+                arg(what, "q", q, T * pages.max_rows * (H * dh // 64), 8), T, H, dh,
+                arg(what, "key_counts", key_counts, pages.pool * H * T * dh, 1), n_sel,
+                arg(what, "sel", sel, pages.max_rows * H * pages.words, 8), arg(what, "ws", ws, 1, 1),
+                0 if ws is None else ws.numel(), stream=stream)
 
 
 def nmdlm_page_select_workspace_size(pages: Pages, T, H, dh) -> int:
@@ -446,15 +451,14 @@ def nmdlm_page_select_workspace_size(pages: Pages, T, H, dh) -> int:
 
 def nmdlm_bbm_attn_paged(pages: Pages, q, T, H, dh, k_pages, v_pages, lut_att, a_out=None, theta_a=0,
                          s_out=None, sel=None, ws=None, stream=None) -> None:
-    what = "nmdlm_bbm_attn_paged"
-    rows, pool = pages._rows(T, H, dh), pages._pool(T, H, dh)
-    pages._need(what, q=(q, *rows), k_pages=(k_pages, *pool), v_pages=(v_pages, *pool),
-                lut_att=(lut_att, 256, 1), a_out=(a_out, T * pages.max_rows * H * dh, 4),
-                s_out=(s_out, *rows), sel=(sel, pages.max_rows * H * -(-pages.max_pages // 64), 8),
-                ws=(ws, 1, 1))
-    _on(pages, load().nmdlm_bbm_attn_paged, what, ptr(q), T, H, dh, ptr(k_pages), ptr(v_pages),
-        ptr(lut_att), ptr(sel), ptr(a_out), theta_a, ptr(s_out), ptr(ws),
-        0 if ws is None else ws.numel(), stream=stream)
+    what, arg = "nmdlm_bbm_attn_paged", pages._arg
+    rows, pool = T * pages.max_rows * (H * dh // 64), pages.pool * H * T * dh
+    pages._call(load().nmdlm_bbm_attn_paged, what, arg(what, "q", q, rows, 8), T, H, dh,
+                arg(what, "k_pages", k_pages, pool, 8), arg(what, "v_pages", v_pages, pool, 8),
+                arg(what, "lut_att", lut_att, 256, 1),
+                arg(what, "sel", sel, pages.max_rows * H * pages.words, 8),
+                arg(what, "a_out", a_out, rows * 64, 4), theta_a, arg(what, "s_out", s_out, rows, 8),
+                arg(what, "ws", ws, 1, 1), 0 if ws is None else ws.numel(), stream=stream)
 
 
 def nmdlm_bbm_attn_paged_workspace_size(pages: Pages, T, H, dh) -> int:

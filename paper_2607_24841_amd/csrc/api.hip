@@ -394,7 +394,8 @@ nmdlm_status nmdlm_page_select(const nmdlm_pages* pg, const uint64_t* q, int T, 
   if (rc != NMDLM_OK) return rc;
   if (!q || !aligned(q, 16) || !key_counts || !aligned(key_counts, 16) || !sel || n_sel < 0)
     return NMDLM_ERR_INVALID_ARG;
-  if (!ws || !aligned(ws, 256) || ws_bytes < page_select_ws(*pg, H)) return NMDLM_ERR_WORKSPACE;
+  const size_t need = page_select_ws(*pg, H);
+  if (need > 0 && (!ws || !aligned(ws, 256) || ws_bytes < need)) return NMDLM_ERR_WORKSPACE;
   return launch_page_select(*pg, q, T, H, dh, key_counts, n_sel, sel, ws, static_cast<hipStream_t>(stream));
 }
 

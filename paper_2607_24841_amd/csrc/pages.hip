@@ -304,9 +304,14 @@ nmdlm_status launch_page_store(const nmdlm_pages& pg, const uint64_t* k, const u
 
 // ---------------------------------------------------------------------------
 // Select, scores.  S = Q . counts over T*dh channels on v_mfma_i32_16x16x64_i8
-// (counts are at most 64, query bits 0 or 1: exact): A = 16 pages, row = page,
-// B = the tile's 16 queries.  Lane (g, c) holds channels 16g .. 16g+15 of page c
-// and of query c, and gets pages 4g + e of query c.
+// (counts are at most 64, query bits 0 or 1: exact): A = 16 queries, B = 16
+// pages; lane (g, c) holds channels 16g .. 16g+15 of query c and of page c and
+// gets queries 4g + e of page c.
+//
+// The counts of a page are one run of T*dh bytes.  Loaded as the operand wants
+// them, adjacent lanes read different pages and a load costs 64 cache accesses;
+// so four lanes take 64 bytes of one page and the operands come from LDS.  Query
+// bits come from LDS too, where a workgroup's rows stand once.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ v4i bits_to_bytes(uint32_t x) {  // byte j of 16 = bit j
   v4i r;
@@ -315,108 +320,329 @@ __device__ __forceinline__ v4i bits_to_bytes(uint32_t x) {  // byte j of 16 = bi
   return r;
 }
 
-template <int DHW>
-__global__ __launch_bounds__(256) void k_page_scores(const PageTile* __restrict__ tiles,
-                                                     const int32_t* __restrict__ table, int max_pages,
-                                                     int pool, const uint64_t* __restrict__ q, int T, int H,
-                                                     int max_rows, const uint8_t* __restrict__ counts,
-                                                     int32_t* __restrict__ scores, int ld) {
-  typedef const uint16_t __attribute__((may_alias)) u16_in;
-  typedef const v4i __attribute__((may_alias)) v4i_in;
-  const PageTile tl = tiles[blockIdx.x];
-  if ((tl.n_full & 63) == 0) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
-  const int h = blockIdx.y, P = tl.n_full >> 6, nr = tl.n_full & 63;
-  const int p0 = ((int)blockIdx.z * 4 + wave) * 16;
-  if (p0 >= P) return;
-  const int id = table[(size_t)tl.s * max_pages + min(p0 + c, P - 1)];
-  const bool there = (unsigned)id < (unsigned)pool;
-  const uint8_t* cp = counts + ((size_t)(there ? id : 0) * H + h) * T * (64 * DHW) + 16 * g;
-  const uint64_t* qp = q + (size_t)(tl.row + min(c, nr - 1)) * (H * DHW) + h * DHW;
-  v4i s = v4i{0, 0, 0, 0};
-  for (int t = 0; t < T; ++t)
-#pragma unroll
-    for (int w = 0; w < DHW; ++w) {
-      v4i x = *reinterpret_cast<v4i_in*>(cp + (t * DHW + w) * 64);
-      if (!there) x = v4i{0, 0, 0, 0};
-      const uint32_t b = reinterpret_cast<u16_in*>(qp + (size_t)t * max_rows * (H * DHW) + w)[g];
-      s = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, bits_to_bytes(b), s, 0, 0, 0);
-    }
-  if (c < nr)
-    *reinterpret_cast<v4i*>(scores + ((size_t)(tl.row + c) * H + h) * ld + p0 + 4 * g) = s;
+struct SelectArgs {
+  const PageTile* tiles;
+  const int32_t* table;
+  const uint64_t* q;
+  const uint8_t* counts;
+  uint64_t* sel;
+  int32_t* scores;  // [max_rows][H][ld], where they do not stay in LDS
+  int max_pages, pool, max_rows, words;
+  int T, H, n_sel, ld;
+};
+
+constexpr int kScoreSteps = 8;                     // k-steps (of 64 channels) staged at once
+constexpr int kScoreLd = kScoreSteps * 4 + 1;      // 16-byte units of a staged page (one of padding)
+
+struct ScoreStage {
+  v4i x[16 * kScoreLd];  // of one wave
+};
+
+// The query bits of the tile's rows, [T][ROWS][DHW] words (rows past the last:
+// the last).  All threads of the workgroup.
+template <int DHW, int ROWS>
+__device__ __forceinline__ void stage_queries(const SelectArgs& a, const PageTile& tl, int h,
+                                              uint64_t* sQ) {
+  const int nr = tl.n_full & 63;
+  for (int i = threadIdx.x; i < a.T * ROWS * DHW; i += blockDim.x) {
+    const int w = i % DHW, r = (i / DHW) % ROWS, t = i / (DHW * ROWS);
+    sQ[i] = a.q[((size_t)t * a.max_rows + tl.row + min(r, nr - 1)) * (a.H * DHW) + h * DHW + w];
+  }
 }
 
-// Select, choice: a wave per row and head.  The n_sel-th largest score is built
-// bit by bit from the top (counting the scores that reach each candidate); the
-// pages above it are taken, and of those equal to it the lowest.
-__global__ __launch_bounds__(256) void k_page_pick(const PageTile* __restrict__ tiles, int H, int n_sel,
-                                                   const int32_t* __restrict__ scores, int ld, int words,
-                                                   uint64_t* __restrict__ sel) {
-  const PageTile tl = tiles[blockIdx.x];
-  if ((tl.n_full & 63) == 0) return;
-  const int h = blockIdx.y, lane = threadIdx.x & 63;
-  const int P = tl.n_full >> 6, nr = tl.n_full & 63, nP = (tl.keys + 63) / 64;
-  for (int r = threadIdx.x >> 6; r < nr; r += 4) {  // wave-uniform
-    const size_t at = (size_t)(tl.row + r) * H + h;
-    const int32_t* sc = scores + at * ld;
-    int thr = 0, take = 0;  // scores above thr, and the first `take` equal ones
-    if (n_sel >= P) {
-      thr = -1;
-    } else if (n_sel > 0) {
-      for (int bit = 1 << 16; bit > 0; bit >>= 1) {  // scores are at most 8*128*64 = 2^16
-        int n = 0;
-        for (int p = lane; p < P; p += 64) n += sc[p] >= (thr | bit) ? 1 : 0;
-        for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
-        if (n >= n_sel) thr |= bit;
+// The pool page of the lane's four among 16 logical pages from p0 on.
+__device__ __forceinline__ int score_id(const SelectArgs& a, const PageTile& tl, int p0, int lane) {
+  return a.table[(size_t)tl.s * a.max_pages + max(min(p0 + (lane >> 2), (tl.n_full >> 6) - 1), 0)];
+}
+
+// Scores of 16 pages and QG groups of 16 rows.  The loads of a round of
+// k-steps are all issued before the first is used.
+template <int DHW, int QG>
+__device__ __forceinline__ void score_pages(const SelectArgs& a, int id, int h, int lane, const uint64_t* sQ,
+                                            ScoreStage& st, v4i (&s)[QG]) {
+  typedef const v4i __attribute__((may_alias)) v4i_in;
+  typedef const uint16_t __attribute__((may_alias)) u16_in;
+  const int g = lane >> 4, c = lane & 15;
+  const bool there = (unsigned)id < (unsigned)a.pool;
+  const uint8_t* cp = a.counts + ((size_t)(there ? id : 0) * a.H + h) * a.T * (64 * DHW) + 16 * (lane & 3);
+  const int steps = a.T * DHW;
+#pragma unroll
+  for (int u = 0; u < QG; ++u) s[u] = v4i{0, 0, 0, 0};
+  for (int k0 = 0; k0 < steps; k0 += kScoreSteps) {  // uniform
+    v4i x[kScoreSteps];
+#pragma unroll
+    for (int k = 0; k < kScoreSteps; ++k)
+      x[k] = *reinterpret_cast<v4i_in*>(cp + min(k0 + k, steps - 1) * 64);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < kScoreSteps; ++k)
+      st.x[(lane >> 2) * kScoreLd + k * 4 + (lane & 3)] = there ? x[k] : v4i{0, 0, 0, 0};
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int k = 0; k < kScoreSteps; ++k) {
+      if (k0 + k >= steps) break;  // uniform
+      const int t = (k0 + k) / DHW, w = (k0 + k) % DHW;
+      const v4i y = st.x[c * kScoreLd + k * 4 + g];
+#pragma unroll
+      for (int u = 0; u < QG; ++u) {
+        const uint32_t b =
+            reinterpret_cast<u16_in*>(sQ + (t * (16 * QG) + 16 * u + c) * DHW + w)[g];
+        s[u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(bits_to_bytes(b), y, s[u], 0, 0, 0);
       }
-      int above = 0;
-      for (int p = lane; p < P; p += 64) above += sc[p] > thr ? 1 : 0;
-      for (int o = 32; o > 0; o >>= 1) above += __shfl_xor(above, o);
-      take = n_sel - above;
-    } else {
-      thr = 1 << 30;
     }
-    for (int w = 0; w < words; ++w) {
-      const int p = w * 64 + lane;
-      const int s = p < P ? sc[p] : -2;
-      const uint64_t own = __builtin_amdgcn_ballot_w64(p >= P && p < nP);
-      uint64_t eq = __builtin_amdgcn_ballot_w64(s == thr);
-      uint64_t word = __builtin_amdgcn_ballot_w64(s > thr) | own;
-      // the lowest `take` of the equal ones
-      const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(eq >> 32),
-                                                   __builtin_amdgcn_mbcnt_lo((uint32_t)eq, 0));
-      word |= __builtin_amdgcn_ballot_w64(s == thr && before < take);
-      take = max(take - (int)__popcll(eq), 0);
-      if (lane == 0) sel[at * words + w] = word;
+    __builtin_amdgcn_wave_barrier();  // the stage is read before the next round's stores
+  }
+}
+
+// Tiles of 32 rows, so that a block's rows read the counts once; a wave per 16
+// pages.
+template <int DHW>
+__global__ __launch_bounds__(256) void k_page_scores(SelectArgs a) {
+  touch_kernargs<sizeof(SelectArgs)>();
+  __shared__ ScoreStage sStage[4];
+  __shared__ uint64_t sQ[NMDLM_MAX_T * 32 * DHW];
+  const PageTile tl = a.tiles[blockIdx.x];
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, h = blockIdx.y;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int nr = tl.n_full & 63, P = tl.n_full >> 6;
+  if (nr == 0 || (int)blockIdx.z * 64 >= P) return;  // uniform
+  const int p0 = ((int)blockIdx.z * 4 + wave) * 16;
+  const int id = score_id(a, tl, p0, lane);
+  stage_queries<DHW, 32>(a, tl, h, sQ);
+  __syncthreads();
+  if (p0 >= P) return;  // wave-uniform
+  v4i s[2];
+  score_pages<DHW, 2>(a, id, h, lane, sQ, sStage[wave], s);
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = 16 * u + 4 * g + e;
+      if (r < nr) a.scores[((size_t)(tl.row + r) * a.H + h) * a.ld + p0 + c] = s[u][e];
+    }
+}
+
+// Select, choice: a wave per row and head.  The scores stand in registers (score
+// p in lane p % 64, register p / 64); the n_sel-th largest is found by bisection
+// between the smallest and the largest, and often earlier:
+// where exactly n_sel scores reach the middle.  Of the scores equal to the last
+// one taken the lowest pages are taken.
+
+// The largest value of a wave: within rows of 16 lanes, then across them.
+__device__ __forceinline__ int wave_max(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x111, 0xf, 0xf, false));  // row_shr:1
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x112, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x114, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x118, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x142, 0xf, 0xf, false));  // row_bcast:15
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x143, 0xf, 0xf, false));  // row_bcast:31
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
+__device__ __forceinline__ int wave_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
+struct Pick {
+  int thr, ties;  // scores above thr, and the first `ties` equal to it
+};
+template <int NR>
+__device__ __forceinline__ Pick pick_threshold(const int (&s)[NR], int P, int n_sel) {
+  if (n_sel >= P) return Pick{-1, 0};  // every page (lanes past the last hold -1)
+  if (n_sel == 0) return Pick{1 << 30, 0};
+  int lo = 1 << 30, hi = 0;
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    lo = min(lo, s[r] < 0 ? 1 << 30 : s[r]);
+    hi = max(hi, s[r]);
+  }
+  lo = -wave_max(-lo);
+  hi = wave_max(hi) + 1;
+  int above = 0;  // scores >= hi; scores >= lo are at least n_sel
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    int n = 0;
+#pragma unroll
+    for (int r = 0; r < NR; ++r) n += s[r] >= mid ? 1 : 0;
+    n = wave_sum(n);
+    if (n == n_sel) return Pick{mid - 1, 0};
+    if (n > n_sel) {
+      lo = mid;
+    } else {
+      hi = mid;
+      above = n;
     }
   }
+  return Pick{lo, n_sel - above};
+}
+
+// lanes below this one whose bit is set
+__device__ __forceinline__ int bits_before(uint64_t m) {
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
+
+// The word of 64 pages whose scores the lanes hold; takes its ties off.
+__device__ __forceinline__ uint64_t pick_word(int s, int thr, int& ties, int p, int P, int nP) {
+  uint64_t word = __builtin_amdgcn_ballot_w64(s > thr || (p >= P && p < nP));
+  if (ties > 0) {  // wave-uniform
+    const uint64_t eq = __builtin_amdgcn_ballot_w64(s == thr);
+    word |= __builtin_amdgcn_ballot_w64(s == thr && bits_before(eq) < ties);
+    ties -= min((int)__popcll(eq), ties);
+  }
+  return word;
+}
+
+template <int NR>
+__device__ __forceinline__ void pick_row(const int32_t* sc, int P, int nP, int n_sel, int words,
+                                         uint64_t* __restrict__ out, int lane) {
+  int s[NR];
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    const int p = r * 64 + lane, x = sc[max(min(p, P - 1), 0)];
+    s[r] = p < P ? x : -1;
+  }
+  Pick k = pick_threshold<NR>(s, P, n_sel);
+  uint64_t mine = 0;
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    const uint64_t w = pick_word(s[r], k.thr, k.ties, r * 64 + lane, P, nP);
+    if (lane == r) mine = w;
+  }
+  // words past the scores': the request's own pages, or none
+  for (int w = lane; w < words; w += 64) {
+    uint64_t x = mine;
+    if (w >= NR) {
+      const int a = max(P - w * 64, 0), b = min(nP - w * 64, 64);
+      x = a < b ? ((b < 64 ? 1ull << b : 0ull) - (1ull << a)) : 0ull;
+    }
+    out[w] = x;
+  }
+}
+
+// The same with the scores read again in every round, for contexts of more
+// pages than the registers hold.
+__device__ void pick_row_long(const int32_t* sc, int P, int nP, int n_sel, int words,
+                              uint64_t* __restrict__ out, int lane) {
+  int thr = n_sel > 0 ? 0 : 1 << 30, ties = 0;
+  if (n_sel >= P) {
+    thr = -1;
+  } else if (n_sel > 0) {
+    for (int bit = 1 << 16; bit > 0; bit >>= 1) {  // scores are at most 8*128*64 = 2^16
+      int n = 0;
+      for (int p = lane; p < P; p += 64) n += sc[p] >= (thr | bit) ? 1 : 0;
+      for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
+      if (n >= n_sel) thr |= bit;
+    }
+    int above = 0;
+    for (int p = lane; p < P; p += 64) above += sc[p] > thr ? 1 : 0;
+    for (int o = 32; o > 0; o >>= 1) above += __shfl_xor(above, o);
+    ties = n_sel - __builtin_amdgcn_readfirstlane(above);
+  }
+  for (int w = 0; w < words; ++w) {
+    const int p = w * 64 + lane;
+    const uint64_t word = pick_word(p < P ? sc[p] : -2, thr, ties, p, P, nP);
+    if (lane == 0) out[w] = word;
+  }
+}
+
+__device__ __forceinline__ void pick_any(const int32_t* sc, int P, int nP, int n_sel, int words,
+                                         uint64_t* __restrict__ out, int lane) {
+  if (P <= 128) pick_row<2>(sc, P, nP, n_sel, words, out, lane);
+  else if (P <= 512) pick_row<8>(sc, P, nP, n_sel, words, out, lane);
+  else if (P <= 2048) pick_row<32>(sc, P, nP, n_sel, words, out, lane);
+  else pick_row_long(sc, P, nP, n_sel, words, out, lane);
+}
+
+__global__ __launch_bounds__(256) void k_page_pick(SelectArgs a) {
+  touch_kernargs<sizeof(SelectArgs)>();
+  const PageTile tl = a.tiles[blockIdx.x];
+  const int r = __builtin_amdgcn_readfirstlane((int)blockIdx.z * 4 + ((int)threadIdx.x >> 6));
+  if (r >= (tl.n_full & 63)) return;  // wave-uniform
+  const size_t at = (size_t)(tl.row + r) * a.H + blockIdx.y;
+  pick_any(a.scores + at * a.ld, tl.n_full >> 6, (tl.keys + 63) / 64, a.n_sel, a.words, a.sel + at * a.words,
+           threadIdx.x & 63);
 }
 
 static int select_ld(const nmdlm_pages& pg) { return (pg.max_pages + 15) / 16 * 16; }
 
+// Scores and choice in one kernel, for a tile of 16 rows and a head: the scores
+// of at most kSelectPages pages meet in LDS; a wave per row.
+constexpr int kSelectWaves = 8;
+template <int DHW>
+__global__ __launch_bounds__(64 * kSelectWaves) void k_page_select(SelectArgs a) {
+  touch_kernargs<sizeof(SelectArgs)>();
+  __shared__ ScoreStage sStage[kSelectWaves];
+  __shared__ uint64_t sQ[NMDLM_MAX_T * 16 * DHW];
+  extern __shared__ int32_t sScores[];  // [16][ld]
+  const PageTile tl = a.tiles[blockIdx.x];
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, h = blockIdx.y;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int nr = tl.n_full & 63, P = tl.n_full >> 6;
+  if (nr == 0) return;  // uniform
+  int id = score_id(a, tl, wave * 16, lane);
+  stage_queries<DHW, 16>(a, tl, h, sQ);
+  __syncthreads();
+  for (int p0 = wave * 16; p0 < P; p0 += kSelectWaves * 16) {
+    v4i s[1];
+    const int next = score_id(a, tl, p0 + kSelectWaves * 16, lane);
+    score_pages<DHW, 1>(a, id, h, lane, sQ, sStage[wave], s);
+    id = next;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sScores[(4 * g + e) * a.ld + p0 + c] = s[0][e];
+  }
+  __syncthreads();
+  for (int r = wave; r < nr; r += kSelectWaves) {
+    const size_t at = (size_t)(tl.row + r) * a.H + h;
+    pick_any(sScores + r * a.ld, P, (tl.keys + 63) / 64, a.n_sel, a.words, a.sel + at * a.words, lane);
+  }
+}
+
+// Scores of up to kSelectPages pages stay in LDS (33 KB), where the table is no wider.
+constexpr int kSelectPages = 512;
+
 size_t page_select_ws(const nmdlm_pages& pg, int H) {
+  if (pg.max_pages <= kSelectPages) return 0;
   return align_up((size_t)pg.max_rows * H * select_ld(pg) * sizeof(int32_t), 256);
+}
+
+template <int DHW>
+static nmdlm_status launch_select(const nmdlm_pages& pg, const uint64_t* q, int T, int H,
+                                  const uint8_t* counts, int n_sel, uint64_t* sel, void* ws,
+                                  hipStream_t st) {
+  PageIndex ix;
+  page_index_layout(pg.n_seq, pg.max_rows, pg.index, &ix);
+  SelectArgs a{ix.t16, pg.table, q, counts, sel, static_cast<int32_t*>(ws), pg.max_pages, pg.pool,
+               pg.max_rows, (pg.max_pages + 63) / 64, T, H, n_sel, select_ld(pg)};
+  if (pg.max_pages <= kSelectPages) {
+    a.ld += 1;  // a row's bank past the row before's
+    const size_t lds = (size_t)a.ld * 16 * sizeof(int32_t);
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(&k_page_select<DHW>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+      return NMDLM_ERR_HIP;
+    hipLaunchKernelGGL(k_page_select<DHW>, dim3(ix.n16, H), dim3(64 * kSelectWaves), lds, st, a);
+    return hip_status();
+  }
+  a.tiles = ix.t32;
+  hipLaunchKernelGGL(k_page_scores<DHW>, dim3(ix.n32, H, (pg.max_pages + 63) / 64), dim3(256), 0, st, a);
+  const nmdlm_status rc = hip_status();
+  if (rc != NMDLM_OK) return rc;
+  hipLaunchKernelGGL(k_page_pick, dim3(ix.n32, H, 8), dim3(256), 0, st, a);
+  return hip_status();
 }
 
 nmdlm_status launch_page_select(const nmdlm_pages& pg, const uint64_t* q, int T, int H, int dh,
                                 const uint8_t* counts, int n_sel, uint64_t* sel, void* ws,
                                 hipStream_t st) {
-  PageIndex ix;
-  page_index_layout(pg.n_seq, pg.max_rows, pg.index, &ix);
-  const int ld = select_ld(pg);
-  int32_t* scores = static_cast<int32_t*>(ws);
-  const dim3 grid((unsigned)ix.n16, (unsigned)H, (unsigned)((pg.max_pages + 63) / 64));
-  if (dh == 64)
-    hipLaunchKernelGGL(k_page_scores<1>, grid, dim3(256), 0, st, ix.t16, pg.table, pg.max_pages, pg.pool, q,
-                       T, H, pg.max_rows, counts, scores, ld);
-  else
-    hipLaunchKernelGGL(k_page_scores<2>, grid, dim3(256), 0, st, ix.t16, pg.table, pg.max_pages, pg.pool, q,
-                       T, H, pg.max_rows, counts, scores, ld);
-  const nmdlm_status rc = hip_status();
-  if (rc != NMDLM_OK) return rc;
-  hipLaunchKernelGGL(k_page_pick, dim3((unsigned)ix.n16, (unsigned)H), dim3(256), 0, st, ix.t16, H, n_sel,
-                     scores, ld, (pg.max_pages + 63) / 64, sel);
-  return hip_status();
+  return dh == 64 ? launch_select<1>(pg, q, T, H, counts, n_sel, sel, ws, st)
+                  : launch_select<2>(pg, q, T, H, counts, n_sel, sel, ws, st);
 }
 
 }  // namespace nmdlm

@@ -88,9 +88,12 @@ def test_pointers():
         assert select(**{name: FAKE + 8}) == INVALID, name
     assert select(sel=None) == INVALID
     assert select(n_sel=-1) == INVALID
-    assert select(ws=None) == WORKSPACE
-    assert select(ws=FAKE + 16) == WORKSPACE
-    assert select(ws_bytes=B.load().nmdlm_page_select_workspace_size(C.byref(pages()), 4, 2, 64) - 1) == WORKSPACE
+    wide = pages(max_pages=2000)
+    need = B.load().nmdlm_page_select_workspace_size(C.byref(wide), 4, 2, 64)
+    assert need > 0
+    assert select(wide, ws=None) == WORKSPACE
+    assert select(wide, ws=FAKE + 16) == WORKSPACE
+    assert select(wide, ws_bytes=need - 1) == WORKSPACE
     for name in ("q", "kp", "vp"):
         assert attn(**{name: None}) == INVALID, name
         assert attn(**{name: FAKE + 8}) == INVALID, name
@@ -127,6 +130,8 @@ def test_binding_checks_its_tensors():
             B.nmdlm_page_store(p, **{**ok, **bad})
     with pytest.raises(B.NmdlmError, match="ctx"):
         B.nmdlm_page_plan(p, torch.zeros(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32))
+    with pytest.raises(B.NmdlmError, match="not on a GPU"):
+        B.nmdlm_page_store(p, **ok)
     with pytest.raises(B.NmdlmError):
         B.Pages(0, 10, 3, 7, device="cpu")
 
