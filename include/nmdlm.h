@@ -534,7 +534,7 @@ size_t nmdlm_block_step_workspace_size(const nmdlm_model* model, int M,
  * such a page count as absent and rows of it are not stored.
  * ------------------------------------------------------------------------ */
 #define NMDLM_PAGE 64
-#define NMDLM_MAX_REQUESTS 65536
+#define NMDLM_MAX_REQUESTS 16384
 #define NMDLM_MAX_PLAN_ROWS 524288   /* 2^19 packed rows                        */
 #define NMDLM_MAX_PAGES 131072       /* pages of a request: NMDLM_MAX_KEYS / 64 */
 #define NMDLM_MAX_POOL 33554432      /* pages of a pool (2^25)                  */

@@ -34,7 +34,7 @@ NMDLM_STATUS_TOKEN_CLAMPED = 0x1
 NMDLM_STATUS_PAGES_SHORT = 0x2
 NMDLM_STATUS_BAD_REQUEST = 0x4
 NMDLM_PAGE = 64           # positions of a page
-NMDLM_MAX_REQUESTS = 65536
+NMDLM_MAX_REQUESTS = 16384
 NMDLM_MAX_PLAN_ROWS = 1 << 19
 NMDLM_MAX_PAGES = 1 << 17   # pages of a request
 NMDLM_MAX_POOL = 1 << 25

@@ -44,6 +44,14 @@ __device__ __forceinline__ v4i attn_norm4(v4i num, int den_i) {
   return a;
 }
 
+// One numerator, as attn_norm4 for fewer than 65536 keys and else as attn_norm.
+__device__ __forceinline__ int32_t attn_norm1(int num, int den_i, bool small) {
+  if (!small) return attn_norm(num, den_i);
+  const float den = (float)max(den_i, 1), n = (float)num;
+  const float q = __builtin_truncf(n * (__builtin_amdgcn_rcpf(den) * (256.0f - 0x1p-12f)));
+  return (int)q + (__builtin_fmaf(-q, den, 256.0f * n) >= den ? 1 : 0);
+}
+
 // ---------------------------------------------------------------------------
 // One wave's share of the attention of 16*QG queries of one head and
 // timestep: 64-key chunks, each lane (g = lane/16, c = lane%16).

@@ -9,14 +9,12 @@
 namespace nmdlm {
 
 // ---------------------------------------------------------------------------
-// k_paged_attn: a workgroup takes one tile of 16*QG rows, a head and one of the
-// tile's splits; wave = (timestep, part).  A page is the 64-key chunk of a wave
-// (attn_device.h).  The pages to visit stand in an LDS list: all of the tile's
-// pages, or those that at least one of its rows selected, with one bit per row
-// that sees them (a score that a row does not see weighs 0, byte -128).  The
-// parts of a timestep take the list's entries in turn.
+// Pages of a request go to its splits as contiguous ranges.  A workgroup lists
+// the pages of its range in LDS, kPageList at a time: all of them, or those that
+// one of its rows selected.
 // ---------------------------------------------------------------------------
-constexpr int kPageList = 512;  // entries of the list (a longer one goes in pieces)
+constexpr int kPageList = 256;   // pages of a range that are listed at once
+constexpr int kSplitPages = 8;   // a split has at least this many pages
 
 struct PagedArgs {
   const PageTile* tiles;
@@ -29,22 +27,43 @@ struct PagedArgs {
   int32_t* a_out;
   uint64_t* s_out;
   uint64_t* u_out;
-  int32_t* part;   // sums of the splits [tile][head][split][T][(16*DHW*... ) + 16]
-  int32_t* nsplit; // [tile][head]: splits that hold sums (0, 1: none)
-  int n_tiles, max_pages, pool, max_rows, words;
+  int32_t* part;  // sums of the splits [row][head][split][T][64 DHW + kPartDen]
+  int max_pages, pool, max_rows, words;
   int T, H, parts, splits;
   int32_t theta;
 };
+constexpr int kPartDen = 4;  // the weights' sum behind the channels' sums, and padding
 
 struct PageEntry {
   int id, keys;  // pool page, keys of it that count (0 outside the pool)
 };
 
-constexpr int kPagesPerSplit = 8;  // a split has at least this many pages
-
-// Ints of one split's sums of a timestep: NT tiles of 64 lanes x 4, 16 weights.
+// Splits of a request of nP pages.
+__device__ __forceinline__ int split_count(int splits, int nP) {
+  return min(splits, max(nP / kSplitPages, 1));
+}
+struct PageRange {
+  int p0, p1;
+};
+__device__ __forceinline__ PageRange split_range(int nP, int z, int n) {
+  return PageRange{(int)((long long)nP * z / n), (int)((long long)nP * (z + 1) / n)};
+}
+__device__ __forceinline__ PageEntry page_entry(const PagedArgs& a, const int32_t* tab, int p, int J) {
+  const int id = tab[p];
+  const bool there = (unsigned)id < (unsigned)a.pool;
+  return PageEntry{there ? id : 0, there ? min(64, J - 64 * p) : 0};
+}
 template <int DHW>
-constexpr int part_ints() { return DHW * 4 * 256 + 16; }
+__device__ __forceinline__ int32_t* split_sums(const PagedArgs& a, int row, int h, int z) {
+  return a.part + (((size_t)row * a.H + h) * a.splits + z) * a.T * (64 * DHW + kPartDen);
+}
+// ---------------------------------------------------------------------------
+// k_paged_attn: a workgroup takes one tile of 16*QG rows, a head and one of the
+// tile's splits; wave = (timestep, part).  A page is the 64-key chunk of a wave
+// (attn_device.h).  With a selection an entry of the list has one bit per row
+// that sees the page (a score that a row does not see weighs 0, byte -128).  The
+// parts of a timestep take the list's entries in turn.
+// ---------------------------------------------------------------------------
 
 // One wave's loads of a page: key row `lane`, value words of channels lane (and
 // lane + 64).
@@ -121,11 +140,7 @@ __device__ __forceinline__ v4i normalise(v4i x, int den, bool small) {
   return r;
 }
 
-// Word w of the tile's selections, row lane of it (0 for lanes without a row).
-__device__ __forceinline__ uint64_t sel_word(const PagedArgs& a, int row0, int nr, int h, int w, int lane) {
-  return lane < nr ? a.sel[((size_t)(row0 + lane) * a.H + h) * a.words + w] : 0ull;
-}
-// The rows that see page `lane` of the word (bit per row).
+// The rows that see page `lane` of a word (bit per row): lane r holds row r's word.
 template <int ROWS>
 __device__ __forceinline__ uint32_t seen_by(uint64_t word, int lane) {
   uint32_t m = 0u;
@@ -139,6 +154,52 @@ __device__ __forceinline__ uint32_t seen_by(uint64_t word, int lane) {
   return m;
 }
 
+// Bits [p0, p1) of word w of a page range.
+__device__ __forceinline__ uint64_t range_bits(int w, int p0, int p1) {
+  const int lo = max(p0 - w * 64, 0), hi = min(p1 - w * 64, 64);
+  if (lo >= hi) return 0ull;
+  return (hi < 64 ? (1ull << hi) - 1 : ~0ull) & ~((1ull << lo) - 1);
+}
+
+// Lists the pages [p0, p1) (at most kPageList) that a row of the tile sees, with
+// the rows; returns their number.  Words go to the waves in turn; sCount has a
+// place for each.  All threads of the workgroup; two barriers.
+constexpr int kListWords = kPageList / 64 + 1;  // a range may begin inside a word
+template <int ROWS>
+__device__ __forceinline__ int list_seen(const PagedArgs& a, const int32_t* tab, const PageTile& tl, int h,
+                                         int p0, int p1, PageEntry* sList, uint32_t* sSeen, int* sCount,
+                                         int lane, int wave, int nwaves) {
+  const int w0 = p0 / 64, nr = tl.n_full & 63;
+  uint32_t seen[kListWords];
+  uint64_t any[kListWords];
+#pragma unroll
+  for (int k = 0; k < kListWords; ++k) {
+    const int w = w0 + k;
+    any[k] = 0;
+    seen[k] = 0;
+    if (k % nwaves != wave || w * 64 >= p1) continue;  // wave-uniform
+    const uint64_t word =
+        lane < nr ? a.sel[((size_t)(tl.row + lane) * a.H + h) * a.words + w] & range_bits(w, p0, p1) : 0ull;
+    seen[k] = seen_by<ROWS>(word, lane);
+    any[k] = __builtin_amdgcn_ballot_w64(seen[k] != 0u);
+    if (lane == 0) sCount[k] = (int)__popcll(any[k]);
+  }
+  __syncthreads();
+  int base = 0;
+#pragma unroll
+  for (int k = 0; k < kListWords; ++k) {
+    if ((w0 + k) * 64 >= p1) break;  // uniform
+    if (seen[k] != 0u) {
+      const int at = base + bits_before(any[k]);
+      sList[at] = page_entry(a, tab, (w0 + k) * 64 + lane, tl.keys);
+      sSeen[at] = seen[k];
+    }
+    base += sCount[k];
+  }
+  __syncthreads();
+  return base;
+}
+
 template <int DHW, int QG, bool SEL>
 __global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_attn(PagedArgs a) {
   constexpr int NT = DHW * 4;
@@ -147,18 +208,19 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_attn(PagedArgs a) {
   __shared__ uint32_t sWord[NMDLM_MAX_T][16][2 * DHW];
   __shared__ PageEntry sList[kPageList];
   __shared__ uint32_t sSeen[SEL ? kPageList : 1];
-  __shared__ int sCount[2];
+  __shared__ int sCount[SEL ? kListWords : 1];
   extern __shared__ v4i sNum[];  // the waves' stages, then the sums [T][NT][64]
   AttnStage<DHW>* sStage = reinterpret_cast<AttnStage<DHW>*>(sNum);
 
+  touch_kernargs<sizeof(PagedArgs)>();
   const int nth = blockDim.x, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nwaves = nth >> 6;
   const int g = lane >> 4, c = lane & 15;
-  const int lid = xcd_order(blockIdx.x, gridDim.x);
-  const int ti = lid % a.n_tiles, hz = lid / a.n_tiles, h = hz / a.splits, z = hz - h * a.splits;
-  const PageTile tl = a.tiles[ti];
-  if ((tl.n_full & 63) == 0) return;  // uniform
-  const int nr = tl.n_full & 63, J = tl.keys, nP = (J + 63) / 64;
+  const int h = blockIdx.x, z = blockIdx.y;
+  const PageTile tl = a.tiles[blockIdx.z];
+  const int nr = tl.n_full & 63, J = tl.keys, nP = (J + 63) / 64, splits = split_count(a.splits, nP);
+  if (nr == 0 || z >= splits) return;  // uniform
+  const PageRange pr = split_range(nP, z, splits);
   const int32_t* tab = a.table + (size_t)tl.s * a.max_pages;
   const int np = a.parts, t = wave / np, part = wave - t * np;
   const int dw = a.H * DHW;
@@ -167,60 +229,22 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_attn(PagedArgs a) {
   uint32_t qraw[QG];
   AttnWave<DHW, QG>::load_queries(qraw, a.q + ((size_t)t * a.max_rows + tl.row) * dw + h * DHW, dw, 0,
                                   nr - 1, g, c);
-  // pages to visit
-  int cnt = nP;
-  if constexpr (SEL) {
-    if (tid == 0) sCount[0] = 0;
-    __syncthreads();
-    int mine = 0;
-    for (int w = wave; w * 64 < nP; w += nwaves) {
-      uint64_t x = sel_word(a, tl.row, nr, h, w, lane);
-      for (int o = 32; o > 0; o >>= 1) x |= __shfl_xor((unsigned long long)x, o);
-      if (nP - w * 64 < 64) x &= (1ull << (nP - w * 64)) - 1;
-      mine += (int)__popcll(x);
-    }
-    if (lane == 0 && mine) atomicAdd(&sCount[0], mine);
-    __syncthreads();
-    cnt = sCount[0];
-  }
-  const int splits = min(a.splits, max((cnt + kPagesPerSplit - 1) / kPagesPerSplit, 1));
-  if (z >= splits) return;  // uniform
-  const int e0 = (int)((long long)cnt * z / splits), e1 = (int)((long long)cnt * (z + 1) / splits);
-
   AttnWave<DHW, QG> w;
-  w.init(qraw);
-  fill_lut(sLut, lr, tid, nth);
   const char* lb = reinterpret_cast<const char*>(&sLut);
   AttnStage<DHW>* const st = &sStage[kAttnStages * wave];
   int keys = 0;
 
-  for (int b = e0; b < e1; b += kPageList) {  // uniform
-    const int m = min(e1 - b, kPageList);
-    __syncthreads();  // the list of the piece before is read
+  for (int b = pr.p0; b < pr.p1; b += kPageList) {  // uniform
+    if (b > pr.p0) __syncthreads();  // the list of the piece before is read
+    int m = min(pr.p1 - b, kPageList);
     if constexpr (SEL) {
-      // entries [b, b + m) of the pages seen by a row, ascending: a wave walks all
-      // words' counts and writes the entries of its own
-      int base = 0;
-      for (int wd = 0; wd * 64 < nP; ++wd) {
-        uint64_t word = sel_word(a, tl.row, nr, h, wd, lane);
-        const uint32_t seen = wd * 64 + lane < nP ? seen_by<16 * QG>(word, lane) : 0u;
-        const uint64_t any = __builtin_amdgcn_ballot_w64(seen != 0u);
-        const int at = base - b + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(any >> 32),
-                                                                 __builtin_amdgcn_mbcnt_lo((uint32_t)any, 0));
-        if (wd % nwaves == wave && seen != 0u && at >= 0 && at < m) {
-          const int p = wd * 64 + lane, id = tab[p];
-          const bool there = (unsigned)id < (unsigned)a.pool;
-          sList[at] = PageEntry{there ? id : 0, there ? min(64, J - 64 * p) : 0};
-          sSeen[at] = seen;
-        }
-        base += (int)__popcll(any);
-      }
+      m = list_seen<16 * QG>(a, tab, tl, h, b, b + m, sList, sSeen, sCount, lane, wave, nwaves);
     } else {
-      for (int i = tid; i < m; i += nth) {
-        const int p = b + i, id = tab[p];
-        const bool there = (unsigned)id < (unsigned)a.pool;
-        sList[i] = PageEntry{there ? id : 0, there ? min(64, J - 64 * p) : 0};
-      }
+      for (int i = tid; i < m; i += nth) sList[i] = page_entry(a, tab, b + i, J);
+    }
+    if (b == pr.p0) {
+      w.init(qraw);
+      fill_lut(sLut, lr, tid, nth);
     }
     __syncthreads();
     if (part >= m) continue;  // wave-uniform
@@ -312,18 +336,19 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_attn(PagedArgs a) {
         atomicAdd(reinterpret_cast<int*>(&sNum[(t * NT + n) * 64 + lane]) + e, w.acc[u][n][e]);
     if (g == 0) atomicAdd(&sDen[t][c], w.den[u] + 128 * keys);
     __syncthreads();
-    if (splits > 1) {  // uniform; QG = 1
-      int32_t* o = a.part + ((size_t)(ti * a.H + h) * a.splits + z) * a.T * part_ints<DHW>();
+    if (splits > 1) {  // uniform
       for (int i = tid; i < a.T * NT * 64; i += nth) {
-        const int tt = i / (NT * 64);
-        *reinterpret_cast<v4i*>(o + (size_t)tt * part_ints<DHW>() + (i - tt * NT * 64) * 4) = sNum[i];
+        const int tt = i / (NT * 64), n = (i >> 6) % NT, r = i & 15, lg = (i >> 4) & 3;
+        if (r < rows)
+          *reinterpret_cast<v4i*>(split_sums<DHW>(a, tl.row + 16 * u + r, h, z) +
+                                  (size_t)tt * (64 * DHW + kPartDen) + 16 * n + 4 * lg) = sNum[i];
       }
       for (int i = tid; i < a.T * 16; i += nth)
-        o[(size_t)(i / 16) * part_ints<DHW>() + NT * 256 + i % 16] = sDen[i / 16][i % 16];
-      if (z == 0 && tid == 0) a.nsplit[ti * a.H + h] = splits;
-      return;
+        if (i % 16 < rows)
+          split_sums<DHW>(a, tl.row + 16 * u + i % 16, h, z)[(size_t)(i / 16) * (64 * DHW + kPartDen) + 64 * DHW] =
+              sDen[i / 16][i % 16];
+      continue;
     }
-    if (a.splits > 1 && tid == 0) a.nsplit[ti * a.H + h] = 1;
     if (rows <= 0) continue;  // uniform
     const bool small = J < 65536;
     fire_rows<DHW>(a, sWord, tl.row + 16 * u, min(rows, 16), h, tid, nth, [&](int tt, int n, int l) {
@@ -332,86 +357,251 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_attn(PagedArgs a) {
   }
 }
 
-// k_paged_join: the sums of a tile's splits (integers: any order gives the same),
-// normalised, and the neuron.
+// ---------------------------------------------------------------------------
+// The neuron of one row and head: num(t) is the channel's sum, den(t) the
+// weights' sum; one wave per 64 channels.
+// ---------------------------------------------------------------------------
+template <int DHW, typename N, typename D>
+__device__ __forceinline__ void fire_row(const PagedArgs& a, int row, int h, int w, int lane, bool small, N num,
+                                         D den) {
+  const int dw = a.H * DHW;
+  int V = 0;
+  uint64_t uor = 0;
+  for (int t = 0; t < a.T; ++t) {
+    const int x = attn_norm1(num(t), den(t), small);
+    const size_t at = ((size_t)t * a.max_rows + row) * dw + h * DHW + w;
+    if (a.a_out) a.a_out[at * 64 + lane] = x;
+    V += x;
+    const bool s = V >= a.theta;
+    if (s) V -= a.theta;
+    const uint64_t word = __builtin_amdgcn_ballot_w64(s);
+    uor |= word;
+    if (a.s_out && lane == 0) a.s_out[at] = word;
+  }
+  if (a.u_out && lane == 0) a.u_out[(size_t)row * dw + h * DHW + w] = uor;
+}
+
+// k_paged_join: the sums of a row's splits (integers: any order gives the same)
+// and the neuron.  A workgroup per row and head, a wave per timestep and 64
+// channels.
 template <int DHW>
-__global__ __launch_bounds__(64 * DHW * 4) void k_paged_join(PagedArgs a) {
-  constexpr int NT = DHW * 4;
-  __shared__ uint32_t sWord[NMDLM_MAX_T][16][2 * DHW];
-  const int ti = blockIdx.x % a.n_tiles, h = blockIdx.x / a.n_tiles;
-  const PageTile tl = a.tiles[ti];
-  if ((tl.n_full & 63) == 0) return;
-  const int splits = a.nsplit[ti * a.H + h];
-  if (splits <= 1) return;
-  const int32_t* base = a.part + (size_t)(ti * a.H + h) * a.splits * a.T * part_ints<DHW>();
-  const size_t zs = (size_t)a.T * part_ints<DHW>();
-  const bool small = tl.keys < 65536;
-  fire_rows<DHW>(a, sWord, tl.row, tl.n_full & 63, h, threadIdx.x, blockDim.x, [&](int t, int n, int l) {
-    const int32_t* o = base + (size_t)t * part_ints<DHW>();
-    v4i x = v4i{0, 0, 0, 0};
-    int den = 0;
-    for (int z = 0; z < splits; ++z) {
-      x += *reinterpret_cast<const v4i*>(o + z * zs + (n * 64 + l) * 4);
-      den += o[z * zs + NT * 256 + (l & 15)];
+__global__ __launch_bounds__(64 * NMDLM_MAX_T * DHW) void k_paged_join(PagedArgs a, const PageTile* rows) {
+  constexpr int LD = 64 * DHW + kPartDen;
+  __shared__ int sNum[NMDLM_MAX_T][64 * DHW];
+  __shared__ int sDen[NMDLM_MAX_T];
+  touch_kernargs<sizeof(PagedArgs) + sizeof(void*)>();
+  const int row = blockIdx.x, h = blockIdx.y;
+  const PageTile tl = rows[row];
+  const int n = split_count(a.splits, (tl.keys + 63) / 64);
+  if ((tl.n_full & 63) == 0 || n == 1) return;  // uniform; a single split fired by itself
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int t = wave / DHW, w = wave - t * DHW;
+  const int32_t* base = split_sums<DHW>(a, row, h, 0) + (size_t)t * LD;
+  const size_t ld = (size_t)a.T * LD;
+  int x = 0, den = 0;
+  for (int z0 = 0; z0 < n; z0 += 8) {
+    int v[8], d[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int32_t* p = base + min(z0 + k, n - 1) * ld;
+      v[k] = p[w * 64 + lane];
+      d[k] = p[64 * DHW];
     }
-    return normalise(x, den, small);
-  });
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (z0 + k < n) {  // uniform
+        x += v[k];
+        den += d[k];
+      }
+  }
+  sNum[t][w * 64 + lane] = x;
+  if (w == 0 && lane == 0) sDen[t] = den;
+  __syncthreads();
+  if (wave < DHW)
+    fire_row<DHW>(a, row, h, wave, lane, tl.keys < 65536, [&](int tt) { return sNum[tt][wave * 64 + lane]; },
+                  [&](int tt) { return sDen[tt]; });
+}
+
+// ---------------------------------------------------------------------------
+// k_paged_token: one row, for requests that bring a token or two.  The matrix
+// cores would work for one query of sixteen; here a wave takes its pages bit by
+// bit: lane = key for the scores (popcount of the key's row and the query, which
+// is the same for all lanes), the weight's eight bits become eight 64-key masks
+// by ballots, and with lane = channel
+//     sum_j p_j V[j,c] = sum_b 2^b popcount(mask_b AND word of channel c).
+// About 100 vector instructions a page of 128 channels, no exchange between
+// lanes, and few registers: the loads of kTokenAhead pages are in flight in each
+// of many waves.
+// ---------------------------------------------------------------------------
+constexpr int kTokenAhead = 4;
+
+template <int DHW>
+struct TokenPage {
+  uint64_t k[DHW], v[DHW];  // key row `lane`; channels DHW*lane (and + 1)
+};
+template <int DHW>
+__device__ __forceinline__ TokenPage<DHW> load_token_page(const PagedArgs& a, int id, int h, int t, int lane) {
+  typedef const ulonglong2 __attribute__((may_alias)) pair;
+  const size_t at = (((size_t)id * a.H + h) * a.T + t) * (64 * DHW);
+  TokenPage<DHW> r;
+  if constexpr (DHW == 2) {
+    const ulonglong2 k = reinterpret_cast<pair*>(a.kp + at)[lane], v = reinterpret_cast<pair*>(a.vp + at)[lane];
+    r.k[0] = k.x;
+    r.k[1] = k.y;
+    r.v[0] = v.x;
+    r.v[1] = v.y;
+  } else {
+    r.k[0] = a.kp[at + lane];
+    r.v[0] = a.vp[at + lane];
+  }
+  return r;
+}
+
+template <int DHW, bool SEL>
+__global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_token(PagedArgs a) {
+  constexpr int DH = 64 * DHW;
+  __shared__ uint8_t sLut[256];
+  __shared__ PageEntry sList[kPageList];
+  __shared__ int sNum[NMDLM_MAX_T][DH];
+  __shared__ int sDen[NMDLM_MAX_T];
+  touch_kernargs<sizeof(PagedArgs)>();
+  const int nth = blockDim.x, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nwaves = nth >> 6;
+  const int h = blockIdx.x, z = blockIdx.y, row = blockIdx.z;
+  const PageTile tl = a.tiles[row];
+  const int J = tl.keys, nP = (J + 63) / 64, splits = split_count(a.splits, nP);
+  if ((tl.n_full & 63) == 0 || z >= splits) return;  // uniform
+  const PageRange pr = split_range(nP, z, splits);
+  const int32_t* tab = a.table + (size_t)tl.s * a.max_pages;
+  const int np = a.parts, t = wave / np, part = wave - t * np;
+  const uint64_t* qp = a.q + ((size_t)t * a.max_rows + row) * (a.H * DHW) + h * DHW;
+  uint64_t q[DHW];
+#pragma unroll
+  for (int w = 0; w < DHW; ++w) {
+    const uint64_t x = qp[w];
+    q[w] = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
+           (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x);
+  }
+  for (int i = tid; i < 256; i += nth) sLut[i] = a.lut[i];
+  for (int i = tid; i < a.T * DH; i += nth) (&sNum[0][0])[i] = 0;
+  if (tid < a.T) sDen[tid] = 0;
+
+  int acc[8][DHW], den = 0;
+#pragma unroll
+  for (int b = 0; b < 8; ++b)
+#pragma unroll
+    for (int w = 0; w < DHW; ++w) acc[b][w] = 0;
+
+  for (int b0 = pr.p0; b0 < pr.p1; b0 += kPageList) {  // uniform
+    const int b1 = min(b0 + kPageList, pr.p1);
+    int m = b1 - b0;
+    if (b0 > pr.p0) __syncthreads();  // the list of the piece before is read
+    if constexpr (SEL) {
+      m = 0;
+      const uint64_t* sw = a.sel + ((size_t)row * a.H + h) * a.words;
+      for (int w = b0 / 64; w * 64 < b1; ++w) {
+        const uint64_t word = sw[w] & range_bits(w, b0, b1);
+        if (w % nwaves == wave && ((word >> lane) & 1))
+          sList[m + bits_before(word)] = page_entry(a, tab, w * 64 + lane, J);
+        m += (int)__popcll(word);
+      }
+      m = __builtin_amdgcn_readfirstlane(m);
+    } else {
+      for (int i = tid; i < m; i += nth) sList[i] = page_entry(a, tab, b0 + i, J);
+    }
+    __syncthreads();
+    if (part >= m) continue;  // wave-uniform
+    auto id_of = [&](int i) { return __builtin_amdgcn_readfirstlane(sList[min(i, m - 1)].id); };
+    TokenPage<DHW> pg[kTokenAhead];
+#pragma unroll
+    for (int j = 0; j < kTokenAhead; ++j) pg[j] = load_token_page<DHW>(a, id_of(part + j * np), h, t, lane);
+    for (int i = part; i < m; i += kTokenAhead * np) {
+#pragma unroll
+      for (int j = 0; j < kTokenAhead; ++j) {
+        const int e = i + j * np;
+        if (e < m) {  // wave-uniform
+          const int keys = sList[e].keys;
+          int s = 0;
+#pragma unroll
+          for (int w = 0; w < DHW; ++w) s += (int)__popcll(pg[j].k[w] & q[w]);
+          int p = sLut[s];
+          p = lane < keys ? p : 0;
+          den += p;
+#pragma unroll
+          for (int b = 0; b < 8; ++b) {
+            const uint64_t mask = __builtin_amdgcn_ballot_w64((p >> b) & 1);
+#pragma unroll
+            for (int w = 0; w < DHW; ++w) acc[b][w] += (int)__popcll(pg[j].v[w] & mask);
+          }
+        }
+        pg[j] = load_token_page<DHW>(a, id_of(e + kTokenAhead * np), h, t, lane);
+      }
+    }
+  }
+  den = wave_sum(den);
+  if (lane == 0) atomicAdd(&sDen[t], den);
+#pragma unroll
+  for (int w = 0; w < DHW; ++w) {
+    int x = 0;
+#pragma unroll
+    for (int b = 7; b >= 0; --b) x = 2 * x + acc[b][w];
+    atomicAdd(&sNum[t][DHW * lane + w], x);
+  }
+  __syncthreads();
+  if (splits > 1) {  // uniform
+    int32_t* o = split_sums<DHW>(a, row, h, z);
+    for (int i = tid; i < a.T * DH; i += nth) o[(i / DH) * (DH + kPartDen) + i % DH] = (&sNum[0][0])[i];
+    if (tid < a.T) o[tid * (DH + kPartDen) + DH] = sDen[tid];
+    return;
+  }
+  for (int w = wave; w < DHW; w += nwaves)
+    fire_row<DHW>(a, row, h, w, lane, J < 65536, [&](int tt) { return sNum[tt][w * 64 + lane]; },
+                  [&](int tt) { return sDen[tt]; });
 }
 
 // ---------------------------------------------------------------------------
 // Which grid.
 // ---------------------------------------------------------------------------
 struct PagedRoute {
+  bool token;
   int groups, parts, splits;
 };
 static PagedRoute paged_route(const nmdlm_pages& pg, int T, int H) {
   const long long t16 = pg.max_rows / 16 + pg.n_seq, t32 = pg.max_rows / 32 + pg.n_seq;
-  PagedRoute r{1, T <= 2 ? 4 : (T <= 4 ? 2 : 1), 1};
-  if (pg.max_rows >= 32LL * pg.n_seq && t32 * H * T >= 2048) {
+  PagedRoute r{false, 1, T <= 2 ? 4 : (T <= 4 ? 2 : 1), 1};
+  if (pg.max_rows <= 2LL * pg.n_seq + 8) {
+    r.token = true;
+  } else if (pg.max_rows >= 32LL * pg.n_seq && t32 * H * T >= 2048) {
     r.groups = 2;
     r.parts = 1;
     return r;
   }
-  const long long wgs = t16 * H;
-  if (wgs < 256)
-    r.splits = (int)std::max(1LL, std::min<long long>({(511 + wgs) / wgs, 64, pg.max_pages / kPagesPerSplit}));
+  const long long wgs = (r.token ? pg.max_rows : t16) * (long long)H;
+  if (wgs < 1024)
+    r.splits = (int)std::max(1LL, std::min<long long>({(1023 + wgs) / wgs, 64, pg.max_pages / kSplitPages}));
   return r;
 }
 
-static int32_t* carve_paged(const nmdlm_pages& pg, const PagedRoute& r, int T, int H, int dh, void* ws,
-                            int32_t** nsplit, size_t* bytes) {
-  Carver cv{static_cast<char*>(ws), 0, (size_t)-1, true};
-  int32_t* part = nullptr;
-  *nsplit = nullptr;
-  if (r.splits > 1) {
-    const size_t th = (size_t)(pg.max_rows / 16 + pg.n_seq) * H;
-    *nsplit = cv.take<int32_t>(th);
-    part = cv.take<int32_t>(th * r.splits * T * (dh / 64 * 1024 + 16));
-  }
-  *bytes = align_up(cv.off, 256);
-  return part;
+static size_t part_bytes(const nmdlm_pages& pg, const PagedRoute& r, int T, int H, int dh) {
+  if (r.splits == 1) return 0;
+  return align_up((size_t)pg.max_rows * H * r.splits * T * (dh + kPartDen) * sizeof(int32_t), 256);
 }
 
 size_t paged_attn_ws(const nmdlm_pages& pg, int T, int H, int dh) {
-  int32_t* ns;
-  size_t bytes;
-  carve_paged(pg, paged_route(pg, T, H), T, H, dh, nullptr, &ns, &bytes);
-  return bytes;
+  return part_bytes(pg, paged_route(pg, T, H), T, H, dh);
 }
 
 constexpr size_t kPagedPlainLds = 49152;  // dynamic LDS that needs no attribute beside the static
 
 template <int DHW, int QG, bool SEL>
-static nmdlm_status launch_paged(const PagedArgs& a, int n_wg, hipStream_t st) {
+static nmdlm_status launch_paged(const PagedArgs& a, dim3 grid, hipStream_t st) {
   const size_t dyn = std::max((size_t)a.T * DHW * 4 * 64 * sizeof(v4i),
                               (size_t)a.T * a.parts * kAttnStages * sizeof(AttnStage<DHW>));
-  const auto fn = &k_paged_attn<DHW, QG, SEL>;
   if (dyn > kPagedPlainLds &&
-      hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize,
-                          (int)dyn) != hipSuccess)
+      hipFuncSetAttribute(reinterpret_cast<const void*>(&k_paged_attn<DHW, QG, SEL>),
+                          hipFuncAttributeMaxDynamicSharedMemorySize, (int)dyn) != hipSuccess)
     return NMDLM_ERR_HIP;
-  hipLaunchKernelGGL((k_paged_attn<DHW, QG, SEL>), dim3((unsigned)n_wg), dim3(64 * a.T * a.parts),
-                     (uint32_t)dyn, st, a);
+  hipLaunchKernelGGL((k_paged_attn<DHW, QG, SEL>), grid, dim3(64 * a.T * a.parts), (uint32_t)dyn, st, a);
   return hip_status();
 }
 
@@ -421,8 +611,13 @@ static nmdlm_status launch_paged_dh(const nmdlm_pages& pg, const PagedAttnCall& 
   PageIndex ix;
   page_index_layout(pg.n_seq, pg.max_rows, pg.index, &ix);
   PagedArgs a{};
-  a.n_tiles = r.groups == 2 ? ix.n32 : ix.n16;
-  a.tiles = r.groups == 2 ? ix.t32 : ix.t16;
+  // heads first: where H is a multiple of 8 the tiles of a head share an XCD, and
+  // the list's empty entries are the last
+  const unsigned n_tiles = r.token ? pg.max_rows : (r.groups == 2 ? ix.n32 : ix.n16);
+  static_assert(2 * NMDLM_MAX_REQUESTS + 8 < 65536 && NMDLM_MAX_PLAN_ROWS / 16 + NMDLM_MAX_REQUESTS < 65536,
+                "tiles fit a grid's third dimension");
+  const dim3 grid(c.H, r.splits, n_tiles);
+  a.tiles = r.token ? ix.t1 : (r.groups == 2 ? ix.t32 : ix.t16);
   a.table = pg.table;
   a.q = c.q;
   a.kp = c.k_pages;
@@ -432,8 +627,7 @@ static nmdlm_status launch_paged_dh(const nmdlm_pages& pg, const PagedAttnCall& 
   a.a_out = c.a_out;
   a.s_out = c.s_out;
   a.u_out = c.u_out;
-  size_t bytes;
-  a.part = carve_paged(pg, r, c.T, c.H, c.dh, c.ws, &a.nsplit, &bytes);
+  a.part = static_cast<int32_t*>(c.ws);
   a.max_pages = pg.max_pages;
   a.pool = pg.pool;
   a.max_rows = pg.max_rows;
@@ -443,16 +637,19 @@ static nmdlm_status launch_paged_dh(const nmdlm_pages& pg, const PagedAttnCall& 
   a.parts = r.parts;
   a.splits = r.splits;
   a.theta = c.theta;
-  // a launch has fewer than 2^32 threads
-  if ((long long)a.n_tiles * c.H * r.splits * (64 * c.T * r.parts) >= 1LL << 32) return NMDLM_ERR_UNSUPPORTED;
-  const int n_wg = a.n_tiles * c.H * r.splits;
   nmdlm_status rc;
-  if (r.groups == 2)
-    rc = c.sel ? launch_paged<DHW, 2, true>(a, n_wg, st) : launch_paged<DHW, 2, false>(a, n_wg, st);
-  else
-    rc = c.sel ? launch_paged<DHW, 1, true>(a, n_wg, st) : launch_paged<DHW, 1, false>(a, n_wg, st);
+  if (r.token) {
+    const dim3 block(64 * c.T * r.parts);
+    if (c.sel) hipLaunchKernelGGL((k_paged_token<DHW, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_paged_token<DHW, false>), grid, block, 0, st, a);
+    rc = hip_status();
+  } else if (r.groups == 2) {
+    rc = c.sel ? launch_paged<DHW, 2, true>(a, grid, st) : launch_paged<DHW, 2, false>(a, grid, st);
+  } else {
+    rc = c.sel ? launch_paged<DHW, 1, true>(a, grid, st) : launch_paged<DHW, 1, false>(a, grid, st);
+  }
   if (rc != NMDLM_OK || r.splits == 1) return rc;
-  hipLaunchKernelGGL(k_paged_join<DHW>, dim3((unsigned)(a.n_tiles * c.H)), dim3(64 * DHW * 4), 0, st, a);
+  hipLaunchKernelGGL(k_paged_join<DHW>, dim3(pg.max_rows, c.H), dim3(64 * c.T * DHW), 0, st, a, ix.t1);
   return hip_status();
 }
 

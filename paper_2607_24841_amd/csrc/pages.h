@@ -2,15 +2,48 @@
 // the paged calls.
 #pragma once
 
+#include <algorithm>
+
 #include "common.h"
 
 namespace nmdlm {
+
+// Over a wave, without LDS: within rows of 16 lanes, then across them.
+__device__ __forceinline__ int row_scan(int x) {  // inclusive sums of a row of 16 lanes
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  return x;
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  x = row_scan(x);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31
+  return x;
+}
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
+__device__ __forceinline__ int wave_max(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x111, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x112, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x114, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x118, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x142, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x143, 0xf, 0xf, false));
+  return __builtin_amdgcn_readlane(x, 63);
+}
+// of m, the bits below this lane
+__device__ __forceinline__ int bits_before(uint64_t m) {
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
 
 // What a plan knows of a request once its lengths are checked.
 struct PageReq {
   int32_t first;  // its first page among those taken from the ring, or -1: refused
   int32_t held;   // pages it held before the call
   int32_t ctx, rows;
+  int32_t row;            // first packed row
+  int32_t t16, t32, run;  // first entries in the lists
 };
 // Up to TS rows of one request, for a workgroup that takes TS queries; no rows:
 // no such tile (an index that is all zeros holds none).
@@ -24,30 +57,34 @@ struct PageRun {
   int32_t page, off, row, n;
 };
 
-// The tiles of request s start at entry cu_rows[s]/TS + s: its ceil(rows/TS)
-// tiles fit before those of s + 1, without a prefix sum of their own.  Runs
-// likewise from cu_rows[s]/64 + 2s (rows of r positions lie in at most r/64 + 2
-// pages).  Entries between are marked.
+// The lists are dense: entries past the last are cleared, so that workgroups
+// without work are a grid's last (spread among the others they kept CUs idle
+// that had been given fewer of the working ones).
 struct PageIndex {
-  int32_t* head;   // [4]: ring's first free page and their number before the
-                   // call, pages given back
+  int32_t* head;   // [8]: the ring's first free page and their number before the
+                   // call, pages given back, tiles of 16 and 32 rows, runs
   PageReq* req;    // [n_seq]
   int32_t* back;   // [n_seq]: pages given back before request s
+  PageTile* t1;    // [max_rows]: entry m is row m
   PageTile* t16;   // [n16]
   PageTile* t32;   // [n32]
   PageRun* runs;   // [n_runs]
-  int n16, n32, n_runs;
+  int n16, n32, n_runs;  // entries there is room for
 };
 
+// a request of r rows has at most r/16 + 1 tiles of 16, and its rows lie in at
+// most r/64 + 2 pages
 inline size_t page_index_layout(int n_seq, int max_rows, void* base, PageIndex* ix) {
   Carver cv{static_cast<char*>(base), 0, (size_t)-1, true};
-  ix->n16 = max_rows / 16 + n_seq;
-  ix->n32 = max_rows / 32 + n_seq;
-  ix->n_runs = max_rows / 64 + 2 * n_seq;
+  const int live = std::min(n_seq, max_rows);  // requests with rows
+  ix->n16 = max_rows / 16 + live;
+  ix->n32 = max_rows / 32 + live;
+  ix->n_runs = max_rows / 64 + 2 * live;
   // Carver aligns offsets to 256 bytes of the base
-  ix->head = cv.take<int32_t>(4);
+  ix->head = cv.take<int32_t>(8);
   ix->req = cv.take<PageReq>(n_seq);
   ix->back = cv.take<int32_t>(n_seq);
+  ix->t1 = cv.take<PageTile>(max_rows);
   ix->t16 = cv.take<PageTile>(ix->n16);
   ix->t32 = cv.take<PageTile>(ix->n32);
   ix->runs = cv.take<PageRun>(ix->n_runs);

@@ -8,9 +8,10 @@
 namespace nmdlm {
 
 // ---------------------------------------------------------------------------
-// Plan.  Two steps: the sums over the requests in order (rows, pages taken,
-// pages given back), by one workgroup; then every output entry by itself, its
-// request found by bisection of cu_rows.
+// Plan.  Two steps: sums over the requests in order (rows, pages taken and given
+// back, list entries), by one workgroup; then every row by itself, its request
+// found by bisection of cu_rows.  Latency bound: a chain of dependent loads,
+// scans and barriers.
 // ---------------------------------------------------------------------------
 struct PlanArgs {
   nmdlm_pages pg;
@@ -21,74 +22,87 @@ struct PlanArgs {
 };
 
 constexpr int kPlanThreads = 1024;
+constexpr int kPlanWaves = kPlanThreads / 64;
 
-// Inclusive sums over the workgroup; `total` is the sum of all.
-template <typename V>
-__device__ __forceinline__ V block_scan(V v, V* sWave, V& total) {
-  constexpr int NW = kPlanThreads / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int o = 1; o < 64; o <<= 1) {
-    const V u = __shfl_up(v, o);
-    if (lane >= o) v += u;
+// Inclusive sums of K values over the workgroup, in place; total: the sums of all.
+template <int K>
+__device__ __forceinline__ void block_scan(int (&x)[K], int (&total)[K], int (*sWave)[kPlanWaves]) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    x[k] = wave_scan(x[k]);
+    if (lane == 63) sWave[k][wave] = x[k];
   }
-  if (lane == 63) sWave[wave] = v;
   __syncthreads();
-  V before = 0, all = 0;
-  for (int w = 0; w < NW; ++w) {
-    if (w < wave) before += sWave[w];
-    all += sWave[w];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {  // the waves' sums, one a lane of a row of 16
+    const int y = row_scan(sWave[k][lane & 15]);
+    total[k] = __builtin_amdgcn_readlane(y, 15);
+    if (wave > 0) x[k] += __builtin_amdgcn_readlane(y, wave - 1);
   }
-  __syncthreads();  // sWave is free again
-  total = all;
-  return v + before;
 }
+static_assert(kPlanWaves == 16, "a row of lanes holds the waves' sums");
 
 // A chunk's sums fit 32 bits (1024 requests of at most 2^19 rows, 2^17 pages);
 // the carries between chunks are 64 bits wide.
-__device__ void plan_sums(const PlanArgs& a) {
-  __shared__ int sRows[kPlanThreads / 64];
-  __shared__ unsigned long long sPages[kPlanThreads / 64];
+__device__ void plan_sums(const PlanArgs& a, int32_t* sCu, PageReq* sReq) {
+  __shared__ int sRows[1][kPlanWaves], sPages[2][kPlanWaves], sLists[3][kPlanWaves];
   __shared__ int sTaken;
   const int tid = threadIdx.x, n = a.pg.n_seq, pool = a.pg.pool;
-  const int head = (int)((uint32_t)a.pg.ring_state[0] % (uint32_t)pool);
+  const int first = a.pg.ring_state[0], head = (unsigned)first < (unsigned)pool ? first : 0;
   const int free_pages = min(max(a.pg.ring_state[1], 0), pool);
   long long row_c = 0, need_c = 0, back_c = 0;
+  int t16_c = 0, t32_c = 0, run_c = 0;
   int bits = 0;
   if (tid == 0) sTaken = 0;
-  __syncthreads();
   for (int s0 = 0; s0 < n; s0 += kPlanThreads) {  // uniform
     const int s = s0 + tid;
     const bool in = s < n;
     const int ctx = in ? a.ctx[s] : 0, rows = in ? a.rows[s] : 0, held = in ? a.pg.held[s] : 0;
     const int r = rows > 0 && rows <= a.pg.max_rows ? rows : 0;
-    int r_all;
-    const long long row_end = row_c + block_scan(r, sRows, r_all);
+    int rs[1] = {r}, r_all[1];
+    block_scan<1>(rs, r_all, sRows);
+    const long long row_end = row_c + rs[0];
     const long long end = (long long)ctx + rows;
     const bool held_ok = held >= 0 && held <= a.pg.max_pages;
     const bool fits = in && rows >= 0 && rows <= a.pg.max_rows && held_ok && ctx >= 0 &&
                       ctx <= (long long)held * NMDLM_PAGE &&
                       end <= (long long)a.pg.max_pages * NMDLM_PAGE && row_end <= a.pg.max_rows;
     const bool ended = in && rows == -1 && held_ok;
-    const int pages = fits ? (int)((end + NMDLM_PAGE - 1) / NMDLM_PAGE) : 0;
-    const unsigned need = max(pages - held, 0) * (fits ? 1 : 0), back = ended ? held : 0;
-    unsigned long long p_all;
-    const unsigned long long p =
-        block_scan((unsigned long long)back << 32 | need, sPages, p_all);
-    const long long need_end = need_c + (uint32_t)p, back_end = back_c + (long long)(p >> 32);
+    const int pages = fits ? (int)((end + NMDLM_PAGE - 1) >> 6) : 0;
+    const int need = fits ? max(pages - held, 0) : 0, back = ended ? held : 0;
+    int ps[2] = {need, back}, p_all[2];
+    block_scan<2>(ps, p_all, sPages);
+    const long long need_end = need_c + ps[0], back_end = back_c + ps[1];
     const bool ok = fits && (need == 0 || need_end <= free_pages);
+    // list entries of a served request
+    const int m = ok ? rows : 0;
+    const int n16 = (m + 15) >> 4, n32 = (m + 31) >> 5, n_run = m > 0 ? pages - (ctx >> 6) : 0;
+    int ls[3] = {n16, n32, n_run}, l_all[3];
+    block_scan<3>(ls, l_all, sLists);
     if (in) {
+      const int cu = (int)min(row_end - r, (long long)a.pg.max_rows);
+      const PageReq q{ok ? (int)min(need_end - need, (long long)pool) : -1, held, ctx, rows, cu,
+                      t16_c + ls[0] - n16, t32_c + ls[1] - n32, run_c + ls[2] - n_run};
       a.pg.cu_rows[s + 1] = (int)min(row_end, (long long)a.pg.max_rows);
-      a.ix.req[s] = PageReq{ok ? (int)min(need_end - need, (long long)pool) : -1, held, ctx, rows};
+      a.ix.req[s] = q;
       a.ix.back[s] = (int)min(back_end - back, (long long)pool);
+      if (sCu) {
+        sCu[s + 1] = (int)min(row_end, (long long)a.pg.max_rows);
+        sReq[s] = q;
+      }
       if (ended) a.pg.held[s] = 0;
       else if (ok) a.pg.held[s] = max(held, pages);
       if (!fits && !ended) bits |= NMDLM_STATUS_BAD_REQUEST;
       if (fits && !ok) bits |= NMDLM_STATUS_PAGES_SHORT;
       if (ok && need > 0) atomicMax(&sTaken, (int)need_end);
     }
-    row_c += r_all;
-    need_c += (uint32_t)p_all;
-    back_c += (long long)(p_all >> 32);
+    row_c += r_all[0];
+    need_c += p_all[0];
+    back_c += p_all[1];
+    t16_c += l_all[0];
+    t32_c += l_all[1];
+    run_c += l_all[2];
   }
   if (bits && a.status) atomicOr(a.status, bits);
   __syncthreads();
@@ -96,16 +110,21 @@ __device__ void plan_sums(const PlanArgs& a) {
     // no more than the pool has room for (a table that repeats pages)
     const int back = (int)min(back_c, (long long)(pool - free_pages));
     a.pg.cu_rows[0] = 0;
+    if (sCu) sCu[0] = 0;
     a.ix.head[0] = head;
     a.ix.head[1] = free_pages;
     a.ix.head[2] = back;
-    a.pg.ring_state[0] = (int)(((long long)head + sTaken) % pool);
+    a.ix.head[3] = t16_c;
+    a.ix.head[4] = t32_c;
+    a.ix.head[5] = run_c;
+    const int next = head + sTaken;
+    a.pg.ring_state[0] = next < pool ? next : next - pool;
     a.pg.ring_state[1] = free_pages - sTaken + back;
   }
 }
 
 // The request of packed row m (n: none).
-__device__ __forceinline__ int row_request(const int32_t* __restrict__ cu, int n, int m) {
+__device__ __forceinline__ int row_request(const int32_t* cu, int n, int m) {
   int lo = 0, hi = n;
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
@@ -114,81 +133,55 @@ __device__ __forceinline__ int row_request(const int32_t* __restrict__ cu, int n
   }
   return lo;
 }
-// The request whose entries (from cu[s] >> shift, plus mul s, on) hold entry i.
-__device__ __forceinline__ int entry_request(const int32_t* __restrict__ cu, int n, int i, int shift,
-                                             int mul) {
-  int lo = 0, hi = n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if ((cu[mid] >> shift) + mul * mid <= i) lo = mid;
-    else hi = mid - 1;
-  }
-  return lo;
-}
-
-struct PlanRing {
-  int head, free_pages;
-};
 
 // Pool page of logical page lp of request s (-1 outside the pool): one it held,
 // or one of those taken in this call.
-__device__ __forceinline__ int plan_page(const PlanArgs& a, const PlanRing& g, const PageReq& q, int s,
-                                         int lp) {
+__device__ __forceinline__ int plan_page(const PlanArgs& a, int head, const PageReq& q, int s, int lp) {
   int page;
   if (lp < q.held) {
     page = a.pg.table[(size_t)s * a.pg.max_pages + lp];
   } else {
-    const long long i = (long long)g.head + q.first + (lp - q.held);
+    const int i = head + q.first + (lp - q.held);
     page = a.pg.ring[i < a.pg.pool ? i : i - a.pg.pool];
   }
   return (unsigned)page < (unsigned)a.pg.pool ? page : -1;
 }
 
-__device__ __forceinline__ PageTile plan_tile(const PlanArgs& a, const int32_t* cu, int i, int shift) {
-  const int s = entry_request(cu, a.pg.n_seq, i, shift, 1);
-  const int at = (i - ((cu[s] >> shift) + s)) << shift;
-  const PageReq q = a.ix.req[s];
-  if (q.first < 0 || at >= q.rows) return PageTile{0, 0, 0, 0};
-  return PageTile{s, cu[s] + at, min(q.rows - at, 1 << shift) | (q.ctx / NMDLM_PAGE) << 6, q.ctx + q.rows};
-}
-
-__device__ void plan_entries(const PlanArgs& a, const int32_t* cu, int tid, int nth) {
-  const PlanRing g{a.ix.head[0], a.ix.head[1]};
-  const int n = a.pg.n_seq;
+// Every row writes its slot and position; the first of a tile or of a page's
+// rows writes the list entry and, for a page taken in this call (each has at
+// least one row), the table's.
+__device__ void plan_rows(const PlanArgs& a, const int32_t* cu, const PageReq* req, int tid, int nth) {
+  const int head = a.ix.head[0], n = a.pg.n_seq;
   for (int m = tid; m < a.pg.max_rows; m += nth) {
     const int s = row_request(cu, n, m);
     long long slot = -1;
     int pos = 0;
+    PageTile tl{0, 0, 0, 0};
     if (s < n) {
-      const PageReq q = a.ix.req[s];
+      const PageReq q = req[s];
       if (q.first >= 0) {
-        pos = q.ctx + m - cu[s];
-        const int page = plan_page(a, g, q, s, pos / NMDLM_PAGE);
-        if (page >= 0) slot = (long long)page * NMDLM_PAGE + pos % NMDLM_PAGE;
+        const int i = m - q.row, end = q.ctx + q.rows, full = q.ctx >> 6 << 6;  // all at least 0
+        pos = q.ctx + i;
+        const int lp = pos >> 6, off = pos & 63, page = plan_page(a, head, q, s, lp);
+        if (page >= 0) slot = (long long)page * NMDLM_PAGE + off;
+        tl = PageTile{s, m, 1 | full, end};
+        if ((i & 15) == 0) a.ix.t16[q.t16 + (i >> 4)] = PageTile{s, m, min(q.rows - i, 16) | full, end};
+        if ((i & 31) == 0) a.ix.t32[q.t32 + (i >> 5)] = PageTile{s, m, min(q.rows - i, 32) | full, end};
+        if (i == 0 || off == 0) {
+          a.ix.runs[q.run + lp - (q.ctx >> 6)] = PageRun{page, off, m, min(NMDLM_PAGE - off, end - pos)};
+          if (lp >= q.held) a.pg.table[(size_t)s * a.pg.max_pages + lp] = page;
+        }
       }
     }
     a.pg.slot[m] = slot;
     a.pg.pos[m] = pos;
+    a.ix.t1[m] = tl;
   }
-  for (int i = tid; i < a.ix.n16; i += nth) a.ix.t16[i] = plan_tile(a, cu, i, 4);
-  for (int i = tid; i < a.ix.n32; i += nth) a.ix.t32[i] = plan_tile(a, cu, i, 5);
-  for (int i = tid; i < a.ix.n_runs; i += nth) {
-    const int s = entry_request(cu, n, i, 6, 2);
-    const PageReq q = a.ix.req[s];
-    PageRun r{-1, 0, 0, 0};
-    if (q.first >= 0) {
-      const int lp = q.ctx / NMDLM_PAGE + (i - ((cu[s] >> 6) + 2 * s));
-      const int b = max(q.ctx, lp * NMDLM_PAGE), e = min(q.ctx + q.rows, (lp + 1) * NMDLM_PAGE);
-      if (b < e) {
-        r = PageRun{plan_page(a, g, q, s, lp), b - lp * NMDLM_PAGE, cu[s] + b - q.ctx, e - b};
-        // a page taken in this call has at least one of its rows
-        if (lp >= q.held) a.pg.table[(size_t)s * a.pg.max_pages + lp] = r.page;
-      }
-    }
-    a.ix.runs[i] = r;
-  }
+  for (int i = a.ix.head[3] + tid; i < a.ix.n16; i += nth) a.ix.t16[i] = PageTile{0, 0, 0, 0};
+  for (int i = a.ix.head[4] + tid; i < a.ix.n32; i += nth) a.ix.t32[i] = PageTile{0, 0, 0, 0};
+  for (int i = a.ix.head[5] + tid; i < a.ix.n_runs; i += nth) a.ix.runs[i] = PageRun{-1, 0, 0, 0};
   // pages of ended requests, behind the ring's last
-  const int back = a.ix.head[2];
+  const int back = a.ix.head[2], free_pages = a.ix.head[1];
   for (int i = tid; i < back; i += nth) {
     int lo = 0, hi = n - 1;
     while (lo < hi) {
@@ -196,29 +189,47 @@ __device__ void plan_entries(const PlanArgs& a, const int32_t* cu, int tid, int 
       if (a.ix.back[mid] <= i) lo = mid;
       else hi = mid - 1;
     }
-    const long long at = (long long)g.head + g.free_pages + i;  // below 3 pool
-    a.pg.ring[at % a.pg.pool] = a.pg.table[(size_t)lo * a.pg.max_pages + (i - a.ix.back[lo])];
+    int at = head + free_pages + i;  // below 3 pool
+    while (at >= a.pg.pool) at -= a.pg.pool;
+    a.pg.ring[at] = a.pg.table[(size_t)lo * a.pg.max_pages + (i - a.ix.back[lo])];
   }
 }
 
+// One launch for few rows and requests: what the rows look up stays in LDS.
+constexpr int kPlanOneRows = 4096;
 __global__ __launch_bounds__(kPlanThreads) void k_page_plan(PlanArgs a) {
-  plan_sums(a);
+  __shared__ int32_t sCu[kPlanThreads + 1];
+  __shared__ PageReq sReq[kPlanThreads];
+  touch_kernargs<sizeof(PlanArgs)>();
+  plan_sums(a, sCu, sReq);
   __syncthreads();
-  plan_entries(a, a.pg.cu_rows, threadIdx.x, kPlanThreads);
-}
-__global__ __launch_bounds__(kPlanThreads) void k_page_sums(PlanArgs a) { plan_sums(a); }
-__global__ __launch_bounds__(256) void k_page_entries(PlanArgs a) {
-  plan_entries(a, a.pg.cu_rows, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+  plan_rows(a, sCu, sReq, threadIdx.x, kPlanThreads);
 }
 
-constexpr long long kPlanOneEntries = 4 * kPlanThreads;  // entries of a plan in one launch
+// Two for many.
+constexpr int kPlanLdsRequests = 4096;  // bisection in LDS up to these
+__global__ __launch_bounds__(kPlanThreads) void k_page_sums(PlanArgs a) {
+  touch_kernargs<sizeof(PlanArgs)>();
+  plan_sums(a, nullptr, nullptr);
+}
+__global__ __launch_bounds__(256) void k_page_rows(PlanArgs a) {
+  __shared__ int32_t sCu[kPlanLdsRequests + 1];
+  touch_kernargs<sizeof(PlanArgs)>();
+  const int n = a.pg.n_seq;
+  const int32_t* cu = a.pg.cu_rows;
+  if (n <= kPlanLdsRequests) {  // uniform
+    for (int i = threadIdx.x; i <= n; i += 256) sCu[i] = cu[i];
+    __syncthreads();
+    cu = sCu;
+  }
+  plan_rows(a, cu, a.ix.req, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+}
 
 nmdlm_status launch_page_plan(const nmdlm_pages& pg, const int32_t* ctx, const int32_t* rows,
                               int32_t* status, hipStream_t st) {
   PlanArgs a{pg, ctx, rows, status, {}};
   page_index_layout(pg.n_seq, pg.max_rows, pg.index, &a.ix);
-  const long long entries = (long long)pg.max_rows + a.ix.n16 + a.ix.n32 + a.ix.n_runs;
-  if (entries <= kPlanOneEntries) {
+  if (pg.max_rows <= kPlanOneRows && pg.n_seq <= kPlanThreads) {
     hipLaunchKernelGGL(k_page_plan, dim3(1), dim3(kPlanThreads), 0, st, a);
     return hip_status();
   }
@@ -226,7 +237,7 @@ nmdlm_status launch_page_plan(const nmdlm_pages& pg, const int32_t* ctx, const i
   const nmdlm_status rc = hip_status();
   if (rc != NMDLM_OK) return rc;
   const unsigned grid = (unsigned)std::min<long long>((pg.max_rows + 255) / 256, 1024);
-  hipLaunchKernelGGL(k_page_entries, dim3(grid), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(k_page_rows, dim3(grid), dim3(256), 0, st, a);
   return hip_status();
 }
 
@@ -430,27 +441,6 @@ __global__ __launch_bounds__(256) void k_page_scores(SelectArgs a) {
 // where exactly n_sel scores reach the middle.  Of the scores equal to the last
 // one taken the lowest pages are taken.
 
-// The largest value of a wave: within rows of 16 lanes, then across them.
-__device__ __forceinline__ int wave_max(int x) {
-  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x111, 0xf, 0xf, false));  // row_shr:1
-  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x112, 0xf, 0xf, false));
-  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x114, 0xf, 0xf, false));
-  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x118, 0xf, 0xf, false));
-  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x142, 0xf, 0xf, false));  // row_bcast:15
-  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x143, 0xf, 0xf, false));  // row_bcast:31
-  return __builtin_amdgcn_readlane(x, 63);
-}
-
-__device__ __forceinline__ int wave_sum(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-  return __builtin_amdgcn_readlane(x, 63);
-}
-
 struct Pick {
   int thr, ties;  // scores above thr, and the first `ties` equal to it
 };
@@ -482,11 +472,6 @@ __device__ __forceinline__ Pick pick_threshold(const int (&s)[NR], int P, int n_
     }
   }
   return Pick{lo, n_sel - above};
-}
-
-// lanes below this one whose bit is set
-__device__ __forceinline__ int bits_before(uint64_t m) {
-  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
 }
 
 // The word of 64 pages whose scores the lanes hold; takes its ties off.

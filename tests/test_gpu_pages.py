@@ -279,6 +279,21 @@ def test_attention_long(dh, share):
     assert_same(d.spikes(), spk, "spikes")
 
 
+@pytest.mark.parametrize("share", [None, 0.02])
+def test_attention_long_tiles(share):
+    """Tiles of rows over more pages than the kernel lists at once."""
+    c = P.make_case(41, [64 * 270 + 9], [500], T=1, H=32, dh=64)
+    d = device(c)
+    d.plan()
+    p = P.plan(c)
+    sel = None if share is None else some_selection(c, p, 1, share)
+    d.attention(sel=None if sel is None else d.put_selection(sel))
+    sync()
+    cur, spk = P.attention(c, p, sel)
+    assert_same(d.cur.cpu().numpy(), cur, "currents")
+    assert_same(d.spikes(), spk, "spikes")
+
+
 @pytest.mark.parametrize("T,H,dh,sel", [(4, 16, 64, False), (4, 16, 128, True), (1, 16, 128, False)])
 def test_attention_wide_tiles(T, H, dh, sel):
     """Enough rows for 32 queries a wave."""
