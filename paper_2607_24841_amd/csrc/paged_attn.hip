@@ -39,8 +39,8 @@ struct PageEntry {
 };
 
 // Splits of a request of nP pages.
-__device__ __forceinline__ int split_count(int splits, int nP) {
-  return min(splits, max(nP / kSplitPages, 1));
+__device__ __forceinline__ int split_count(const PagedArgs& a, int nP) {
+  return min(a.splits, max(nP / kSplitPages, 1));
 }
 struct PageRange {
   int p0, p1;
@@ -70,8 +70,9 @@ __device__ __forceinline__ int32_t* split_sums(const PagedArgs& a, int row, int 
 template <int DHW>
 __device__ __forceinline__ void load_page(AttnChunk<DHW>& ch, const uint64_t* __restrict__ kp,
                                           const uint64_t* __restrict__ vp, size_t at, int lane) {
-  const uint64_t* kr = kp + at * (64 * DHW);
-  const uint64_t* vr = vp + at * (64 * DHW);
+  const uint64_t *kr = kp + at, *vr = vp + at;
+  // the page's address stays in scalar registers, the lane's offset in one of its own
+  asm("" : "+s"(kr), "+s"(vr));
 #pragma unroll
   for (int w = 0; w < DHW; ++w) {
     ch.k[w] = kr[(uint32_t)(lane * DHW + w)];
@@ -201,7 +202,7 @@ __device__ __forceinline__ int list_seen(const PagedArgs& a, const int32_t* tab,
 }
 
 template <int DHW, int QG, bool SEL>
-__global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_attn(PagedArgs a) {
+__global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_paged_attn(PagedArgs a) {
   constexpr int NT = DHW * 4;
   __shared__ AttnLut sLut;
   __shared__ int sDen[NMDLM_MAX_T][16];
@@ -218,7 +219,7 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_attn(PagedArgs a) {
   const int g = lane >> 4, c = lane & 15;
   const int h = blockIdx.x, z = blockIdx.y;
   const PageTile tl = a.tiles[blockIdx.z];
-  const int nr = tl.n_full & 63, J = tl.keys, nP = (J + 63) / 64, splits = split_count(a.splits, nP);
+  const int nr = tl.n_full & 63, J = tl.keys, nP = (J + 63) / 64, splits = split_count(a, nP);
   if (nr == 0 || z >= splits) return;  // uniform
   const PageRange pr = split_range(nP, z, splits);
   const int32_t* tab = a.table + (size_t)tl.s * a.max_pages;
@@ -231,6 +232,9 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_attn(PagedArgs a) {
                                   nr - 1, g, c);
   AttnWave<DHW, QG> w;
   const char* lb = reinterpret_cast<const char*>(&sLut);
+  // words of a pool page; a head's and timestep's keys and values in it
+  const size_t page_words = (size_t)a.H * a.T * (64 * DHW), at_ht = ((size_t)h * a.T + t) * (64 * DHW);
+  const uint64_t *kp = a.kp + at_ht, *vp = a.vp + at_ht;
   AttnStage<DHW>* const st = &sStage[kAttnStages * wave];
   int keys = 0;
 
@@ -250,30 +254,29 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_attn(PagedArgs a) {
     if (part >= m) continue;  // wave-uniform
 
     // as AttnWave::run: the weighted sum of one page while the table reads of the
-    // next and the loads of the one after are in flight
-    auto entry = [&](int i) {
-      const PageEntry e = sList[min(i, m - 1)];
-      return PageEntry{__builtin_amdgcn_readfirstlane(e.id), __builtin_amdgcn_readfirstlane(e.keys)};
+    // next are in flight, and the loads of the one after that; what the list says of
+    // a page is read before the table reads, which it would wait for
+    auto id_at = [&](int i) { return sList[min(i, m - 1)].id; };
+    auto load = [&](AttnChunk<DHW>& ch, int id) {
+      load_page(ch, kp, vp, (size_t)(uint32_t)__builtin_amdgcn_readfirstlane(id) * page_words, lane);
     };
-    auto place = [&](int id) { return ((size_t)id * a.H + h) * a.T + t; };
     AttnStage<DHW>*s0 = st, *s1 = st + 1, *s2 = st + 2;
     v4i s[QG][4], p[QG];
     uint32_t k[4], v[NT];
-    AttnChunk<DHW> first, nxt;
-    PageEntry ec = entry(part), en = entry(part + np), ef = entry(part + 2 * np);
-    load_page(first, a.kp, a.vp, place(ec.id), lane);
-    load_page(nxt, a.kp, a.vp, place(en.id), lane);
+    AttnChunk<DHW> first, next;
+    load(first, id_at(part));
+    load(next, id_at(part + np));
     w.put(first, *s0, lane);
     w.key_pieces(*s0, k, g, c);
-    w.put(nxt, *s1, lane);
-    load_page(nxt, a.kp, a.vp, place(ef.id), lane);
+    w.put(next, *s1, lane);
+    load(next, id_at(part + 2 * np));
+    uint32_t seen = SEL ? sSeen[part] : 0u;
     w.scores(k, s);
     w.lookup(s, lb);
     w.key_pieces(*s1, k, g, c);
     w.pack(s, p);
-    auto unseen = [&](int i) {  // weight 0 where the row does not see the page
+    auto unseen = [&]() {  // weight 0 where the row does not see the page
       if constexpr (SEL) {
-        const uint32_t seen = sSeen[i];
 #pragma unroll
         for (int u = 0; u < QG; ++u)
           if (!((seen >> (16 * u + c)) & 1u)) p[u] = v4i{1, 1, 1, 1} * (int)0x80808080u;
@@ -292,31 +295,29 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_attn(PagedArgs a) {
       keys += nk;
     };
     int i = part;
-    unseen(i);
-    for (i += np; i < m; i += np) {
+    unseen();
+    for (i += np; i < m; i += np) {  // wave-uniform
+      const int id = id_at(i + 2 * np), nk = sList[i - np].keys;
+      if constexpr (SEL) seen = sSeen[i];
       w.value_pieces(*s0, v, g, c);
       w.scores(k, s);
       __builtin_amdgcn_sched_barrier(0);
       w.lookup(s, lb);
-      w.put(nxt, *s2, lane);
-      const PageEntry ex = entry(i + 2 * np);
-      load_page(nxt, a.kp, a.vp, place(ex.id), lane);
+      w.put(next, *s2, lane);
+      load(next, id);
       w.key_pieces(*s2, k, g, c);
-      partial(ec.keys);
+      partial(__builtin_amdgcn_readfirstlane(nk));
       w.weigh(v, p);
       __builtin_amdgcn_sched_barrier(0);
       w.pack(s, p);
-      unseen(i);
-      ec = en;
-      en = ef;
-      ef = ex;
+      unseen();
       AttnStage<DHW>* const tmp = s0;
       s0 = s1;
       s1 = s2;
       s2 = tmp;
     }
     w.value_pieces(*s0, v, g, c);
-    partial(ec.keys);
+    partial(__builtin_amdgcn_readfirstlane(sList[i - np].keys));
     w.weigh(v, p);
   }
   w.finish(reinterpret_cast<char*>(st), lane, g, c);
@@ -392,7 +393,7 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T * DHW) void k_paged_join(PagedArgs
   touch_kernargs<sizeof(PagedArgs) + sizeof(void*)>();
   const int row = blockIdx.x, h = blockIdx.y;
   const PageTile tl = rows[row];
-  const int n = split_count(a.splits, (tl.keys + 63) / 64);
+  const int n = split_count(a, (tl.keys + 63) / 64);
   if ((tl.n_full & 63) == 0 || n == 1) return;  // uniform; a single split fired by itself
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int t = wave / DHW, w = wave - t * DHW;
@@ -469,7 +470,7 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_token(PagedArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nwaves = nth >> 6;
   const int h = blockIdx.x, z = blockIdx.y, row = blockIdx.z;
   const PageTile tl = a.tiles[row];
-  const int J = tl.keys, nP = (J + 63) / 64, splits = split_count(a.splits, nP);
+  const int J = tl.keys, nP = (J + 63) / 64, splits = split_count(a, nP);
   if ((tl.n_full & 63) == 0 || z >= splits) return;  // uniform
   const PageRange pr = split_range(nP, z, splits);
   const int32_t* tab = a.table + (size_t)tl.s * a.max_pages;
@@ -567,7 +568,7 @@ struct PagedRoute {
   int groups, parts, splits;
 };
 static PagedRoute paged_route(const nmdlm_pages& pg, int T, int H) {
-  const long long t16 = pg.max_rows / 16 + pg.n_seq, t32 = pg.max_rows / 32 + pg.n_seq;
+  const long long t32 = pg.max_rows / 32 + pg.n_seq;
   PagedRoute r{false, 1, T <= 2 ? 4 : (T <= 4 ? 2 : 1), 1};
   if (pg.max_rows <= 2LL * pg.n_seq + 8) {
     r.token = true;
@@ -576,9 +577,9 @@ static PagedRoute paged_route(const nmdlm_pages& pg, int T, int H) {
     r.parts = 1;
     return r;
   }
-  const long long wgs = (r.token ? pg.max_rows : t16) * (long long)H;
-  if (wgs < 1024)
-    r.splits = (int)std::max(1LL, std::min<long long>({(1023 + wgs) / wgs, 64, pg.max_pages / kSplitPages}));
+  const long long tiles = r.token ? pg.max_rows : std::max((pg.max_rows + 15) / 16, pg.n_seq);
+  r.splits = (int)std::max(1LL, std::min<long long>({(r.token ? 1024 : 512) / (tiles * H), 64,
+                                                     pg.max_pages / kSplitPages}));
   return r;
 }
 
