@@ -245,36 +245,75 @@ nmdlm_status launch_page_plan(const nmdlm_pages& pg, const int32_t* ctx, const i
 // Store.  A wave takes one run of rows (of one page), a head and a timestep:
 // lane j = position j of the page.  Keys go to their rows as they are; values
 // are a 64 x 64 bit transpose per 64 channels, lane j's word (channels) becoming
-// lane c's word (positions); the keys are transposed too, for the counts.
+// lane c's word (positions); the keys are transposed too, for the counts.  The
+// waves of a workgroup are the heads of one timestep, which share the rows'
+// lines.
 // ---------------------------------------------------------------------------
 
-// bit (lane i, bit j) <-> bit (lane j, bit i): for s = 32 .. 1 the blocks off
-// the diagonal of every 2s x 2s block change places.
-__device__ __forceinline__ uint64_t transpose64(uint64_t x, int lane) {
-  constexpr uint64_t keep[6] = {0x00000000FFFFFFFFull, 0x0000FFFF0000FFFFull, 0x00FF00FF00FF00FFull,
-                                0x0F0F0F0F0F0F0F0Full, 0x3333333333333333ull, 0x5555555555555555ull};
-#pragma unroll
-  for (int k = 0; k < 6; ++k) {
-    const int s = 32 >> k;
-    const uint64_t y = __shfl_xor((unsigned long long)x, s);
-    x = lane & s ? (x & ~keep[k]) | ((y & ~keep[k]) >> s) : (x & keep[k]) | ((y & keep[k]) << s);
+// What a lane needs of the transpose's steps: the bits it keeps and how far the
+// partner's are rotated.
+struct TransposeLane {
+  uint32_t sel8, keep4, rot4, keep2, rot2, keep1, rot1;
+  __device__ __forceinline__ explicit TransposeLane(int lane) {
+    sel8 = lane & 8 ? 0x03070105u : 0x06020400u;  // bytes of (partner, own): see step8
+    keep4 = lane & 4 ? 0xF0F0F0F0u : 0x0F0F0F0Fu;
+    rot4 = lane & 4 ? 4u : 28u;
+    keep2 = lane & 2 ? 0xCCCCCCCCu : 0x33333333u;
+    rot2 = lane & 2 ? 2u : 30u;
+    keep1 = lane & 1 ? 0xAAAAAAAAu : 0x55555555u;
+    rot1 = lane & 1 ? 1u : 31u;
   }
-  return x;
+};
+
+// bit (lane i, bit j) <-> bit (lane j, bit i): for s = 32 .. 1 the blocks off the
+// diagonal of every 2s x 2s block change places.  Lanes 32 and 16 apart swap
+// registers, nearer ones exchange by DPP; a partner's bits come rotated by s, what
+// crosses a block's border falling on bits that are kept.
+__device__ __forceinline__ uint64_t transpose64(uint64_t x, const TransposeLane& tl) {
+  uint32_t lo = (uint32_t)x, hi = (uint32_t)(x >> 32);
+  {
+    const auto r = __builtin_amdgcn_permlane32_swap(lo, hi, false, false);
+    lo = r[0];
+    hi = r[1];
+  }
+  {
+    const uint32_t p = __builtin_amdgcn_perm(hi, lo, 0x05040100u);  // the low halves
+    const uint32_t q = __builtin_amdgcn_perm(hi, lo, 0x07060302u);  // the high halves
+    const auto r = __builtin_amdgcn_permlane16_swap(p, q, false, false);
+    lo = __builtin_amdgcn_perm(r[1], r[0], 0x05040100u);
+    hi = __builtin_amdgcn_perm(r[1], r[0], 0x07060302u);
+  }
+  uint32_t d[2] = {lo, hi};
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    uint32_t v = d[k], y;
+    y = __builtin_amdgcn_update_dpp(0, v, 0x128, 0xf, 0xf, true);  // row_ror:8: lane ^ 8
+    v = __builtin_amdgcn_perm(y, v, tl.sel8);
+    y = __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, true);  // half mirror: lane ^ 7
+    y = __builtin_amdgcn_update_dpp(0, y, 0x1B, 0xf, 0xf, true);   // quad_perm 3210: lane ^ 3
+    v = (v & tl.keep4) | (__builtin_amdgcn_alignbit(y, y, tl.rot4) & ~tl.keep4);
+    y = __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, true);   // quad_perm 1032 of pairs: lane ^ 2
+    v = (v & tl.keep2) | (__builtin_amdgcn_alignbit(y, y, tl.rot2) & ~tl.keep2);
+    y = __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, true);   // lane ^ 1
+    v = (v & tl.keep1) | (__builtin_amdgcn_alignbit(y, y, tl.rot1) & ~tl.keep1);
+    d[k] = v;
+  }
+  return (uint64_t)d[1] << 32 | d[0];
 }
 
+constexpr int kStoreWaves = 16;
+
 template <int DHW>
-__global__ __launch_bounds__(256) void k_page_store(const PageRun* __restrict__ runs,
-                                                    const uint64_t* __restrict__ k,
-                                                    const uint64_t* __restrict__ v, int T, int H,
-                                                    int max_rows, int pool,
-                                                    uint64_t* __restrict__ k_pages,
-                                                    uint64_t* __restrict__ v_pages,
-                                                    uint8_t* __restrict__ counts) {
-  const PageRun r = runs[blockIdx.x];
-  const int unit = __builtin_amdgcn_readfirstlane((int)blockIdx.y * 4 + ((int)threadIdx.x >> 6));
-  if ((unsigned)r.page >= (unsigned)pool || r.n < 1 || unit >= T * H) return;  // wave-uniform
+__global__ __launch_bounds__(64 * kStoreWaves) void k_page_store(
+    const PageRun* __restrict__ runs, const uint64_t* __restrict__ k, const uint64_t* __restrict__ v, int T,
+    int H, int max_rows, int pool, uint64_t* __restrict__ k_pages, uint64_t* __restrict__ v_pages,
+    uint8_t* __restrict__ counts) {
+  const PageRun r = runs[blockIdx.z];
+  const int t = blockIdx.x;
+  const int h = __builtin_amdgcn_readfirstlane((int)(blockIdx.y * (blockDim.x >> 6)) + ((int)threadIdx.x >> 6));
+  if ((unsigned)r.page >= (unsigned)pool || r.n < 1 || h >= H) return;  // wave-uniform
   const int lane = threadIdx.x & 63;
-  const int t = unit / H, h = unit - t * H;
+  const TransposeLane tl(lane);
   const int dw = H * DHW;
   const size_t at = ((size_t)r.page * H + h) * T + t;
   uint64_t* kp = k_pages + at * NMDLM_PAGE * DHW;
@@ -293,8 +332,8 @@ __global__ __launch_bounds__(256) void k_page_store(const PageRun* __restrict__ 
 #pragma unroll
   for (int w = 0; w < DHW; ++w) {
     if (in) kp[lane * DHW + w] = kw[w];
-    vp[w * 64 + lane] = (vo[w] & ~mask) | transpose64(vw[w], lane);
-    counts[at * 64 * DHW + w * 64 + lane] = (uint8_t)__popcll(transpose64(kw[w], lane));
+    vp[w * 64 + lane] = (vo[w] & ~mask) | transpose64(vw[w], tl);
+    counts[at * 64 * DHW + w * 64 + lane] = (uint8_t)__popcll(transpose64(kw[w], tl));
   }
 }
 
@@ -303,12 +342,14 @@ nmdlm_status launch_page_store(const nmdlm_pages& pg, const uint64_t* k, const u
                                hipStream_t st) {
   PageIndex ix;
   page_index_layout(pg.n_seq, pg.max_rows, pg.index, &ix);
-  const dim3 grid((unsigned)ix.n_runs, (unsigned)((T * H + 3) / 4));
+  // heads of a workgroup: evenly, at most kStoreWaves; empty runs are the grid's last
+  const int groups = (H + kStoreWaves - 1) / kStoreWaves, waves = (H + groups - 1) / groups;
+  const dim3 grid(T, groups, ix.n_runs), block(64 * waves);
   if (dh == 64)
-    hipLaunchKernelGGL(k_page_store<1>, grid, dim3(256), 0, st, ix.runs, k, v, T, H, pg.max_rows, pg.pool,
+    hipLaunchKernelGGL(k_page_store<1>, grid, block, 0, st, ix.runs, k, v, T, H, pg.max_rows, pg.pool,
                        k_pages, v_pages, counts);
   else
-    hipLaunchKernelGGL(k_page_store<2>, grid, dim3(256), 0, st, ix.runs, k, v, T, H, pg.max_rows, pg.pool,
+    hipLaunchKernelGGL(k_page_store<2>, grid, block, 0, st, ix.runs, k, v, T, H, pg.max_rows, pg.pool,
                        k_pages, v_pages, counts);
   return hip_status();
 }
