@@ -383,12 +383,10 @@ struct SelectArgs {
   int T, H, n_sel, ld;
 };
 
-constexpr int kScoreSteps = 8;                     // k-steps (of 64 channels) staged at once
-constexpr int kScoreLd = kScoreSteps * 4 + 1;      // 16-byte units of a staged page (one of padding)
-
-struct ScoreStage {
-  v4i x[16 * kScoreLd];  // of one wave
-};
+// k-steps (of 64 channels) staged at once, and the 16-byte units between a wave's
+// staged pages (one of padding): as many as the call has, for more workgroups a CU.
+constexpr int kScoreSteps = 8;
+__host__ __device__ constexpr int score_ld(int steps) { return (steps < kScoreSteps ? steps : kScoreSteps) * 4 + 1; }
 
 // The query bits of the tile's rows, [T][ROWS][DHW] words (rows past the last:
 // the last).  All threads of the workgroup.
@@ -411,13 +409,13 @@ __device__ __forceinline__ int score_id(const SelectArgs& a, const PageTile& tl,
 // k-steps are all issued before the first is used.
 template <int DHW, int QG>
 __device__ __forceinline__ void score_pages(const SelectArgs& a, int id, int h, int lane, const uint64_t* sQ,
-                                            ScoreStage& st, v4i (&s)[QG]) {
+                                            v4i* st, v4i (&s)[QG]) {
   typedef const v4i __attribute__((may_alias)) v4i_in;
   typedef const uint16_t __attribute__((may_alias)) u16_in;
   const int g = lane >> 4, c = lane & 15;
   const bool there = (unsigned)id < (unsigned)a.pool;
   const uint8_t* cp = a.counts + ((size_t)(there ? id : 0) * a.H + h) * a.T * (64 * DHW) + 16 * (lane & 3);
-  const int steps = a.T * DHW;
+  const int steps = a.T * DHW, ld = score_ld(steps);
 #pragma unroll
   for (int u = 0; u < QG; ++u) s[u] = v4i{0, 0, 0, 0};
   for (int k0 = 0; k0 < steps; k0 += kScoreSteps) {  // uniform
@@ -428,7 +426,7 @@ __device__ __forceinline__ void score_pages(const SelectArgs& a, int id, int h, 
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 0; k < kScoreSteps; ++k)
-      st.x[(lane >> 2) * kScoreLd + k * 4 + (lane & 3)] = there ? x[k] : v4i{0, 0, 0, 0};
+      if (k0 + k < steps) st[(lane >> 2) * ld + k * 4 + (lane & 3)] = there ? x[k] : v4i{0, 0, 0, 0};
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -436,7 +434,7 @@ __device__ __forceinline__ void score_pages(const SelectArgs& a, int id, int h, 
     for (int k = 0; k < kScoreSteps; ++k) {
       if (k0 + k >= steps) break;  // uniform
       const int t = (k0 + k) / DHW, w = (k0 + k) % DHW;
-      const v4i y = st.x[c * kScoreLd + k * 4 + g];
+      const v4i y = st[c * ld + k * 4 + g];
 #pragma unroll
       for (int u = 0; u < QG; ++u) {
         const uint32_t b =
@@ -453,7 +451,7 @@ __device__ __forceinline__ void score_pages(const SelectArgs& a, int id, int h, 
 template <int DHW>
 __global__ __launch_bounds__(256) void k_page_scores(SelectArgs a) {
   touch_kernargs<sizeof(SelectArgs)>();
-  __shared__ ScoreStage sStage[4];
+  extern __shared__ v4i sStage[];  // of the four waves
   __shared__ uint64_t sQ[NMDLM_MAX_T * 32 * DHW];
   const PageTile tl = a.tiles[blockIdx.x];
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, h = blockIdx.y;
@@ -466,7 +464,7 @@ __global__ __launch_bounds__(256) void k_page_scores(SelectArgs a) {
   __syncthreads();
   if (p0 >= P) return;  // wave-uniform
   v4i s[2];
-  score_pages<DHW, 2>(a, id, h, lane, sQ, sStage[wave], s);
+  score_pages<DHW, 2>(a, id, h, lane, sQ, sStage + wave * 16 * score_ld(a.T * DHW), s);
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -478,7 +476,7 @@ __global__ __launch_bounds__(256) void k_page_scores(SelectArgs a) {
 
 // Select, choice: a wave per row and head.  The scores stand in registers (score
 // p in lane p % 64, register p / 64); the n_sel-th largest is found by bisection
-// between the smallest and the largest, and often earlier:
+// between 0 and the largest, and often earlier:
 // where exactly n_sel scores reach the middle.  Of the scores equal to the last
 // one taken the lowest pages are taken.
 
@@ -489,21 +487,22 @@ template <int NR>
 __device__ __forceinline__ Pick pick_threshold(const int (&s)[NR], int P, int n_sel) {
   if (n_sel >= P) return Pick{-1, 0};  // every page (lanes past the last hold -1)
   if (n_sel == 0) return Pick{1 << 30, 0};
-  int lo = 1 << 30, hi = 0;
+  int lo = 0, hi = 0;
 #pragma unroll
-  for (int r = 0; r < NR; ++r) {
-    lo = min(lo, s[r] < 0 ? 1 << 30 : s[r]);
-    hi = max(hi, s[r]);
-  }
-  lo = -wave_max(-lo);
+  for (int r = 0; r < NR; ++r) hi = max(hi, s[r]);
   hi = wave_max(hi) + 1;
   int above = 0;  // scores >= hi; scores >= lo are at least n_sel
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     int n = 0;
+    if constexpr (NR <= 8) {  // by the scalar unit: fewer instructions than a sum over lanes
 #pragma unroll
-    for (int r = 0; r < NR; ++r) n += s[r] >= mid ? 1 : 0;
-    n = wave_sum(n);
+      for (int r = 0; r < NR; ++r) n += (int)__popcll(__builtin_amdgcn_ballot_w64(s[r] >= mid));
+    } else {
+#pragma unroll
+      for (int r = 0; r < NR; ++r) n += s[r] >= mid ? 1 : 0;
+      n = wave_sum(n);
+    }
     if (n == n_sel) return Pick{mid - 1, 0};
     if (n > n_sel) {
       lo = mid;
@@ -581,7 +580,8 @@ __device__ void pick_row_long(const int32_t* sc, int P, int nP, int n_sel, int w
 
 __device__ __forceinline__ void pick_any(const int32_t* sc, int P, int nP, int n_sel, int words,
                                          uint64_t* __restrict__ out, int lane) {
-  if (P <= 128) pick_row<2>(sc, P, nP, n_sel, words, out, lane);
+  if (P <= 64) pick_row<1>(sc, P, nP, n_sel, words, out, lane);
+  else if (P <= 128) pick_row<2>(sc, P, nP, n_sel, words, out, lane);
   else if (P <= 512) pick_row<8>(sc, P, nP, n_sel, words, out, lane);
   else if (P <= 2048) pick_row<32>(sc, P, nP, n_sel, words, out, lane);
   else pick_row_long(sc, P, nP, n_sel, words, out, lane);
@@ -605,9 +605,9 @@ constexpr int kSelectWaves = 8;
 template <int DHW>
 __global__ __launch_bounds__(64 * kSelectWaves) void k_page_select(SelectArgs a) {
   touch_kernargs<sizeof(SelectArgs)>();
-  __shared__ ScoreStage sStage[kSelectWaves];
   __shared__ uint64_t sQ[NMDLM_MAX_T * 16 * DHW];
-  extern __shared__ int32_t sScores[];  // [16][ld]
+  extern __shared__ v4i sStage[];  // of the waves, then the scores [16][ld]
+  int32_t* sScores = reinterpret_cast<int32_t*>(sStage + kSelectWaves * 16 * score_ld(a.T * DHW));
   const PageTile tl = a.tiles[blockIdx.x];
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, h = blockIdx.y;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -619,7 +619,7 @@ __global__ __launch_bounds__(64 * kSelectWaves) void k_page_select(SelectArgs a)
   for (int p0 = wave * 16; p0 < P; p0 += kSelectWaves * 16) {
     v4i s[1];
     const int next = score_id(a, tl, p0 + kSelectWaves * 16, lane);
-    score_pages<DHW, 1>(a, id, h, lane, sQ, sStage[wave], s);
+    score_pages<DHW, 1>(a, id, h, lane, sQ, sStage + wave * 16 * score_ld(a.T * DHW), s);
     id = next;
 #pragma unroll
     for (int e = 0; e < 4; ++e) sScores[(4 * g + e) * a.ld + p0 + c] = s[0][e];
@@ -647,9 +647,10 @@ static nmdlm_status launch_select(const nmdlm_pages& pg, const uint64_t* q, int 
   page_index_layout(pg.n_seq, pg.max_rows, pg.index, &ix);
   SelectArgs a{ix.t16, pg.table, q, counts, sel, static_cast<int32_t*>(ws), pg.max_pages, pg.pool,
                pg.max_rows, (pg.max_pages + 63) / 64, T, H, n_sel, select_ld(pg)};
+  const size_t stage = 16 * score_ld(T * DHW) * sizeof(v4i);  // of a wave
   if (pg.max_pages <= kSelectPages) {
     a.ld += 1;  // a row's bank past the row before's
-    const size_t lds = (size_t)a.ld * 16 * sizeof(int32_t);
+    const size_t lds = kSelectWaves * stage + (size_t)a.ld * 16 * sizeof(int32_t);
     if (hipFuncSetAttribute(reinterpret_cast<const void*>(&k_page_select<DHW>),
                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
       return NMDLM_ERR_HIP;
@@ -657,7 +658,7 @@ static nmdlm_status launch_select(const nmdlm_pages& pg, const uint64_t* q, int 
     return hip_status();
   }
   a.tiles = ix.t32;
-  hipLaunchKernelGGL(k_page_scores<DHW>, dim3(ix.n32, H, (pg.max_pages + 63) / 64), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(k_page_scores<DHW>, dim3(ix.n32, H, (pg.max_pages + 63) / 64), dim3(256), 4 * stage, st, a);
   const nmdlm_status rc = hip_status();
   if (rc != NMDLM_OK) return rc;
   hipLaunchKernelGGL(k_page_pick, dim3(ix.n32, H, 8), dim3(256), 0, st, a);
