@@ -648,6 +648,37 @@ nmdlm_status nmdlm_bbm_attn_paged(const nmdlm_pages* pages, const uint64_t* q, i
                                   uint64_t* s_out, void* ws, size_t ws_bytes, void* stream);
 size_t nmdlm_bbm_attn_paged_workspace_size(const nmdlm_pages* pages, int T, int H, int dh);
 
+/* ------------------------------------------------------------------------
+ * nmdlm_block_step_paged — nmdlm_block_step (the same layers, head and
+ * unmasking) for the packed rows of a page plan: requests of different lengths
+ * in one step, or a prefill of their prompts (NMDLM_NO_HEAD).  The plan is made
+ * before (nmdlm_page_plan) and may serve several steps; per layer the step
+ * makes the calls nmdlm_page_store, nmdlm_page_select (n_sel >= 0) and
+ * nmdlm_bbm_attn_paged between its products.
+ *
+ *   model       layers[l].k_cache and vt_cache are the layer's k_pages and
+ *               v_pages; cache_cap and max_seq are not read
+ *   key_counts  HOST array [n_layers] of the layers' key_counts
+ *   n_sel       context pages that a row and head sees besides its own request's
+ *               last ones, or below 0: all pages
+ *   io          token-indexed buffers have max_rows rows (x_in, y_out
+ *               [T][max_rows][d/64], tokens, masked, pred, conf [max_rows], logits
+ *               [max_rows][V]), unmasked_pos [n_seq][k_unmask] holds positions
+ *               within a request's rows (-1: fewer were masked).  M, C, pos0 and
+ *               n_seq are not read; a row's position comes from the plan, and one
+ *               at or past max_pos has no position spike and sets
+ *               NMDLM_STATUS_BAD_REQUEST.  Of a request's rows the first
+ *               NMDLM_MAX_HEAD_M can be unmasked; rows without a page are not,
+ *               and their outputs mean nothing.
+ * Limits: T*max_rows <= 2^19; errors as for nmdlm_block_step and the paged calls.
+ * ------------------------------------------------------------------------ */
+nmdlm_status nmdlm_block_step_paged(const nmdlm_model* model, const nmdlm_pages* pages,
+                                    uint8_t* const* key_counts, int n_sel,
+                                    nmdlm_step_io* io, void* ws, size_t ws_bytes,
+                                    void* stream);
+size_t nmdlm_block_step_paged_workspace_size(const nmdlm_model* model,
+                                             const nmdlm_pages* pages, unsigned flags);
+
 /* Clears a workspace region with a fill kernel on the stream (use once on a
  * new workspace). */
 nmdlm_status nmdlm_workspace_clear(void* ws, size_t ws_bytes, void* stream);

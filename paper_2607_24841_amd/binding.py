@@ -60,7 +60,8 @@ EXPORTS = (
     "nmdlm_qbsm_blocked", "nmdlm_weight_blocked_bytes", "nmdlm_weight_block",
     "nmdlm_page_index_bytes", "nmdlm_page_plan", "nmdlm_page_store", "nmdlm_page_select",
     "nmdlm_page_select_workspace_size", "nmdlm_bbm_attn_paged",
-    "nmdlm_bbm_attn_paged_workspace_size",
+    "nmdlm_bbm_attn_paged_workspace_size", "nmdlm_block_step_paged",
+    "nmdlm_block_step_paged_workspace_size",
 )
 
 
@@ -179,6 +180,10 @@ def load(path: str = LIB_PATH):
                                          vp, vp, sz, vp]
     lib.nmdlm_bbm_attn_paged_workspace_size.argtypes = [pg, C.c_int, C.c_int, C.c_int]
     lib.nmdlm_bbm_attn_paged_workspace_size.restype = sz
+    lib.nmdlm_block_step_paged.argtypes = [C.POINTER(Model), pg, C.POINTER(vp), C.c_int,
+                                           C.POINTER(StepIO), vp, sz, vp]
+    lib.nmdlm_block_step_paged_workspace_size.argtypes = [C.POINTER(Model), pg, u]
+    lib.nmdlm_block_step_paged_workspace_size.restype = sz
     lib.nmdlm_workspace_clear.argtypes = [vp, sz, vp]
     lib.nmdlm_status_string.argtypes = [C.c_int]
     lib.nmdlm_status_string.restype = C.c_char_p
@@ -344,13 +349,14 @@ class Pages:
     of `pool` pages.  The state that lives from step to step (table, held,
     ring, ring_state) is one tensor, `state`; at first every page is free."""
 
-    def __init__(self, n_seq: int, max_rows: int, max_pages: int, pool: int, device="cuda"):
+    def __init__(self, n_seq: int, max_rows: int, max_pages: int, pool: int, device="cuda", state=None):
         nbytes = load().nmdlm_page_index_bytes(n_seq, max_rows)
         if nbytes == 0 or max_pages < 1 or pool < 1:
             raise NmdlmError(NMDLM_ERR_INVALID_ARG, "Pages: sizes")
         self.n_seq, self.max_rows, self.max_pages, self.pool = n_seq, max_rows, max_pages, pool
         i32 = dict(dtype=torch.int32, device=device)
-        self.state = torch.zeros(n_seq * max_pages + n_seq + pool + 2, **i32)
+        fresh = state is None
+        self.state = torch.zeros(n_seq * max_pages + n_seq + pool + 2, **i32) if fresh else state
         self.device = self.state.device
         self._index = self.state.get_device()   # of the GPU, -1 on the host
         self.words = -(-max_pages // 64)        # words of a row and head in a selection
@@ -361,7 +367,8 @@ class Pages:
         self.pos = torch.zeros(max_rows, **i32)
         self.slot = torch.full((max_rows,), -1, dtype=torch.int64, device=device)
         self.index = torch.zeros(nbytes, dtype=torch.uint8, device=device)
-        self.reset()
+        if fresh:
+            self.reset()
         self.c = PagesC(n_seq, max_rows, max_pages, pool, ptr(self.table), ptr(self.held),
                         ptr(self.ring), ptr(self.ring_state), ptr(self.cu_rows), ptr(self.slot),
                         ptr(self.pos), ptr(self.index), nbytes)
@@ -380,6 +387,11 @@ class Pages:
                          (self.ring_state, ring_state)):
             if src is not None:
                 dst.copy_(torch.as_tensor(src, dtype=torch.int32).view(dst.shape))
+
+    def view(self, max_rows: int) -> "Pages":
+        """A plan of other packed rows over the same state: tables, ring and
+        pools are shared, so the two take turns."""
+        return Pages(self.n_seq, max_rows, self.max_pages, self.pool, self.device, state=self.state)
 
     def pools(self, T: int, H: int, dh: int):
         """A layer's empty pools: key pages, value pages, key counts."""
@@ -577,6 +589,42 @@ class ModelView:
                        self._c_layers, p.emb, p.pos_ch, p.w_head if head else None,
                        p.head_scale if head else None, p.max_seq,
                        p.w_head_b if head else None)
+
+
+class PagedModel:
+    """A model's layers with pools of pages in place of contiguous caches, one
+    pool a layer, for the requests of a plan (weights are shared, not copied)."""
+
+    def __init__(self, parent: DeviceModel, pages: Pages, head: bool = True, pools=None):
+        self.parent, self.pages = parent, pages   # keep the device tensors alive
+        self.pools = pools or [pages.pools(parent.T, parent.H, parent.d // parent.H)
+                               for _ in parent.layers]
+        n = len(parent.layers)
+        self._c_layers = (Layer * max(1, n))(*[l.c for l in parent.layers])
+        self.key_counts = (C.c_void_p * max(1, n))()
+        for i, (k, v, counts) in enumerate(self.pools):
+            self._c_layers[i].k_cache, self._c_layers[i].vt_cache = ptr(k), ptr(v)
+            self.key_counts[i] = ptr(counts)
+        p = parent.c
+        self.c = Model(n, p.d, p.H, p.F, p.V, p.T, 0, p.max_pos, self._c_layers, p.emb, p.pos_ch,
+                       p.w_head if head else None, p.head_scale if head else None, 0,
+                       p.w_head_b if head else None)
+
+    def view(self, pages: Pages, head: bool) -> "PagedModel":
+        """The same layers and pools under another plan of the same pages."""
+        return PagedModel(self.parent, pages, head, self.pools)
+
+
+def nmdlm_block_step_paged(model: PagedModel, io: StepIO, ws: torch.Tensor, n_sel: int = -1,
+                           stream=None) -> None:
+    what, pages = "nmdlm_block_step_paged", model.pages
+    fn, ref, counts = load().nmdlm_block_step_paged, C.byref(model.c), model.key_counts
+    pages._call(lambda pg, st: fn(ref, pg, counts, n_sel, C.byref(io), pages._arg(what, "ws", ws, 1, 1),
+                                  ws.numel(), st), what, stream=stream)
+
+
+def nmdlm_block_step_paged_workspace_size(model: PagedModel, flags: int = 0) -> int:
+    return load().nmdlm_block_step_paged_workspace_size(C.byref(model.c), model.pages._ref, flags)
 
 
 def step_io(M, C_, pos0=0, flags=0, x_in=None, tokens=None, masked=None, k_unmask=0, y_out=None,

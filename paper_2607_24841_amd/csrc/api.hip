@@ -8,8 +8,9 @@
 
 namespace nmdlm {
 size_t block_step_ws_size(const nmdlm_model* md, int M, unsigned flags);
+size_t block_step_paged_ws_size(const nmdlm_model* md, const nmdlm_pages& pg, unsigned flags);
 nmdlm_status block_step_impl(const nmdlm_model* md, nmdlm_step_io* io, void* ws, size_t ws_bytes,
-                             hipStream_t st);
+                             hipStream_t st, const PagedStep* paged);
 }  // namespace nmdlm
 
 using namespace nmdlm;
@@ -61,6 +62,64 @@ bool weights_ok(const int8_t* W, int K, int N, int64_t ldw) {
   if (ldw < N || (ldw % 16) != 0) return false;
   if ((int64_t)K * ldw >= (int64_t)1 << 31) return false;
   return true;
+}
+
+// the layers' weights, tables and thresholds
+nmdlm_status layers_ok(const nmdlm_model* md, unsigned flags) {
+  if (md->n_layers > 0 && !md->layers) return NMDLM_ERR_INVALID_ARG;
+  const unsigned path_req = (flags >> NMDLM_PATH_SHIFT) & 0x7u;
+  const bool forced_blocked = path_req == 6u || path_req == 7u;
+  for (int l = 0; l < md->n_layers; ++l) {
+    const nmdlm_layer& L = md->layers[l];
+    if (!weights_ok(L.w_qkv, md->d, 3 * md->d, 3 * (int64_t)md->d) ||
+        !weights_ok(L.w_o, md->d, md->d, md->d) || !weights_ok(L.w_up, md->d, md->F, md->F) ||
+        !weights_ok(L.w_dn, md->F, md->d, md->d))
+      return NMDLM_ERR_INVALID_ARG;
+    if (!L.lut_att || !L.lut_act || !L.k_cache || !L.vt_cache) return NMDLM_ERR_INVALID_ARG;
+    if (!blocked_ok(L.w_qkv_b, md->d, 3 * md->d) || !blocked_ok(L.w_o_b, md->d, md->d) ||
+        !blocked_ok(L.w_up_b, md->d, md->F) || !blocked_ok(L.w_dn_b, md->F, md->d))
+      return NMDLM_ERR_INVALID_ARG;
+    // paths 6 and 7 (every word from the blocked copies) need every copy
+    if (forced_blocked && (!L.w_qkv_b || !L.w_o_b || !L.w_up_b || !L.w_dn_b))
+      return NMDLM_ERR_INVALID_ARG;
+    if (L.theta_q <= 0 || L.theta_k <= 0 || L.theta_v <= 0 || L.theta_a <= 0 || L.theta_o <= 0 ||
+        L.theta_up <= 0 || L.theta_dn <= 0)
+      return NMDLM_ERR_INVALID_ARG;
+    if (L.s_up < 0 || L.s_up > 31) return NMDLM_ERR_INVALID_ARG;
+  }
+  return NMDLM_OK;
+}
+
+// the head's weights and what it reads and writes
+nmdlm_status head_ok(const nmdlm_model* md, const nmdlm_step_io* io) {
+  if (io->flags & NMDLM_NO_HEAD) return NMDLM_OK;
+  const unsigned path_req = (io->flags >> NMDLM_PATH_SHIFT) & 0x7u;
+  const bool forced_blocked = path_req == 6u || path_req == 7u;
+  if (!weights_ok(md->w_head, md->d, md->V, md->V) || !md->head_scale ||
+      !blocked_ok(md->w_head_b, md->d, md->V) || (forced_blocked && !md->w_head_b))
+    return NMDLM_ERR_INVALID_ARG;
+  if (!io->tokens || !io->masked || io->k_unmask < 0) return NMDLM_ERR_INVALID_ARG;
+  return NMDLM_OK;
+}
+
+// timing events are plain records: not available inside stream capture
+nmdlm_status events_ok(const nmdlm_step_io* io, void* stream) {
+  if (!io->prof_events || io->n_prof_events <= 0) return NMDLM_OK;
+  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(static_cast<hipStream_t>(stream), &cs) != hipSuccess) return NMDLM_ERR_HIP;
+  return cs == hipStreamCaptureStatusNone ? NMDLM_OK : NMDLM_ERR_UNSUPPORTED;
+}
+
+// the sizes of a model
+nmdlm_status model_ok(const nmdlm_model* md) {
+  if (md->n_layers < 0 || md->T < 1 || md->d < 64 || md->H < 1 || md->F < 1 || md->V < 1)
+    return NMDLM_ERR_INVALID_ARG;
+  if (md->T > NMDLM_MAX_T) return NMDLM_ERR_UNSUPPORTED;
+  if (md->d % 64 != 0 || md->d % md->H != 0) return NMDLM_ERR_UNSUPPORTED;
+  const int dh = md->d / md->H;
+  if (dh != 64 && dh != 128) return NMDLM_ERR_UNSUPPORTED;
+  if (md->d > NMDLM_MAX_K || md->F > NMDLM_MAX_K) return NMDLM_ERR_UNSUPPORTED;
+  return NMDLM_OK;
 }
 
 }  // namespace
@@ -427,13 +486,8 @@ size_t nmdlm_block_step_workspace_size(const nmdlm_model* model, int M, unsigned
 nmdlm_status nmdlm_block_step(const nmdlm_model* md, nmdlm_step_io* io, void* ws, size_t ws_bytes,
                               void* stream) {
   if (!md || !io) return NMDLM_ERR_INVALID_ARG;
-  if (md->n_layers < 0 || md->T < 1 || md->d < 64 || md->H < 1 || md->F < 1 || md->V < 1)
-    return NMDLM_ERR_INVALID_ARG;
-  if (md->T > NMDLM_MAX_T) return NMDLM_ERR_UNSUPPORTED;
-  if (md->d % 64 != 0 || md->d % md->H != 0) return NMDLM_ERR_UNSUPPORTED;
-  const int dh = md->d / md->H;
-  if (dh != 64 && dh != 128) return NMDLM_ERR_UNSUPPORTED;
-  if (md->d > NMDLM_MAX_K || md->F > NMDLM_MAX_K) return NMDLM_ERR_UNSUPPORTED;
+  nmdlm_status rc = model_ok(md);
+  if (rc != NMDLM_OK) return rc;
   if (io->M < 1 || io->C < 0 || io->pos0 < 0) return NMDLM_ERR_INVALID_ARG;
   if (md->max_seq < 0 || io->n_seq < 0) return NMDLM_ERR_INVALID_ARG;
   const int n_seq = std::max(io->n_seq, 1);
@@ -446,49 +500,49 @@ nmdlm_status nmdlm_block_step(const nmdlm_model* md, nmdlm_step_io* io, void* ws
     return NMDLM_ERR_INVALID_ARG;
   if ((int64_t)io->C + io->M > NMDLM_MAX_KEYS || md->cache_cap / 64 > INT_MAX)
     return NMDLM_ERR_UNSUPPORTED;
-  if (md->n_layers > 0 && !md->layers) return NMDLM_ERR_INVALID_ARG;
-  const unsigned path_req = (io->flags >> NMDLM_PATH_SHIFT) & 0x7u;
-  const bool forced_blocked = path_req == 6u || path_req == 7u;
-  for (int l = 0; l < md->n_layers; ++l) {
-    const nmdlm_layer& L = md->layers[l];
-    if (!weights_ok(L.w_qkv, md->d, 3 * md->d, 3 * (int64_t)md->d) ||
-        !weights_ok(L.w_o, md->d, md->d, md->d) || !weights_ok(L.w_up, md->d, md->F, md->F) ||
-        !weights_ok(L.w_dn, md->F, md->d, md->d))
-      return NMDLM_ERR_INVALID_ARG;
-    if (!L.lut_att || !L.lut_act || !L.k_cache || !L.vt_cache) return NMDLM_ERR_INVALID_ARG;
-    if (!blocked_ok(L.w_qkv_b, md->d, 3 * md->d) || !blocked_ok(L.w_o_b, md->d, md->d) ||
-        !blocked_ok(L.w_up_b, md->d, md->F) || !blocked_ok(L.w_dn_b, md->F, md->d))
-      return NMDLM_ERR_INVALID_ARG;
-    // paths 6 and 7 (every word from the blocked copies) need every copy
-    if (forced_blocked && (!L.w_qkv_b || !L.w_o_b || !L.w_up_b || !L.w_dn_b))
-      return NMDLM_ERR_INVALID_ARG;
-    if (L.theta_q <= 0 || L.theta_k <= 0 || L.theta_v <= 0 || L.theta_a <= 0 || L.theta_o <= 0 ||
-        L.theta_up <= 0 || L.theta_dn <= 0)
-      return NMDLM_ERR_INVALID_ARG;
-    if (L.s_up < 0 || L.s_up > 31) return NMDLM_ERR_INVALID_ARG;
-  }
+  if ((rc = layers_ok(md, io->flags)) != NMDLM_OK) return rc;
   if (!io->x_in) {
     if (!md->emb || !md->pos_ch) return NMDLM_ERR_INVALID_ARG;
     if (!io->tokens && !io->masked) return NMDLM_ERR_INVALID_ARG;
     if ((int64_t)io->pos0 + io->M > md->max_pos) return NMDLM_ERR_INVALID_ARG;
   }
-  const bool head = !(io->flags & NMDLM_NO_HEAD);
-  if (head) {
-    if (!weights_ok(md->w_head, md->d, md->V, md->V) || !md->head_scale ||
-        !blocked_ok(md->w_head_b, md->d, md->V) || (forced_blocked && !md->w_head_b))
-      return NMDLM_ERR_INVALID_ARG;
-    if (!io->tokens || !io->masked || io->k_unmask < 0) return NMDLM_ERR_INVALID_ARG;
-    if (io->M > NMDLM_MAX_HEAD_M) return NMDLM_ERR_UNSUPPORTED;
-  }
+  if ((rc = head_ok(md, io)) != NMDLM_OK) return rc;
+  if (!(io->flags & NMDLM_NO_HEAD) && io->M > NMDLM_MAX_HEAD_M) return NMDLM_ERR_UNSUPPORTED;
   if (!ws || !aligned(ws, 256) || ws_bytes < block_step_ws_size(md, (int)Mt, io->flags))
     return NMDLM_ERR_WORKSPACE;
-  if (io->prof_events && io->n_prof_events > 0) {
-    // timing events are plain records: not available inside stream capture
-    hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
-    if (hipStreamIsCapturing(static_cast<hipStream_t>(stream), &cs) != hipSuccess) return NMDLM_ERR_HIP;
-    if (cs != hipStreamCaptureStatusNone) return NMDLM_ERR_UNSUPPORTED;
+  if ((rc = events_ok(io, stream)) != NMDLM_OK) return rc;
+  return block_step_impl(md, io, ws, ws_bytes, static_cast<hipStream_t>(stream), nullptr);
+}
+
+size_t nmdlm_block_step_paged_workspace_size(const nmdlm_model* md, const nmdlm_pages* pages, unsigned flags) {
+  if (!md || model_ok(md) != NMDLM_OK) return 0;
+  if (paged_call_ok(pages, md->T, md->H, md->d / md->H) != NMDLM_OK) return 0;
+  return block_step_paged_ws_size(md, *pages, flags);
+}
+
+nmdlm_status nmdlm_block_step_paged(const nmdlm_model* md, const nmdlm_pages* pages,
+                                    uint8_t* const* key_counts, int n_sel, nmdlm_step_io* io, void* ws,
+                                    size_t ws_bytes, void* stream) {
+  if (!md || !io) return NMDLM_ERR_INVALID_ARG;
+  nmdlm_status rc = model_ok(md);
+  if (rc != NMDLM_OK) return rc;
+  if ((rc = paged_call_ok(pages, md->T, md->H, md->d / md->H)) != NMDLM_OK) return rc;
+  if ((rc = layers_ok(md, io->flags)) != NMDLM_OK) return rc;
+  if (md->n_layers > 0 && !key_counts) return NMDLM_ERR_INVALID_ARG;
+  for (int l = 0; l < md->n_layers; ++l)
+    for (const void* p : {(const void*)md->layers[l].k_cache, (const void*)md->layers[l].vt_cache,
+                          (const void*)key_counts[l]})
+      if (!p || !aligned(p, 16)) return NMDLM_ERR_INVALID_ARG;
+  if (!io->x_in) {
+    if (!md->emb || !md->pos_ch || md->max_pos < 0) return NMDLM_ERR_INVALID_ARG;
+    if (!io->tokens && !io->masked) return NMDLM_ERR_INVALID_ARG;
   }
-  return block_step_impl(md, io, ws, ws_bytes, static_cast<hipStream_t>(stream));
+  if ((rc = head_ok(md, io)) != NMDLM_OK) return rc;
+  if (!ws || !aligned(ws, 256) || ws_bytes < block_step_paged_ws_size(md, *pages, io->flags))
+    return NMDLM_ERR_WORKSPACE;
+  if ((rc = events_ok(io, stream)) != NMDLM_OK) return rc;
+  const PagedStep paged{pages, key_counts, n_sel};
+  return block_step_impl(md, io, ws, ws_bytes, static_cast<hipStream_t>(stream), &paged);
 }
 
 nmdlm_status nmdlm_workspace_clear(void* ws, size_t ws_bytes, void* stream) {

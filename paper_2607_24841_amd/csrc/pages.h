@@ -105,6 +105,13 @@ struct PagedAttnCall {
   void* ws;
 };
 
+// A block step over pages: each layer's k_cache / vt_cache are its pools.
+struct PagedStep {
+  const nmdlm_pages* pages;
+  uint8_t* const* key_counts;  // host array [n_layers]
+  int n_sel;                   // selected context pages, or below 0: all
+};
+
 nmdlm_status launch_page_plan(const nmdlm_pages& pg, const int32_t* ctx, const int32_t* rows,
                               int32_t* status, hipStream_t st);
 nmdlm_status launch_page_store(const nmdlm_pages& pg, const uint64_t* k, const uint64_t* v, int T, int H,

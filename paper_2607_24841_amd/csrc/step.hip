@@ -7,6 +7,7 @@
 #include <algorithm>
 
 #include "common.h"
+#include "pages.h"
 
 namespace nmdlm {
 
@@ -36,6 +37,43 @@ __global__ __launch_bounds__(256) void k_assemble(const uint64_t* __restrict__ e
   uint64_t word = emb[((size_t)tok * T + t) * dw + w];
   const int pc = pos_ch[(size_t)(pos0 + m % Mseq) * T + t];
   if ((pc >> 6) == w) word |= 1ull << (pc & 63);
+  X[i] = word;
+}
+
+// The same for the packed rows of a page plan: row m at position pos[m] of its
+// request.  Rows without a page are empty; a position past the table has no
+// position spike and sets NMDLM_STATUS_BAD_REQUEST.
+__global__ __launch_bounds__(256) void k_assemble_rows(const uint64_t* __restrict__ emb,
+                                                       const int32_t* __restrict__ pos_ch, int max_pos,
+                                                       const int32_t* __restrict__ tokens,
+                                                       const uint8_t* __restrict__ masked,
+                                                       const int64_t* __restrict__ slot,
+                                                       const int32_t* __restrict__ pos, int V, int T,
+                                                       int M, int dw, uint64_t* __restrict__ X,
+                                                       int32_t* __restrict__ status) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (long long)T * M * dw) return;
+  const int w = (int)(i % dw);
+  const int m = (int)((i / dw) % M);
+  const int t = (int)(i / ((long long)dw * M));
+  if (slot[m] < 0) {
+    X[i] = 0ull;
+    return;
+  }
+  int tok = (masked && masked[m]) ? V : (tokens ? tokens[m] : V);
+  int bits = 0;
+  if (tok < 0 || tok > V) {
+    bits = NMDLM_STATUS_TOKEN_CLAMPED;
+    tok = min(max(tok, 0), V);
+  }
+  uint64_t word = emb[((size_t)tok * T + t) * dw + w];
+  if (pos[m] < max_pos) {
+    const int pc = pos_ch[(size_t)pos[m] * T + t];
+    if ((pc >> 6) == w) word |= 1ull << (pc & 63);
+  } else {
+    bits |= NMDLM_STATUS_BAD_REQUEST;
+  }
+  if (bits && status && t == 0 && w == 0) atomicOr(status, bits);
   X[i] = word;
 }
 
@@ -169,18 +207,12 @@ __global__ __launch_bounds__(kConfThreads) void k_conf(const ConfPart* __restric
 constexpr int kUnmaskMaxM = 64 * 64;
 static_assert(kUnmaskMaxM >= NMDLM_MAX_HEAD_M, "unmask register mask covers every head step");
 
-__global__ __launch_bounds__(64) void k_unmask(int32_t* __restrict__ tokens,
-                                               uint8_t* __restrict__ masked,
-                                               const int32_t* __restrict__ pred,
-                                               const double* __restrict__ conf, int M, int k,
-                                               int32_t* __restrict__ chosen) {
+__device__ __forceinline__ void unmask_block(int32_t* __restrict__ tokens,
+                                             uint8_t* __restrict__ masked,
+                                             const int32_t* __restrict__ pred,
+                                             const double* __restrict__ conf, int M, int k,
+                                             int32_t* __restrict__ chosen) {
   const int lane = threadIdx.x;
-  const size_t so = (size_t)blockIdx.x * M;
-  tokens += so;
-  masked += so;
-  pred += so;
-  conf += so;
-  if (chosen) chosen += (size_t)blockIdx.x * k;
   if (M <= 64) {
     // one position per lane: its rank among the masked positions (higher
     // confidence first, ties to the lower position) decides it in one pass;
@@ -243,6 +275,33 @@ __global__ __launch_bounds__(64) void k_unmask(int32_t* __restrict__ tokens,
   }
 }
 
+__global__ __launch_bounds__(64) void k_unmask(int32_t* __restrict__ tokens,
+                                               uint8_t* __restrict__ masked,
+                                               const int32_t* __restrict__ pred,
+                                               const double* __restrict__ conf, int M, int k,
+                                               int32_t* __restrict__ chosen) {
+  const size_t so = (size_t)blockIdx.x * M;
+  unmask_block(tokens + so, masked + so, pred + so, conf + so, M, k,
+               chosen ? chosen + (size_t)blockIdx.x * k : nullptr);
+}
+
+// The same for the requests of a page plan: request s's rows [cu[s], cu[s+1])
+// (at most kUnmaskMaxM of them).  Rows without a page (a refused request's)
+// are left as they are, with nothing chosen.
+__global__ __launch_bounds__(64) void k_unmask_rows(int32_t* __restrict__ tokens,
+                                                    uint8_t* __restrict__ masked,
+                                                    const int32_t* __restrict__ pred,
+                                                    const double* __restrict__ conf,
+                                                    const int32_t* __restrict__ cu,
+                                                    const int64_t* __restrict__ slot, int k,
+                                                    int32_t* __restrict__ chosen) {
+  const int r0 = cu[blockIdx.x];
+  int M = min(cu[blockIdx.x + 1] - r0, kUnmaskMaxM);
+  if (M > 0 && slot[r0] < 0) M = 0;
+  unmask_block(tokens + r0, masked + r0, pred + r0, conf + r0, M, k,
+               chosen ? chosen + (size_t)blockIdx.x * k : nullptr);
+}
+
 // ---------------------------------------------------------------------------
 // workspace layout of a block step
 // ---------------------------------------------------------------------------
@@ -303,6 +362,30 @@ static void carve_step(Carver& cv, const nmdlm_model* md, int M, unsigned flags,
   b->pred = (head && need_pred) ? cv.take<int32_t>(M) : nullptr;
   b->conf = (head && need_conf) ? cv.take<double>(M) : nullptr;
   carve_qbsm_scratch(cv, step_limits(md, M, flags), &b->qs);
+}
+
+// What a step over pages has besides: keys and values of the rows, the
+// selection and the calls' workspaces.
+struct PagedBuffers {
+  uint64_t *K, *V, *sel;
+  char *ws_select, *ws_attn;
+};
+static void carve_paged(Carver& cv, const nmdlm_model* md, const nmdlm_pages& pg, PagedBuffers* b) {
+  const size_t sp = (size_t)md->T * pg.max_rows * (md->d / 64);
+  b->K = cv.take<uint64_t>(sp);
+  b->V = cv.take<uint64_t>(sp);
+  b->sel = cv.take<uint64_t>((size_t)pg.max_rows * md->H * ((pg.max_pages + 63) / 64));
+  b->ws_select = cv.take<char>(page_select_ws(pg, md->H));
+  b->ws_attn = cv.take<char>(paged_attn_ws(pg, md->T, md->H, md->d / md->H));
+}
+
+size_t block_step_paged_ws_size(const nmdlm_model* md, const nmdlm_pages& pg, unsigned flags) {
+  Carver cv{nullptr, 0, (size_t)-1, true};
+  StepBuffers b;
+  PagedBuffers pb;
+  carve_step(cv, md, pg.max_rows, flags, true, true, true, true, &b);
+  carve_paged(cv, md, pg, &pb);
+  return align_up(cv.off, 256);
 }
 
 size_t block_step_ws_size(const nmdlm_model* md, int M, unsigned flags) {
@@ -377,9 +460,11 @@ static void attach_events(QbsmCall& c, const nmdlm_step_io* io, int i) {
 }
 
 nmdlm_status block_step_impl(const nmdlm_model* md, nmdlm_step_io* io, void* ws, size_t ws_bytes,
-                             hipStream_t st) {
-  // Ms tokens in each of n_seq sequences; every product takes all M rows
-  const int T = md->T, Ms = io->M, n_seq = std::max(io->n_seq, 1), M = n_seq * Ms, C = io->C;
+                             hipStream_t st, const PagedStep* paged) {
+  // Ms tokens in each of n_seq sequences, or the packed rows of a page plan; every
+  // product takes all M rows
+  const int T = md->T, Ms = paged ? paged->pages->max_rows : io->M;
+  const int n_seq = paged ? 1 : std::max(io->n_seq, 1), M = n_seq * Ms, C = io->C;
   const int d = md->d, F = md->F, H = md->H;
   const int dh = d / H, dw = d / 64, Fw = (F + 63) / 64;
   const int64_t cap = md->cache_cap, capw = cap / 64;
@@ -390,11 +475,25 @@ nmdlm_status block_step_impl(const nmdlm_model* md, nmdlm_step_io* io, void* ws,
   StepBuffers b;
   carve_step(cv, md, M, io->flags, io->x_in == nullptr, io->logits == nullptr,
              io->pred == nullptr, io->conf == nullptr, &b);
+  PagedBuffers pb{};
+  if (paged) carve_paged(cv, md, *paged->pages, &pb);
   if (!cv.ok) return NMDLM_ERR_WORKSPACE;
 
   nmdlm_status rc = NMDLM_OK;
   const uint64_t* X = io->x_in;
-  if (!X) {
+  if (paged) {
+    // attention writes no rows without a page: those stay empty through the layers
+    if ((rc = launch_fill_zero(b.A, align_up((size_t)T * M * dw * 8, 16), st)) != NMDLM_OK) return rc;
+    if ((rc = launch_fill_zero(b.uA, align_up((size_t)M * dw * 8, 16), st)) != NMDLM_OK) return rc;
+  }
+  if (!X && paged) {
+    const long long total = (long long)T * M * dw;
+    hipLaunchKernelGGL(k_assemble_rows, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, md->emb,
+                       md->pos_ch, md->max_pos, io->tokens, io->masked, paged->pages->slot, paged->pages->pos,
+                       md->V, T, M, dw, b.X, io->status);
+    if ((rc = hip_status()) != NMDLM_OK) return rc;
+    X = b.X;
+  } else if (!X) {
     const long long total = (long long)T * M * dw;
     hipLaunchKernelGGL(k_assemble, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st,
                        md->emb, md->pos_ch, io->tokens, io->masked, md->V, T, M, Ms, dw, io->pos0,
@@ -424,6 +523,10 @@ nmdlm_status block_step_impl(const nmdlm_model* md, nmdlm_step_io* io, void* ws,
     qkv.seg[2].transposed = 1;
     qkv.seg[2].ld_p = d;
     qkv.seg[2].pos0 = C;
+    if (paged) {
+      qkv.seg[1] = natural_seg(pb.K, sp_t, dw, ly.theta_k);
+      qkv.seg[2] = natural_seg(pb.V, sp_t, dw, ly.theta_v);
+    }
     if (n_seq > 1) {
       qkv.seq_len = Ms;
       for (int i = 1; i < 3; ++i) {
@@ -437,10 +540,23 @@ nmdlm_status block_step_impl(const nmdlm_model* md, nmdlm_step_io* io, void* ws,
     attach_events(qkv, io, 4 * l + 0);
     if ((rc = launch_qbsm(qkv, b.qs, st)) != NMDLM_OK) return rc;
 
-    AttnCall at{b.Q, ly.k_cache, ly.vt_cache, cap, T, Ms, C, H, dh, n_seq, seq_words, ly.lut_att,
-                ly.theta_a, nullptr, b.a, b.A, b.uA,
-                (io->flags & NMDLM_ATTN_FUSED) != 0 && n_seq == 1, true};
-    if ((rc = launch_attention(at, st)) != NMDLM_OK) return rc;
+    if (paged) {
+      const nmdlm_pages& pg = *paged->pages;
+      uint8_t* const counts = paged->key_counts[l];
+      if ((rc = launch_page_store(pg, pb.K, pb.V, T, H, dh, ly.k_cache, ly.vt_cache, counts, st)) != NMDLM_OK)
+        return rc;
+      if (paged->n_sel >= 0 && (rc = launch_page_select(pg, b.Q, T, H, dh, counts, paged->n_sel, pb.sel,
+                                                        pb.ws_select, st)) != NMDLM_OK)
+        return rc;
+      const PagedAttnCall pa{b.Q, ly.k_cache, ly.vt_cache, T, H, dh, ly.lut_att,
+                             paged->n_sel >= 0 ? pb.sel : nullptr, nullptr, ly.theta_a, b.A, b.uA, pb.ws_attn};
+      if ((rc = launch_paged_attn(pg, pa, st)) != NMDLM_OK) return rc;
+    } else {
+      AttnCall at{b.Q, ly.k_cache, ly.vt_cache, cap, T, Ms, C, H, dh, n_seq, seq_words, ly.lut_att,
+                  ly.theta_a, nullptr, b.a, b.A, b.uA,
+                  (io->flags & NMDLM_ATTN_FUSED) != 0 && n_seq == 1, true};
+      if ((rc = launch_attention(at, st)) != NMDLM_OK) return rc;
+    }
 
     QbsmCall o = base_call(b.A, T, M, d, ly.w_o, d, d, EPI_IF, io->flags, stl ? stl + 1 : nullptr);
     o.seg[0] = natural_seg(b.X1, sp_t, dw, ly.theta_o);
@@ -510,6 +626,11 @@ nmdlm_status block_step_impl(const nmdlm_model* md, nmdlm_step_io* io, void* ws,
   if ((rc = hip_status()) != NMDLM_OK) return rc;
   hipLaunchKernelGGL(k_conf, dim3(M), dim3(kConfThreads), 0, st, b.cpart, nch, pred, conf);
   if ((rc = hip_status()) != NMDLM_OK) return rc;
+  if (paged) {
+    hipLaunchKernelGGL(k_unmask_rows, dim3(paged->pages->n_seq), dim3(64), 0, st, io->tokens, io->masked, pred,
+                       conf, paged->pages->cu_rows, paged->pages->slot, io->k_unmask, io->unmasked_pos);
+    return hip_status();
+  }
   hipLaunchKernelGGL(k_unmask, dim3(n_seq), dim3(64), 0, st, io->tokens, io->masked, pred, conf,
                      Ms, io->k_unmask, io->unmasked_pos);
   return hip_status();

@@ -3,7 +3,8 @@
 finished block's keys/values stay in the caches as context.  The host only
 loops and marshals; every step runs in libnmdlm's kernels and the token
 state stays on the device until the end.  Several sequences (prompts of
-one length) advance together, one batched step per denoising step."""
+one length) advance together, one batched step per denoising step; requests
+of different lengths share pools of pages (PagedGenerator)."""
 from __future__ import annotations
 
 import numpy as np
@@ -77,3 +78,89 @@ def generate_batch(dm: B.DeviceModel, prompts: np.ndarray, n_blocks: int, block:
     out = g.run(ids, n_blocks, steps, k_unmask, log)
     torch.cuda.synchronize()
     return out.cpu().numpy(), [c.cpu().numpy() for c in log]
+
+
+class PagedGenerator:
+    """Block diffusion for up to n_seq requests of different lengths at once.
+
+    Their keys and values live in one pool of pages a layer, `pool` pages of 64
+    positions for all requests, at most max_len positions for one.  A request is
+    admitted with its prompt, advances by one block a call of run_block and
+    gives its pages back when it is released.  n_sel: context pages that a row
+    and head attends to besides its block's own (None: all)."""
+
+    def __init__(self, dm: B.DeviceModel, n_seq: int, block: int, max_len: int, pool: int,
+                 max_prompt_rows: int | None = None, n_sel: int | None = None):
+        self.block, self.n, self.n_sel = block, n_seq, -1 if n_sel is None else int(n_sel)
+        max_pages = -(-max_len // B.NMDLM_PAGE)
+        # prompts go through a plan of their own over the same tables: a step's
+        # rows are as many as its plan has room for
+        self.pages = B.Pages(n_seq, n_seq * block, max_pages, pool)
+        self.prompt_pages = self.pages.view(max_prompt_rows or max_len)
+        self.model = B.PagedModel(dm, self.pages)
+        self.prompt_model = self.model.view(self.prompt_pages, head=False)
+        self.ws = B.workspace(max(
+            B.nmdlm_block_step_paged_workspace_size(self.model, 0),
+            B.nmdlm_block_step_paged_workspace_size(self.prompt_model, B.NMDLM_NO_HEAD)))
+        self.ctx = np.zeros(n_seq, dtype=np.int32)      # positions that a request holds
+        self.live = np.zeros(n_seq, dtype=bool)
+        rows = n_seq * block
+        self.tokens = torch.zeros(rows, dtype=torch.int32, device="cuda")
+        self.masked = torch.ones(rows, dtype=torch.uint8, device="cuda")
+        self.chosen = torch.zeros(n_seq, block, dtype=torch.int32, device="cuda")
+        self.status = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def _plan(self, pages: B.Pages, new: np.ndarray) -> None:
+        """Makes the step's plan; raises when a request does not get its pages."""
+        self.status.zero_()
+        B.nmdlm_page_plan(pages, torch.from_numpy(self.ctx).cuda(),
+                          torch.from_numpy(new.astype(np.int32)).cuda(), status=self.status)
+        bits = int(self.status)
+        if bits:
+            raise RuntimeError("the pool has too few pages" if bits == B.NMDLM_STATUS_PAGES_SHORT
+                               else f"a request is longer than the plan holds (status {bits})")
+
+    def admit(self, prompts: dict[int, np.ndarray]) -> None:
+        """Prefills the prompts (request number -> ids) in one step."""
+        new = np.zeros(self.n, dtype=np.int64)
+        for s, ids in prompts.items():
+            if self.live[s]:
+                raise ValueError(f"request {s} is running")
+            new[s] = len(ids)
+        rows = int(new.sum())
+        if rows > self.prompt_pages.max_rows or any(n < 1 for n in new[list(prompts)]):
+            raise ValueError(f"prompts of {rows} tokens in all: 1 to {self.prompt_pages.max_rows}")
+        self._plan(self.prompt_pages, new)
+        ids = np.zeros(self.prompt_pages.max_rows, dtype=np.int32)
+        ids[:rows] = np.concatenate([np.asarray(prompts[s]) for s in sorted(prompts)])
+        tokens = torch.from_numpy(ids).cuda()
+        io = B.step_io(0, 0, flags=B.NMDLM_NO_HEAD, tokens=tokens)
+        B.nmdlm_block_step_paged(self.prompt_model, io, self.ws, n_sel=self.n_sel)
+        for s in prompts:
+            self.ctx[s], self.live[s] = new[s], True
+
+    def run_block(self, steps: int, k_unmask: int, log: list | None = None) -> dict[int, torch.Tensor]:
+        """One block for every running request: request number -> its ids."""
+        order = np.flatnonzero(self.live)
+        new = np.where(self.live, self.block, 0)
+        self._plan(self.pages, new)
+        self.tokens.zero_()
+        self.masked.fill_(1)
+        chosen = self.chosen.view(-1)[:self.n * k_unmask].view(self.n, k_unmask)
+        io = B.step_io(0, 0, tokens=self.tokens, masked=self.masked, k_unmask=k_unmask,
+                       unmasked_pos=self.chosen)
+        for _ in range(steps):
+            B.nmdlm_block_step_paged(self.model, io, self.ws, n_sel=self.n_sel)
+            if log is not None:
+                log.append(chosen.clone())
+        self.ctx += new.astype(np.int32)
+        out = self.tokens[:len(order) * self.block].view(len(order), self.block).clone()
+        return {int(s): out[i] for i, s in enumerate(order)}
+
+    def release(self, requests) -> None:
+        """Gives the pages of the requests back."""
+        new = np.zeros(self.n, dtype=np.int64)
+        new[list(requests)] = -1
+        self._plan(self.pages, new)
+        for s in requests:
+            self.ctx[s], self.live[s] = 0, False

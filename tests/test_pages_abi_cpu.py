@@ -136,6 +136,41 @@ def test_binding_checks_its_tensors():
         B.Pages(0, 10, 3, 7, device="cpu")
 
 
+def test_step_over_pages_argument_errors():
+    lib = B.load()
+    layer = [FAKE] * 4 + [200] * 7 + [4] + [FAKE] * 4
+
+    def model(n=1, d=128, H=2, T=4, layers=layer, head=None, pos=FAKE):
+        arr = (B.Layer * 1)(B.Layer(*layers))
+        return B.Model(n, d, H, 256, 300, T, 0, 10, arr, FAKE, pos, head, head)
+
+    def call(m=None, p=None, counts=FAKE, io=None, ws=FAKE, less=0):
+        m, p = m or model(), p or pages()
+        arr = None if counts is None else (C.c_void_p * 1)(counts or None)
+        io = io or B.step_io(0, 0, flags=B.NMDLM_NO_HEAD, tokens=FAKE)
+        need = lib.nmdlm_block_step_paged_workspace_size(C.byref(m), C.byref(p), io.flags)
+        return lib.nmdlm_block_step_paged(C.byref(m), C.byref(p), arr, 2, C.byref(io), ws, max(need - less, 0), None)
+    assert call(counts=None) == INVALID
+    assert call(counts=0) == INVALID
+    assert call(counts=FAKE + 8) == INVALID
+    assert call(m=model(layers=layer[:12] + [FAKE, FAKE, FAKE + 8, FAKE])) == INVALID   # key pages
+    assert call(m=model(layers=layer[:12] + [FAKE, FAKE, FAKE, None])) == INVALID
+    assert call(m=model(layers=layer[:5] + [0] + layer[6:])) == INVALID                 # a threshold of 0
+    assert call(m=model(d=192, H=2)) == UNSUPPORTED                                     # heads of 96
+    assert call(m=model(T=9)) == UNSUPPORTED
+    assert call(p=pages(pool=0)) == INVALID
+    assert call(p=pages(max_rows=(1 << 17) + 1)) == UNSUPPORTED
+    assert call(m=model(pos=None)) == INVALID                                           # no token tables
+    assert call(io=B.step_io(0, 0, flags=B.NMDLM_NO_HEAD)) == INVALID                   # and no input
+    assert call(io=B.step_io(0, 0, tokens=FAKE, masked=FAKE)) == INVALID                # a head without weights
+    assert call(m=model(head=FAKE), io=B.step_io(0, 0, tokens=FAKE, masked=FAKE, k_unmask=-1)) == INVALID
+    assert call(ws=None) == WORKSPACE
+    assert call(less=1) == WORKSPACE
+    assert lib.nmdlm_block_step_paged_workspace_size(None, C.byref(pages()), 0) == 0
+    assert lib.nmdlm_block_step_paged_workspace_size(C.byref(model(T=9)), C.byref(pages()), 0) == 0
+    assert lib.nmdlm_block_step_paged_workspace_size(C.byref(model()), C.byref(pages(pool=0)), 0) == 0
+
+
 def test_constants_match_the_header():
     import re
 
