@@ -561,24 +561,40 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_token(PagedArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Which grid.
+// Which kernel and grid; the lengths are on the device, the rule sees the plan's
+// sizes.  All measured with spikes out, H = 16, T = 4, dh = 128 unless said.
+//  * The token kernel up to 2 rows a request (and 8 rows more, a plan's spare
+//    ones): 64 requests x 1 row x 4001 keys 100 us against 133 in tiles, x 501 keys 20
+//    against 30; 2 rows 136 against 132 and 30 against 31; 3 rows 181 against 133.  One
+//    request of 8 rows x 508 keys 6.9 against 10.7, x 4008 keys 18.0 against 15.1.
+//  * 32 rows a wave (QG = 2) where the tiles give 1024 such waves: 4 x 200 rows x
+//    500 keys 24 us against 29 with 16, 1 x 2048 x 2348 109 against 135, T = 1, 16 x
+//    100 x 400 17.0 against 18.5; below, T = 4, 1 x 300 x 600 19.5 against 17.6, T = 1,
+//    1 x 1024 x 1324 26 against 18.
+//  * Parts: eight waves a workgroup where T allows (32 x 16 x 2016 keys, one, two
+//    and four parts: T = 1 26, 21 and 15 us, T = 2 34, 23 and 23, T = 4 38 and 36); sixteen
+//    waves (T = 4, four parts) 46.
+//  * Splits to give each CU one workgroup of tiles, or two of tokens: 1 x 16 rows x
+//    64016 keys 391 us whole, 109 in 4, 42 in 16, 43 in 32; 4 x 16 x 16016 105 whole, 42 in
+//    4 (one a CU), 47 in 6 (some CUs two), 42 in 8; 64 selected of 2047 pages, 32
+//    rows, 70 whole, 25 in 8 (one a CU), 31 in 10 or 16.  16 x 16 x 2016 keys, a
+//    workgroup a CU without: 23 whole, 40 in 2.
 // ---------------------------------------------------------------------------
 struct PagedRoute {
   bool token;
   int groups, parts, splits;
 };
 static PagedRoute paged_route(const nmdlm_pages& pg, int T, int H) {
+  PagedRoute r{pg.max_rows <= 2LL * pg.n_seq + 8, 1, T <= 2 ? 4 : (T <= 4 ? 2 : 1), 1};
   const long long t32 = pg.max_rows / 32 + pg.n_seq;
-  PagedRoute r{false, 1, T <= 2 ? 4 : (T <= 4 ? 2 : 1), 1};
-  if (pg.max_rows <= 2LL * pg.n_seq + 8) {
-    r.token = true;
-  } else if (pg.max_rows >= 32LL * pg.n_seq && t32 * H * T >= 2048) {
+  if (!r.token && pg.max_rows >= 32LL * pg.n_seq && t32 * H * T >= 1024) {
     r.groups = 2;
     r.parts = 1;
     return r;
   }
-  const long long tiles = r.token ? pg.max_rows : std::max((pg.max_rows + 15) / 16, pg.n_seq);
-  r.splits = (int)std::max(1LL, std::min<long long>({(r.token ? 1024 : 512) / (tiles * H), 64,
+  // rows or tiles of every request, less what a plan may have to spare
+  const long long units = std::max(r.token ? pg.max_rows / 2 : pg.max_rows / 16, pg.n_seq);
+  r.splits = (int)std::max(1LL, std::min<long long>({(r.token ? 512 : 256) / (units * H), 64,
                                                      pg.max_pages / kSplitPages}));
   return r;
 }
