@@ -580,11 +580,7 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_token(PagedArgs a) {
 //    rows, 70 whole, 25 in 8 (one a CU), 31 in 10 or 16.  16 x 16 x 2016 keys, a
 //    workgroup a CU without: 23 whole, 40 in 2.
 // ---------------------------------------------------------------------------
-struct PagedRoute {
-  bool token;
-  int groups, parts, splits;
-};
-static PagedRoute paged_route(const nmdlm_pages& pg, int T, int H) {
+PagedRoute paged_route(const nmdlm_pages& pg, int T, int H) {
   PagedRoute r{pg.max_rows <= 2LL * pg.n_seq + 8, 1, T <= 2 ? 4 : (T <= 4 ? 2 : 1), 1};
   const long long t32 = pg.max_rows / 32 + pg.n_seq;
   if (!r.token && pg.max_rows >= 32LL * pg.n_seq && t32 * H * T >= 1024) {

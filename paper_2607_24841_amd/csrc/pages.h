@@ -117,10 +117,17 @@ nmdlm_status launch_page_plan(const nmdlm_pages& pg, const int32_t* ctx, const i
 nmdlm_status launch_page_store(const nmdlm_pages& pg, const uint64_t* k, const uint64_t* v, int T, int H,
                                int dh, uint64_t* k_pages, uint64_t* v_pages, uint8_t* counts,
                                hipStream_t st);
+bool select_fused(const nmdlm_pages& pg, int H);  // scores and choice in one kernel
 size_t page_select_ws(const nmdlm_pages& pg, int H);
 nmdlm_status launch_page_select(const nmdlm_pages& pg, const uint64_t* q, int T, int H, int dh,
                                 const uint8_t* counts, int n_sel, uint64_t* sel, void* ws,
                                 hipStream_t st);
+// The row kernel or tiles of 16 * groups rows, waves a timestep, most splits.
+struct PagedRoute {
+  bool token;
+  int groups, parts, splits;
+};
+PagedRoute paged_route(const nmdlm_pages& pg, int T, int H);
 size_t paged_attn_ws(const nmdlm_pages& pg, int T, int H, int dh);
 nmdlm_status launch_paged_attn(const nmdlm_pages& pg, const PagedAttnCall& c, hipStream_t st);
 

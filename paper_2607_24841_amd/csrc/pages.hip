@@ -195,8 +195,11 @@ __device__ void plan_rows(const PlanArgs& a, const int32_t* cu, const PageReq* r
   }
 }
 
-// One launch for few rows and requests: what the rows look up stays in LDS.
-constexpr int kPlanOneRows = 4096;
+// One launch for few rows and requests: what the rows look up stays in LDS.  64
+// requests of 8 rows 7.6 us (with the copy that puts the state back) against 9.6 in
+// two launches, of 32 10.2 against 10.9, of 63 12.5 against 11.4; 1000 of one 9.9
+// against 11.8; 8 of 250 8.5 against 9.5, of 500 10.3 against 9.4.
+constexpr int kPlanOneRows = 2560;
 __global__ __launch_bounds__(kPlanThreads) void k_page_plan(PlanArgs a) {
   __shared__ int32_t sCu[kPlanThreads + 1];
   __shared__ PageReq sReq[kPlanThreads];
@@ -631,13 +634,21 @@ __global__ __launch_bounds__(64 * kSelectWaves) void k_page_select(SelectArgs a)
   }
 }
 
-// Scores of up to kSelectPages pages stay in LDS (33 KB), where the table is no wider.
-constexpr int kSelectPages = 512;
+// One kernel where the table is narrow and its workgroups, which choose after
+// they score, fill the chip: 32 requests of 16 rows, 93 context pages, 12.7 us
+// against 14.2 in two kernels; one such request 9.2 against 7.4; 187 pages, one
+// request 13.2 against 9.0, eight 13.2 against 10.1.
+constexpr int kSelectPages = 128;
+bool select_fused(const nmdlm_pages& pg, int H) {
+  return pg.max_pages <= kSelectPages && std::max(pg.max_rows / 16, pg.n_seq) * H >= 256;
+}
 
 size_t page_select_ws(const nmdlm_pages& pg, int H) {
-  if (pg.max_pages <= kSelectPages) return 0;
+  if (select_fused(pg, H)) return 0;
   return align_up((size_t)pg.max_rows * H * select_ld(pg) * sizeof(int32_t), 256);
 }
+
+constexpr size_t kSelectPlainLds = 57344;  // dynamic LDS that needs no attribute beside the static
 
 template <int DHW>
 static nmdlm_status launch_select(const nmdlm_pages& pg, const uint64_t* q, int T, int H,
@@ -648,10 +659,11 @@ static nmdlm_status launch_select(const nmdlm_pages& pg, const uint64_t* q, int 
   SelectArgs a{ix.t16, pg.table, q, counts, sel, static_cast<int32_t*>(ws), pg.max_pages, pg.pool,
                pg.max_rows, (pg.max_pages + 63) / 64, T, H, n_sel, select_ld(pg)};
   const size_t stage = 16 * score_ld(T * DHW) * sizeof(v4i);  // of a wave
-  if (pg.max_pages <= kSelectPages) {
+  if (select_fused(pg, H)) {
     a.ld += 1;  // a row's bank past the row before's
     const size_t lds = kSelectWaves * stage + (size_t)a.ld * 16 * sizeof(int32_t);
-    if (hipFuncSetAttribute(reinterpret_cast<const void*>(&k_page_select<DHW>),
+    if (lds > kSelectPlainLds &&
+        hipFuncSetAttribute(reinterpret_cast<const void*>(&k_page_select<DHW>),
                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
       return NMDLM_ERR_HIP;
     hipLaunchKernelGGL(k_page_select<DHW>, dim3(ix.n16, H), dim3(64 * kSelectWaves), lds, st, a);

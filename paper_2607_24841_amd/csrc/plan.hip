@@ -3,6 +3,7 @@
 // is stored channel-major.  Not part of the installed header; nothing is
 // launched and no GPU is needed.
 #include "common.h"
+#include "pages.h"
 
 using namespace nmdlm;
 
@@ -68,6 +69,21 @@ void nmdlm_internal_attn_route(int T, int M, int C, int H, int dh, int n_seq, in
   out[0] = r.groups;
   out[1] = r.parts;
   out[2] = r.split ? 1 : 0;
+}
+
+// The route of a paged attention call: 1 for the row kernel, 16-row groups of a
+// wave, waves per timestep, most splits; and 1 when the selection is one kernel.
+void nmdlm_internal_paged_route(int n_seq, int max_rows, int max_pages, int T, int H, int32_t* out) {
+  nmdlm_pages pg{};
+  pg.n_seq = n_seq;
+  pg.max_rows = max_rows;
+  pg.max_pages = max_pages;
+  const PagedRoute r = paged_route(pg, T, H);
+  out[0] = r.token ? 1 : 0;
+  out[1] = r.groups;
+  out[2] = r.parts;
+  out[3] = r.splits;
+  out[4] = select_fused(pg, H) ? 1 : 0;
 }
 
 // The runs of row block y of M tokens into out[4 i ..]: sequence, first position,

@@ -130,7 +130,13 @@ class PagedGenerator:
         rows = int(new.sum())
         if rows > self.prompt_pages.max_rows or any(n < 1 for n in new[list(prompts)]):
             raise ValueError(f"prompts of {rows} tokens in all: 1 to {self.prompt_pages.max_rows}")
-        self._plan(self.prompt_pages, new)
+        try:
+            self._plan(self.prompt_pages, new)
+        except RuntimeError:   # what the others of them were given goes back
+            self.status.zero_()
+            B.nmdlm_page_plan(self.prompt_pages, torch.from_numpy(self.ctx).cuda(),
+                              torch.from_numpy(np.where(new > 0, -1, 0).astype(np.int32)).cuda())
+            raise
         ids = np.zeros(self.prompt_pages.max_rows, dtype=np.int32)
         ids[:rows] = np.concatenate([np.asarray(prompts[s]) for s in sorted(prompts)])
         tokens = torch.from_numpy(ids).cuda()

@@ -88,6 +88,22 @@ def attention(c, p, sel=None):
     return cur, spk
 
 
+def route(n_seq, max_rows, max_pages, T, H):
+    """The kernels a call takes (a host-side query): by rows, 16-row groups of a
+    wave, waves per timestep, most splits, selection in one kernel."""
+    import ctypes as C
+
+    from paper_2607_24841_amd import binding as B
+
+    out = (C.c_int32 * 5)()
+    B.load().nmdlm_internal_paged_route(n_seq, max_rows, max_pages, T, H, out)
+    return SimpleNamespace(token=bool(out[0]), groups=out[1], parts=out[2], splits=out[3], fused=bool(out[4]))
+
+
+def case_route(c):
+    return route(c.n, c.max_rows, c.max_pages, c.T, c.H)
+
+
 class Device:
     """The case on the GPU."""
 

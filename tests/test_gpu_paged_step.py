@@ -73,14 +73,20 @@ def test_pool_runs_out():
     from paper_2607_24841_amd.generate import PagedGenerator
 
     m = small_model()
-    g = PagedGenerator(device_model(B, m), 2, 8, max_len=192, pool=3)
+    g = PagedGenerator(device_model(B, m), 2, 8, max_len=192, pool=3, max_prompt_rows=210)
     ps = prompts_of([100, 100], m.V)
     g.admit({0: ps[0]})
     with pytest.raises(RuntimeError, match="too few pages"):
         g.admit({1: ps[1]})
+    assert g.pages.ring_state.tolist()[1] == 1 and g.pages.held.tolist() == [2, 0]
     with pytest.raises(ValueError):
         g.admit({1: np.zeros(0, np.int32)})
-    # the first goes on
+    g.release([0])
+    with pytest.raises(RuntimeError, match="too few pages"):
+        g.admit({0: ps[0], 1: ps[1]})         # the first's pages go back with the refusal
+    assert g.pages.ring_state.tolist()[1] == 3 and g.pages.held.tolist() == [0, 0]
+    g.admit({0: ps[0]})
+    # and it goes on by itself
     want = O.generate(m, ps[0], 1, 8, 2, 4)[0]
     assert_same(g.run_block(2, 4)[0].cpu().numpy(), want, "ids")
 

@@ -215,6 +215,34 @@ def test_select_long():
     assert_same(d.selection(), P.select(c, P.plan(c), 40), "selected pages")
 
 
+@pytest.mark.parametrize("T,H,dh,n_sel", [(4, 4, 64, 3), (1, 4, 128, 1), (8, 4, 128, 20), (3, 4, 64, 0)])
+def test_select_one_kernel(T, H, dh, n_sel):
+    """Requests enough for scores and choice in one kernel."""
+    rng = np.random.default_rng(T)
+    ctx, new = rng.integers(0, 900, size=70), rng.integers(1, 20, size=70)
+    ctx[0], new[0], new[1] = 64 * 126, 17, 0
+    c = P.make_case(T + 24, ctx, new, T=T, H=H, dh=dh, spare_pages=0)
+    assert P.case_route(c).fused
+    d = device(c)
+    d.plan()
+    d.select(n_sel)
+    sync()
+    assert_same(d.selection(), P.select(c, P.plan(c), n_sel), "selected pages")
+
+
+@pytest.mark.parametrize("n_sel", [1, 64, 600])
+def test_select_widths(n_sel):
+    """Contexts in every class of the choice: up to 64, 128, 512 and 2048 pages and more."""
+    pages = [64, 65, 128, 129, 512, 513, 700, 2048, 2049]
+    c = P.make_case(25, [64 * p for p in pages], [1] * len(pages), T=1, H=1)
+    assert not P.case_route(c).fused
+    d = device(c)
+    d.plan()
+    d.select(n_sel)
+    sync()
+    assert_same(d.selection(), P.select(c, P.plan(c), n_sel), "selected pages")
+
+
 # --------------------------------------------------------------------------
 # attention
 # --------------------------------------------------------------------------
@@ -303,6 +331,40 @@ def test_attention_wide_tiles(T, H, dh, sel):
     p = P.plan(c)
     s = some_selection(c, p, 2, 0.2) if sel else None
     d.attention(sel=d.put_selection(s) if sel else None)
+    sync()
+    cur, spk = P.attention(c, p, s)
+    assert_same(d.cur.cpu().numpy(), cur, "currents")
+    assert_same(d.spikes(), spk, "spikes")
+
+
+@pytest.mark.parametrize("T,H,dh,share", [(1, 64, 64, None), (2, 20, 128, 0.3), (8, 5, 128, None)])
+def test_attention_wide_tiles_other_timesteps(T, H, dh, share):
+    c = P.make_case(51, [100, 0], [600, 333], T=T, H=H, dh=dh)
+    assert P.case_route(c).groups == 2
+    d = device(c)
+    d.plan()
+    p = P.plan(c)
+    s = None if share is None else some_selection(c, p, 3, share)
+    d.attention(sel=None if s is None else d.put_selection(s))
+    sync()
+    cur, spk = P.attention(c, p, s)
+    assert_same(d.cur.cpu().numpy(), cur, "currents")
+    assert_same(d.spikes(), spk, "spikes")
+
+
+@pytest.mark.parametrize("new,splits", [(1, 20), (20, 20)])
+@pytest.mark.parametrize("share", [None, 0.1, 0.0])
+def test_attention_many_splits(new, splits, share):
+    """Rows and tiles over a context in many splits, whole, selected and with
+    nothing selected; a short request beside it in one."""
+    c = P.make_case(52, [64 * 160, 40], [new, new], T=3, H=1, dh=128)
+    r = P.case_route(c)
+    assert r.token == (new == 1) and r.splits == splits
+    d = device(c)
+    d.plan()
+    p = P.plan(c)
+    s = None if share is None else some_selection(c, p, 3, share)
+    d.attention(sel=None if s is None else d.put_selection(s))
     sync()
     cur, spk = P.attention(c, p, s)
     assert_same(d.cur.cpu().numpy(), cur, "currents")

@@ -171,6 +171,27 @@ def test_step_over_pages_argument_errors():
     assert lib.nmdlm_block_step_paged_workspace_size(C.byref(model()), C.byref(pages(pool=0)), 0) == 0
 
 
+def test_routes():
+    from ._pages import route
+
+    # rows by themselves up to two a request
+    assert route(64, 64, 70, 4, 16).token and route(64, 136, 70, 4, 16).token
+    assert not route(64, 137, 70, 4, 16).token and not route(1, 16, 70, 4, 16).token
+    # 32 rows a wave from 1024 such waves on, of requests that fill them
+    assert route(1, 480, 20, 4, 16).groups == 2 and route(1, 479, 20, 4, 16).groups == 1
+    assert route(20, 639, 20, 4, 16).groups == 1
+    # splits: as many as fill the chip, of eight pages at least, none beside wide tiles
+    assert route(1, 16, 2000, 4, 16).splits == 16 and route(1, 16, 20, 4, 16).splits == 2
+    assert route(1, 16, 7, 4, 16).splits == 1 and route(16, 256, 500, 4, 16).splits == 1
+    assert route(1, 1, 2000, 4, 16).splits == 32 and route(1, 1, 2000, 1, 1).splits == 64
+    assert route(1, 2000, 2000, 4, 16).splits == 1
+    for T in range(1, 9):
+        for r in (route(1, 1, 9, T, 1), route(2, 60, 9, T, 1), route(1, 4000, 9, T, 64)):
+            assert 1 <= T * r.parts <= 8
+    assert route(64, 64, 128, 4, 4).fused and not route(63, 64, 128, 4, 4).fused
+    assert not route(64, 64, 129, 4, 16).fused
+
+
 def test_constants_match_the_header():
     import re
 
