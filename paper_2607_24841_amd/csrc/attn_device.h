@@ -153,7 +153,10 @@ struct AttnChunk {
   uint64_t k[DHW], v[DHW];
 };
 
-template <int DHW, int QG>
+// FUSED: the value bits' shift and OR in one instruction, where the compiler
+// takes two and shares the shift; 3% of the paged kernels' time, but two registers
+// too many for the contiguous ones' occupancy.
+template <int DHW, int QG, bool FUSED = false>
 struct AttnWave {
   static constexpr int NT = DHW * 4;
   v4i q[QG][DHW];
@@ -285,7 +288,9 @@ struct AttnWave {
     for (int n = 0; n < NT; ++n) {
       const uint32_t h = v[n];
       cnt[n] += __popc(h);
-      const v4i va = bytes16(h | (h << 12));
+      uint32_t x = h | (h << 12);
+      if constexpr (FUSED) asm("v_lshl_or_b32 %0, %1, 12, %1" : "=v"(x) : "v"(h));
+      const v4i va = bytes16(x);
 #pragma unroll
       for (int w = 0; w < QG; ++w)
         acc[w][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(va, p[w], acc[w][n], 0, 0, 0);

@@ -228,9 +228,9 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_paged_att
 
   const LutRegs lr = load_lut(a.lut, tid, nth);
   uint32_t qraw[QG];
-  AttnWave<DHW, QG>::load_queries(qraw, a.q + ((size_t)t * a.max_rows + tl.row) * dw + h * DHW, dw, 0,
+  AttnWave<DHW, QG, true>::load_queries(qraw, a.q + ((size_t)t * a.max_rows + tl.row) * dw + h * DHW, dw, 0,
                                   nr - 1, g, c);
-  AttnWave<DHW, QG> w;
+  AttnWave<DHW, QG, true> w;
   const char* lb = reinterpret_cast<const char*>(&sLut);
   // words of a pool page; a head's and timestep's keys and values in it
   const size_t page_words = (size_t)a.H * a.T * (64 * DHW), at_ht = ((size_t)h * a.T + t) * (64 * DHW);
