@@ -70,7 +70,8 @@ __device__ __forceinline__ int32_t* split_sums(const PagedArgs& a, int row, int 
 template <int DHW>
 __device__ __forceinline__ void load_page(AttnChunk<DHW>& ch, const uint64_t* __restrict__ kp,
                                           const uint64_t* __restrict__ vp, size_t at, int lane) {
-  const uint64_t *kr = kp + at, *vr = vp + at;
+  typedef const __attribute__((address_space(1))) uint64_t gword;  // global, beyond the asm too
+  gword *kr = (gword*)(kp + at), *vr = (gword*)(vp + at);
   // the page's address stays in scalar registers, the lane's offset in one of its own
   asm("" : "+s"(kr), "+s"(vr));
 #pragma unroll
