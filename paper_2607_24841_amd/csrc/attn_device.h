@@ -44,6 +44,21 @@ __device__ __forceinline__ v4i attn_norm4(v4i num, int den_i) {
   return a;
 }
 
+// attn_norm4 in two: the factor k of a denominator and four numerators.
+__device__ __forceinline__ float attn_factor(float den) {
+  return __builtin_amdgcn_rcpf(den) * (256.0f - 0x1p-12f);
+}
+__device__ __forceinline__ v4i attn_norm4(v4i num, float den, float k) {
+  v4i a;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float n = (float)num[e];
+    const float q = __builtin_truncf(n * k);
+    a[e] = (int)q + (__builtin_fmaf(-q, den, 256.0f * n) >= den ? 1 : 0);
+  }
+  return a;
+}
+
 // One numerator, as attn_norm4 for fewer than 65536 keys and else as attn_norm.
 __device__ __forceinline__ int32_t attn_norm1(int num, int den_i, bool small) {
   if (!small) return attn_norm(num, den_i);

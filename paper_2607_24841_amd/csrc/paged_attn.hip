@@ -81,22 +81,40 @@ __device__ __forceinline__ void load_page(AttnChunk<DHW>& ch, const uint64_t* __
   }
 }
 
-// The neuron of 16 rows: cur(t, n, lane) is the normalised current of row lane%16,
-// channels 16n + 4(lane/16) + e; waves share the NT tiles.  All threads of the
-// workgroup call it.
-template <int DHW, typename F>
-__device__ __forceinline__ void fire_rows(const PagedArgs& a, uint32_t (*sWord)[16][2 * DHW], int row0,
-                                          int nr, int h, int tid, int nth, F cur) {
+// The neuron of 16 rows over their sums: sNum [part][t][tile][lane] (row lane%16,
+// channels 16n + 4(lane/16) + e) and sDen [part][t][row].  Waves share the NT
+// tiles of 16 channels; a timestep's weights are summed and inverted once for
+// all tiles of a wave.  All threads of the workgroup call it.
+template <int DHW>
+__device__ __forceinline__ void fire_rows(const PagedArgs& a, const v4i* sNum, const int (*sDen)[16],
+                                          uint32_t (*sWord)[16][2 * DHW], int row0, int nr, int h, bool small,
+                                          int tid, int nth) {
   constexpr int NT = DHW * 4, DH = DHW * 64;
-  const int lane = tid & 63, wave = tid >> 6, nwaves = nth >> 6, g = lane >> 4, c = lane & 15;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nwaves = nth >> 6;
+  const int g = lane >> 4, c = lane & 15;
   const int d = a.H * DH, dw = d / 64;
   const bool vec = (reinterpret_cast<uintptr_t>(a.a_out) & 15) == 0;
   for (int i = tid; i < a.T * 32 * DHW; i += nth) (&sWord[0][0][0])[i] = 0u;
   __syncthreads();
-  for (int n = wave; n < NT; n += nwaves) {
-    v4i V = v4i{0, 0, 0, 0};
-    for (int t = 0; t < a.T; ++t) {
-      const v4i x = cur(t, n, lane);
+  v4i V[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) V[j] = v4i{0, 0, 0, 0};
+  for (int t = 0; t < a.T; ++t) {
+    int den = 0;
+    for (int p = 0; p < a.parts; ++p) den += sDen[p * a.T + t][c];
+    const float den_f = (float)max(den, 1), k = attn_factor(den_f);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int n = wave + j * nwaves;
+      if (n >= NT) break;  // wave-uniform
+      v4i x = sNum[(t * NT + n) * 64 + lane];
+      for (int p = 1; p < a.parts; ++p) x += sNum[((p * a.T + t) * NT + n) * 64 + lane];
+      if (small) {  // uniform
+        x = attn_norm4(x, den_f, k);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = attn_norm(x[e], den);
+      }
       if (a.a_out && c < nr) {
         int32_t* o = a.a_out + ((size_t)t * a.max_rows + row0 + c) * d + h * DH + n * 16 + 4 * g;
         if (vec) {
@@ -109,9 +127,9 @@ __device__ __forceinline__ void fire_rows(const PagedArgs& a, uint32_t (*sWord)[
       uint32_t bits = 0u;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        V[e] += x[e];
-        const bool s = V[e] >= a.theta;
-        if (s) V[e] -= a.theta;
+        V[j][e] += x[e];
+        const bool s = V[j][e] >= a.theta;
+        if (s) V[j][e] -= a.theta;
         bits |= (uint32_t)s << e;
       }
       atomicOr(&sWord[t][c][n >> 1], bits << (16 * (n & 1) + 4 * g));
@@ -132,14 +150,6 @@ __device__ __forceinline__ void fire_rows(const PagedArgs& a, uint32_t (*sWord)[
       for (int t = 0; t < a.T; ++t) uor |= sWord[t][m][2 * k] | (uint64_t)sWord[t][m][2 * k + 1] << 32;
       if (m < nr) a.u_out[(size_t)(row0 + m) * dw + h * DHW + k] = uor;
     }
-}
-
-__device__ __forceinline__ v4i normalise(v4i x, int den, bool small) {
-  if (small) return attn_norm4(x, den);
-  v4i r;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) r[e] = attn_norm(x[e], den);
-  return r;
 }
 
 // The rows that see page `lane` of a word (bit per row): lane r holds row r's word.
@@ -206,12 +216,12 @@ template <int DHW, int QG, bool SEL>
 __global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_paged_attn(PagedArgs a) {
   constexpr int NT = DHW * 4;
   __shared__ AttnLut sLut;
-  __shared__ int sDen[NMDLM_MAX_T][16];
+  __shared__ int sDen[NMDLM_MAX_T][16];  // [part][T], at most eight waves
   __shared__ uint32_t sWord[NMDLM_MAX_T][16][2 * DHW];
   __shared__ PageEntry sList[kPageList];
   __shared__ uint32_t sSeen[SEL ? kPageList : 1];
   __shared__ int sCount[SEL ? kListWords : 1];
-  extern __shared__ v4i sNum[];  // the waves' stages, then the sums [T][NT][64]
+  extern __shared__ v4i sNum[];  // the waves' stages, then their sums [part][T][NT][64]
   AttnStage<DHW>* sStage = reinterpret_cast<AttnStage<DHW>*>(sNum);
 
   touch_kernargs<sizeof(PagedArgs)>();
@@ -327,35 +337,32 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_paged_att
 #pragma unroll
   for (int u = 0; u < QG; ++u) {
     if (u > 0) __syncthreads();  // the sums and words of the group before are read
-    const int rows = nr - 16 * u;
-    for (int i = tid; i < a.T * NT * 64; i += nth) sNum[i] = v4i{0, 0, 0, 0};
-    for (int i = tid; i < a.T * 16; i += nth) (&sDen[0][0])[i] = 0;
-    __syncthreads();
+    const int rows = nr - 16 * u, pt = part * a.T + t;
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        atomicAdd(reinterpret_cast<int*>(&sNum[(t * NT + n) * 64 + lane]) + e, w.acc[u][n][e]);
-    if (g == 0) atomicAdd(&sDen[t][c], w.den[u] + 128 * keys);
+    for (int n = 0; n < NT; ++n) sNum[(pt * NT + n) * 64 + lane] = w.acc[u][n];
+    if (g == 0) sDen[pt][c] = w.den[u] + 128 * keys;
     __syncthreads();
     if (splits > 1) {  // uniform
       for (int i = tid; i < a.T * NT * 64; i += nth) {
         const int tt = i / (NT * 64), n = (i >> 6) % NT, r = i & 15, lg = (i >> 4) & 3;
-        if (r < rows)
+        if (r < rows) {
+          v4i x = sNum[i];
+          for (int p = 1; p < np; ++p) x += sNum[p * a.T * NT * 64 + i];
           *reinterpret_cast<v4i*>(split_sums<DHW>(a, tl.row + 16 * u + r, h, z) +
-                                  (size_t)tt * (64 * DHW + kPartDen) + 16 * n + 4 * lg) = sNum[i];
+                                  (size_t)tt * (64 * DHW + kPartDen) + 16 * n + 4 * lg) = x;
+        }
       }
       for (int i = tid; i < a.T * 16; i += nth)
-        if (i % 16 < rows)
+        if (i % 16 < rows) {
+          int den = 0;
+          for (int p = 0; p < np; ++p) den += sDen[p * a.T + i / 16][i % 16];
           split_sums<DHW>(a, tl.row + 16 * u + i % 16, h, z)[(size_t)(i / 16) * (64 * DHW + kPartDen) + 64 * DHW] =
-              sDen[i / 16][i % 16];
+              den;
+        }
       continue;
     }
     if (rows <= 0) continue;  // uniform
-    const bool small = J < 65536;
-    fire_rows<DHW>(a, sWord, tl.row + 16 * u, min(rows, 16), h, tid, nth, [&](int tt, int n, int l) {
-      return normalise(sNum[(tt * NT + n) * 64 + l], sDen[tt][l & 15], small);
-    });
+    fire_rows<DHW>(a, sNum, sDen, sWord, tl.row + 16 * u, min(rows, 16), h, J < 65536, tid, nth);
   }
 }
 
@@ -609,8 +616,8 @@ constexpr size_t kPagedPlainLds = 49152;  // dynamic LDS that needs no attribute
 
 template <int DHW, int QG, bool SEL>
 static nmdlm_status launch_paged(const PagedArgs& a, dim3 grid, hipStream_t st) {
-  const size_t dyn = std::max((size_t)a.T * DHW * 4 * 64 * sizeof(v4i),
-                              (size_t)a.T * a.parts * kAttnStages * sizeof(AttnStage<DHW>));
+  const size_t dyn = (size_t)a.T * a.parts * std::max(DHW * 4 * 64 * sizeof(v4i),
+                                                      kAttnStages * sizeof(AttnStage<DHW>));
   if (dyn > kPagedPlainLds &&
       hipFuncSetAttribute(reinterpret_cast<const void*>(&k_paged_attn<DHW, QG, SEL>),
                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)dyn) != hipSuccess)
