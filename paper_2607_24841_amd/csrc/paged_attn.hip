@@ -63,6 +63,12 @@ __device__ __forceinline__ int32_t* split_sums(const PagedArgs& a, int row, int 
 // (attn_device.h).  With a selection an entry of the list has one bit per row
 // that sees the page (a score that a row does not see weighs 0, byte -128).  The
 // parts of a timestep take the list's entries in turn.
+//
+// Bound by instruction issue: a page and 16 rows cost 173 vector instructions, 16
+// MFMAs and 32 LDS instructions (vector 72% of the busy cycles, matrix cores 27%, LDS
+// 50%).  T = 4, 16 heads of 128: 32 requests x 16 rows x 2016 keys 34 us, 4.0 TB/s and
+// 1.0 POP/s; 32 rows a wave, 3 x 2048 x 2048 243 us, 1.7 POP/s (one request 92 us,
+// where the contiguous cache's kernel takes 87).
 // ---------------------------------------------------------------------------
 
 // One wave's loads of a page: key row `lane`, value words of channels lane (and
@@ -392,7 +398,8 @@ __device__ __forceinline__ void fire_row(const PagedArgs& a, int row, int h, int
 
 // k_paged_join: the sums of a row's splits (integers: any order gives the same)
 // and the neuron.  A workgroup per row and head, a wave per timestep and 64
-// channels.
+// channels: 5 us for 32 rows of 16 heads in 8 splits, a chain of three loads (18 us
+// with a workgroup per tile and head).
 template <int DHW>
 __global__ __launch_bounds__(64 * NMDLM_MAX_T * DHW) void k_paged_join(PagedArgs a, const PageTile* rows) {
   constexpr int LD = 64 * DHW + kPartDen;
@@ -440,7 +447,8 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T * DHW) void k_paged_join(PagedArgs
 //     sum_j p_j V[j,c] = sum_b 2^b popcount(mask_b AND word of channel c).
 // About 100 vector instructions a page of 128 channels, no exchange between
 // lanes, and few registers: the loads of kTokenAhead pages are in flight in each
-// of many waves.
+// of many waves.  Bound by HBM: T = 4, 16 heads of 128, 64 requests x 2048 keys, 268 MB,
+// 46 us or 5.8 TB/s (64 in tiles).
 // ---------------------------------------------------------------------------
 constexpr int kTokenAhead = 4;
 
