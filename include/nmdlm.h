@@ -525,7 +525,8 @@ size_t nmdlm_block_step_workspace_size(const nmdlm_model* model, int M,
  * requests one after the other: spikes [T][max_rows][H*dh/64], rows
  * [cu_rows[s], cu_rows[s+1]) being request s's.  Rows past the last
  * request's are not read as queries, keys or values, and nothing is written
- * for them.  A page belongs to one request.
+ * for them.  A page belongs to one request.  The calls after nmdlm_page_plan read
+ * what it left on the device, so they follow it in stream order.
  *
  * The plan is device memory of the caller.  The table, held, ring and
  * ring_state arrays live from step to step; initially held = 0, ring = the page numbers 0 .. pool-1

@@ -124,8 +124,8 @@ class PagedGenerator:
         """Prefills the prompts (request number -> ids) in one step."""
         new = np.zeros(self.n, dtype=np.int64)
         for s, ids in prompts.items():
-            if self.live[s]:
-                raise ValueError(f"request {s} is running")
+            if not 0 <= s < self.n or self.live[s]:
+                raise ValueError(f"request {s}: running, or not one of {self.n}")
             new[s] = len(ids)
         rows = int(new.sum())
         if rows > self.prompt_pages.max_rows or any(n < 1 for n in new[list(prompts)]):
@@ -166,7 +166,10 @@ class PagedGenerator:
     def release(self, requests) -> None:
         """Gives the pages of the requests back."""
         new = np.zeros(self.n, dtype=np.int64)
-        new[list(requests)] = -1
+        for s in requests:
+            if not 0 <= s < self.n:
+                raise ValueError(f"request {s}: not one of {self.n}")
+            new[s] = -1
         self._plan(self.pages, new)
         for s in requests:
             self.ctx[s], self.live[s] = 0, False

@@ -71,7 +71,7 @@ def test_plan(name):
 
 
 @pytest.mark.parametrize("n,hi,seed", [(1, 5000, 0), (37, 40, 1), (300, 12, 2), (1024, 3, 3), (1025, 200, 4),
-                                       (3000, 30, 5), (700, 0, 6)])
+                                       (3000, 30, 5), (700, 0, 6), (16384, 9, 7)])
 def test_plan_many(n, hi, seed):
     """One launch and two, more requests than a chunk of the sums, and the ring
     running out."""
@@ -256,7 +256,8 @@ SHAPES = {
 
 
 @pytest.mark.parametrize("name", SHAPES)
-@pytest.mark.parametrize("T,H,dh", [(1, 1, 64), (2, 3, 128), (3, 2, 64), (4, 2, 128), (8, 1, 64)])
+@pytest.mark.parametrize("T,H,dh", [(1, 1, 64), (2, 3, 128), (3, 2, 64), (4, 2, 128), (5, 1, 128), (7, 2, 64),
+                                    (8, 1, 64)])
 def test_attention(name, T, H, dh):
     c = P.make_case(T + H, *SHAPES[name], T=T, H=H, dh=dh)
     d = device(c)
@@ -290,11 +291,13 @@ def test_attention_selected(name, T, H, dh, share):
     assert_same(d.spikes(), spk, "spikes")
 
 
+@pytest.mark.parametrize("new", [(3, 2), (14, 9)])
 @pytest.mark.parametrize("dh,share", [(64, None), (128, None), (64, 0.4), (128, 0.02)])
-def test_attention_long(dh, share):
-    """Contexts of more pages than the kernel lists at once, from 65536 keys on
-    (sums beyond 24 bits), beside a short one."""
-    c = P.make_case(40, [64 * 1200 + 7, 30], [3, 2], T=1, H=1, dh=dh)
+def test_attention_long(new, dh, share):
+    """Contexts from 65536 keys on (sums beyond 24 bits) beside a short one, by
+    rows and by tiles."""
+    c = P.make_case(40, [64 * 1200 + 7, 30], new, T=1, H=1, dh=dh)
+    assert P.case_route(c).token == (new == (3, 2))
     c.lut[:] = 255
     d = device(c)
     d.plan()
@@ -457,6 +460,66 @@ def test_together(T, H, dh):
     run_all(d, 3)
     sync()
     check_all(d, c, 3)
+
+
+@pytest.mark.parametrize("new", [20, 1])
+def test_refused_requests_between_others(new):
+    """Rows of refused requests are neither selected for nor attended, whichever
+    kernel takes the rows."""
+    c = P.make_case(72, [100, 0, 70, 0, 200], [new, new, new, 70 if new > 1 else 1, new], T=2, H=2, dh=64, spare_rows=0)
+    assert P.case_route(c).token == (new == 1)
+    c.ctx[2] = 129                            # beyond its pages
+    c.ring_state[1] = 1                       # the second takes the only page
+    d = device(c)
+    run_all(d, 1)
+    sync()
+    p = P.plan(c)
+    assert p["ok"].tolist() == [True, True, False, False, True]
+    check_all(d, c, 1)
+
+
+def test_nothing_to_do():
+    """Idle and ended requests only: no row, nothing written."""
+    c = P.make_case(73, [100, 0, 70], [0, 0, -1], T=2, H=2, dh=64)
+    d = device(c)
+    run_all(d, 1)
+    sync()
+    check_all(d, c, 1)
+
+
+def test_a_pool_beyond_32_bits():
+    """Pages whose words lie past 2^32 of the pool's first."""
+    import torch
+
+    c = P.make_case(74, [64 * 9, 30], [9, 1], T=8, H=16, dh=128)
+    d = device(c)
+    words = 16 * 8 * 128                     # of a page's keys, and of its values
+    pool, shift = 2 ** 32 // words + 40 + c.pool, 2 ** 32 // words + 40
+    free, _ = torch.cuda.mem_get_info()
+    if free < 2 * 8 * pool * words + pool * words + (8 << 30):
+        pytest.skip("not enough memory")
+    n = P.Device.__new__(P.Device)
+    n.__dict__.update(d.__dict__)
+    n.pages = d.B.Pages(c.n, c.max_rows, c.max_pages, pool)
+    move = lambda x: torch.where(x >= 0, x + shift, x)  # noqa: E731
+    ring = torch.zeros(pool, dtype=torch.int32, device="cuda")
+    head, k = c.ring_state
+    ring[:k] = torch.from_numpy(c.ring[(head + np.arange(k)) % c.pool].astype(np.int32)).cuda() + shift
+    n.pages.set_state(move(d.pages.table), d.pages.held, ring, torch.tensor([0, k], dtype=torch.int32))
+    n.k_pages, n.v_pages, n.counts = n.pages.pools(8, 16, 128)
+    for big, small in ((n.k_pages, d.k_pages), (n.v_pages, d.v_pages), (n.counts, d.counts)):
+        big[shift:] = small
+    run_all(n, 3)
+    sync()
+    n.k_pages, n.v_pages, n.counts = (x[shift:].clone() for x in (n.k_pages, n.v_pages, n.counts))
+    p = P.plan(c)
+    store_oracle(c, p)
+    check_store(n, c)
+    sel = P.select(c, p, 3)
+    cur, spk = P.attention(c, p, sel)
+    assert_same(n.selection(), sel, "selected pages")
+    assert_same(n.cur.cpu().numpy(), cur, "currents")
+    assert_same(n.spikes(), spk, "spikes")
 
 
 def test_on_another_stream_and_in_a_graph():
