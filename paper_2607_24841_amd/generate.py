@@ -84,14 +84,19 @@ class PagedGenerator:
     """Block diffusion for up to n_seq requests of different lengths at once.
 
     Their keys and values live in one pool of pages a layer, `pool` pages of 64
-    positions for all requests, at most max_len positions for one.  A request is
-    admitted with its prompt, advances by one block a call of run_block and
-    gives its pages back when it is released.  n_sel: context pages that a row
-    and head attends to besides its block's own (None: all)."""
+    positions for all requests, at most max_len positions for one (and no more
+    than the model's position table has: `limit`).  A request is admitted with
+    its prompt, advances by one block a call of run_block and gives its pages
+    back when it is released.  n_sel: context pages that a row and head attends
+    to besides its block's own (None: all).
+
+    admit and run_block raise ValueError before anything is taken when a request
+    would pass its limit; run_block goes on once that request is released."""
 
     def __init__(self, dm: B.DeviceModel, n_seq: int, block: int, max_len: int, pool: int,
                  max_prompt_rows: int | None = None, n_sel: int | None = None):
         self.block, self.n, self.n_sel = block, n_seq, -1 if n_sel is None else int(n_sel)
+        self.limit = min(max_len, dm.max_pos)           # positions of a request
         max_pages = -(-max_len // B.NMDLM_PAGE)
         # prompts go through a plan of their own over the same tables: a step's
         # rows are as many as its plan has room for
@@ -109,6 +114,12 @@ class PagedGenerator:
         self.masked = torch.ones(rows, dtype=torch.uint8, device="cuda")
         self.chosen = torch.zeros(n_seq, block, dtype=torch.int32, device="cuda")
         self.status = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def _check_lengths(self, new: np.ndarray) -> None:
+        """A step has no position spike to give past the position table, so no
+        request is taken there."""
+        for s in np.flatnonzero((new > 0) & (self.ctx + new > self.limit)):
+            raise ValueError(f"request {s}: {self.ctx[s]} positions and {new[s]} new ones, of at most {self.limit}")
 
     def _plan(self, pages: B.Pages, new: np.ndarray) -> None:
         """Makes the step's plan; raises when a request does not get its pages."""
@@ -130,6 +141,7 @@ class PagedGenerator:
         rows = int(new.sum())
         if rows > self.prompt_pages.max_rows or any(n < 1 for n in new[list(prompts)]):
             raise ValueError(f"prompts of {rows} tokens in all: 1 to {self.prompt_pages.max_rows}")
+        self._check_lengths(new)
         try:
             self._plan(self.prompt_pages, new)
         except RuntimeError:   # what the others of them were given goes back
@@ -149,6 +161,7 @@ class PagedGenerator:
         """One block for every running request: request number -> its ids."""
         order = np.flatnonzero(self.live)
         new = np.where(self.live, self.block, 0)
+        self._check_lengths(new)
         self._plan(self.pages, new)
         self.tokens.zero_()
         self.masked.fill_(1)

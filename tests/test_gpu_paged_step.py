@@ -196,3 +196,27 @@ def test_positions_past_the_table_and_ids_outside_it():
     B.nmdlm_block_step_paged(pm, B.step_io(0, 0, flags=B.NMDLM_NO_HEAD, tokens=tokens, status=status), ws)
     torch.cuda.synchronize()
     assert int(status) == B.NMDLM_STATUS_TOKEN_CLAMPED | B.NMDLM_STATUS_BAD_REQUEST
+
+
+@pytest.mark.parametrize("max_len,max_pos", [(192, 70), (70, 512)])
+def test_generator_stops_at_the_last_position(max_len, max_pos):
+    """70 positions, by the position table or by the caller's word (pages hold
+    more): no block begins past them, and what the others get is unchanged."""
+    torch, B = need_gpu()
+    from paper_2607_24841_amd.generate import PagedGenerator
+
+    m = small_model(max_pos=max_pos)
+    g = PagedGenerator(device_model(B, m), 2, 8, max_len=max_len, pool=6, max_prompt_rows=128)
+    ps = prompts_of([62, 40], m.V)
+    with pytest.raises(ValueError, match="request 0"):
+        g.admit({0: synth.random_tokens(9, 71, m.V)})
+    g.admit({0: ps[0], 1: ps[1]})
+    a = g.run_block(2, 4)
+    free = g.pages.ring_state.tolist()
+    with pytest.raises(ValueError, match="request 0"):
+        g.run_block(2, 4)
+    assert g.pages.ring_state.tolist() == free and g.ctx.tolist() == [70, 48]
+    g.release([0])
+    b = g.run_block(2, 4)
+    assert_same(a[0].cpu().numpy(), O.generate(m, ps[0], 1, 8, 2, 4)[0], "up to the last position")
+    assert_same(torch.cat([a[1], b[1]]).cpu().numpy(), O.generate(m, ps[1], 2, 8, 2, 4)[0], "the other")
