@@ -91,10 +91,13 @@ class PagedGenerator:
     to besides its block's own (None: all).
 
     admit and run_block raise ValueError before anything is taken when a request
-    would pass its limit; run_block goes on once that request is released."""
+    would pass its limit; run_block goes on once that request is released.  A
+    block has at most NMDLM_MAX_HEAD_M rows, all that a step can unmask."""
 
     def __init__(self, dm: B.DeviceModel, n_seq: int, block: int, max_len: int, pool: int,
                  max_prompt_rows: int | None = None, n_sel: int | None = None):
+        if not 1 <= block <= B.NMDLM_MAX_HEAD_M:
+            raise ValueError(f"a block of {block} rows: 1 to {B.NMDLM_MAX_HEAD_M}")
         self.block, self.n, self.n_sel = block, n_seq, -1 if n_sel is None else int(n_sel)
         self.limit = min(max_len, dm.max_pos)           # positions of a request
         max_pages = -(-max_len // B.NMDLM_PAGE)

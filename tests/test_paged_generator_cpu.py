@@ -33,3 +33,9 @@ def test_requests_past_their_last_position():
     for live in ((1, 0, 0), (1, 1, 0)):      # up to the last one; released requests do not count
         with pytest.raises(AssertionError, match="planned"):
             bare(ctx=(92, 92, 93), live=live).run_block(1, 1)
+
+
+@pytest.mark.parametrize("block", [-1, 0, 4097])
+def test_blocks_that_a_step_cannot_unmask(block):
+    with pytest.raises(ValueError, match="block"):
+        G.PagedGenerator(SimpleNamespace(max_pos=1 << 20), 1, block, max_len=1 << 14, pool=256)
