@@ -129,13 +129,20 @@ class PagedGenerator:
         self.status.zero_()
         B.nmdlm_page_plan(pages, torch.from_numpy(self.ctx).cuda(),
                           torch.from_numpy(new.astype(np.int32)).cuda(), status=self.status)
+        self._check_status()
+
+    def _check_status(self) -> None:
+        """Raises for what the plan, or the steps since, have set."""
         bits = int(self.status)
+        if bits & B.NMDLM_STATUS_TOKEN_CLAMPED:
+            raise ValueError("token ids outside the model's table")
         if bits:
             raise RuntimeError("the pool has too few pages" if bits == B.NMDLM_STATUS_PAGES_SHORT
                                else f"a request is longer than the plan holds (status {bits})")
 
     def admit(self, prompts: dict[int, np.ndarray]) -> None:
-        """Prefills the prompts (request number -> ids) in one step."""
+        """Prefills the prompts (request number -> ids of the model's table) in
+        one step; when it raises, none of them is admitted."""
         new = np.zeros(self.n, dtype=np.int64)
         for s, ids in prompts.items():
             if not 0 <= s < self.n or self.live[s]:
@@ -145,18 +152,19 @@ class PagedGenerator:
         if rows > self.prompt_pages.max_rows or any(n < 1 for n in new[list(prompts)]):
             raise ValueError(f"prompts of {rows} tokens in all: 1 to {self.prompt_pages.max_rows}")
         self._check_lengths(new)
+        ids = np.zeros(self.prompt_pages.max_rows, dtype=np.int32)
+        # ids beyond 32 bits stay outside the table
+        ids[:rows] = np.clip(np.concatenate([np.asarray(prompts[s]) for s in sorted(prompts)]), -1, 2**31 - 1)
         try:
             self._plan(self.prompt_pages, new)
-        except RuntimeError:   # what the others of them were given goes back
-            self.status.zero_()
+            tokens = torch.from_numpy(ids).cuda()
+            io = B.step_io(0, 0, flags=B.NMDLM_NO_HEAD, tokens=tokens, status=self.status)
+            B.nmdlm_block_step_paged(self.prompt_model, io, self.ws, n_sel=self.n_sel)
+            self._check_status()
+        except (RuntimeError, ValueError):   # what they were given goes back
             B.nmdlm_page_plan(self.prompt_pages, torch.from_numpy(self.ctx).cuda(),
                               torch.from_numpy(np.where(new > 0, -1, 0).astype(np.int32)).cuda())
             raise
-        ids = np.zeros(self.prompt_pages.max_rows, dtype=np.int32)
-        ids[:rows] = np.concatenate([np.asarray(prompts[s]) for s in sorted(prompts)])
-        tokens = torch.from_numpy(ids).cuda()
-        io = B.step_io(0, 0, flags=B.NMDLM_NO_HEAD, tokens=tokens)
-        B.nmdlm_block_step_paged(self.prompt_model, io, self.ws, n_sel=self.n_sel)
         for s in prompts:
             self.ctx[s], self.live[s] = new[s], True
 
@@ -170,11 +178,12 @@ class PagedGenerator:
         self.masked.fill_(1)
         chosen = self.chosen.view(-1)[:self.n * k_unmask].view(self.n, k_unmask)
         io = B.step_io(0, 0, tokens=self.tokens, masked=self.masked, k_unmask=k_unmask,
-                       unmasked_pos=self.chosen)
+                       unmasked_pos=self.chosen, status=self.status)
         for _ in range(steps):
             B.nmdlm_block_step_paged(self.model, io, self.ws, n_sel=self.n_sel)
             if log is not None:
                 log.append(chosen.clone())
+        self._check_status()
         self.ctx += new.astype(np.int32)
         out = self.tokens[:len(order) * self.block].view(len(order), self.block).clone()
         return {int(s): out[i] for i, s in enumerate(order)}

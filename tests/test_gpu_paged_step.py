@@ -220,3 +220,27 @@ def test_generator_stops_at_the_last_position(max_len, max_pos):
     b = g.run_block(2, 4)
     assert_same(a[0].cpu().numpy(), O.generate(m, ps[0], 1, 8, 2, 4)[0], "up to the last position")
     assert_same(torch.cat([a[1], b[1]]).cpu().numpy(), O.generate(m, ps[1], 2, 8, 2, 4)[0], "the other")
+
+
+@pytest.mark.parametrize("bad", [-1, 305, 2 ** 32 + 5])
+def test_generator_refuses_ids_outside_the_table(bad):
+    """None of the prompts is admitted, their pages go back, and the request
+    that runs beside them goes on as before."""
+    torch, B = need_gpu()
+    from paper_2607_24841_amd.generate import PagedGenerator
+
+    m = small_model()
+    g = PagedGenerator(device_model(B, m), 3, 8, max_len=192, pool=6, max_prompt_rows=200)
+    ps = prompts_of([30, 70, 40], m.V)
+    g.admit({0: ps[0]})
+    wrong = ps[1].astype(np.int64)
+    wrong[69] = bad
+    with pytest.raises(ValueError, match="ids"):
+        g.admit({1: wrong, 2: ps[2]})
+    assert g.live.tolist() == [True, False, False] and g.ctx.tolist() == [30, 0, 0]
+    assert g.pages.held.tolist() == [1, 0, 0] and g.pages.ring_state.tolist()[1] == 5
+    a = g.run_block(2, 4)
+    assert_same(a[0].cpu().numpy(), O.generate(m, ps[0], 1, 8, 2, 4)[0], "the first")
+    g.admit({1: ps[1]})
+    b = g.run_block(2, 4)
+    assert_same(b[1].cpu().numpy(), O.generate(m, ps[1], 1, 8, 2, 4)[0], "the second")
