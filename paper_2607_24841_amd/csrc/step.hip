@@ -312,7 +312,7 @@ struct StepBuffers {
   uint64_t* X1;
   uint64_t* Hs;     // [T][M][Fw]
   uint64_t* Y[2];
-  int32_t* a;       // attention output [T][M][d]
+  int32_t* a;       // attention output [T][M][d] (none over pages: spikes come at once)
   uint64_t* uA;     // partial unions of A  [M][dw]
   uint64_t* uX1;    // partial unions of X1 [M][dw] (at most one per token)
   uint64_t* uH;     // partial unions of H  [M][Fw]
@@ -340,7 +340,7 @@ static QbsmLimits step_limits(const nmdlm_model* md, int M, unsigned flags) {
 }
 
 static void carve_step(Carver& cv, const nmdlm_model* md, int M, unsigned flags, bool need_x,
-                       bool need_logits, bool need_pred, bool need_conf, StepBuffers* b) {
+                       bool need_logits, bool need_pred, bool need_conf, bool need_a, StepBuffers* b) {
   const int T = md->T, dw = md->d / 64, Fw = (md->F + 63) / 64;
   const size_t sp = (size_t)T * M * dw;
   b->X = need_x ? cv.take<uint64_t>(sp) : nullptr;
@@ -350,7 +350,7 @@ static void carve_step(Carver& cv, const nmdlm_model* md, int M, unsigned flags,
   b->Hs = cv.take<uint64_t>((size_t)T * M * Fw);
   b->Y[0] = cv.take<uint64_t>(sp);
   b->Y[1] = cv.take<uint64_t>(sp);
-  b->a = cv.take<int32_t>((size_t)T * M * md->d);
+  b->a = need_a ? cv.take<int32_t>((size_t)T * M * md->d) : nullptr;
   b->uA = cv.take<uint64_t>((size_t)M * dw);
   b->uX1 = cv.take<uint64_t>((size_t)M * dw);
   b->uH = cv.take<uint64_t>((size_t)M * Fw);
@@ -383,7 +383,7 @@ size_t block_step_paged_ws_size(const nmdlm_model* md, const nmdlm_pages& pg, un
   Carver cv{nullptr, 0, (size_t)-1, true};
   StepBuffers b;
   PagedBuffers pb;
-  carve_step(cv, md, pg.max_rows, flags, true, true, true, true, &b);
+  carve_step(cv, md, pg.max_rows, flags, true, true, true, true, false, &b);
   carve_paged(cv, md, pg, &pb);
   return align_up(cv.off, 256);
 }
@@ -391,7 +391,7 @@ size_t block_step_paged_ws_size(const nmdlm_model* md, const nmdlm_pages& pg, un
 size_t block_step_ws_size(const nmdlm_model* md, int M, unsigned flags) {
   Carver cv{nullptr, 0, (size_t)-1, true};
   StepBuffers b;
-  carve_step(cv, md, M, flags, true, true, true, true, &b);
+  carve_step(cv, md, M, flags, true, true, true, true, true, &b);
   return align_up(cv.off, 256);
 }
 
@@ -474,7 +474,7 @@ nmdlm_status block_step_impl(const nmdlm_model* md, nmdlm_step_io* io, void* ws,
   Carver cv{static_cast<char*>(ws), 0, ws_bytes, true};
   StepBuffers b;
   carve_step(cv, md, M, io->flags, io->x_in == nullptr, io->logits == nullptr,
-             io->pred == nullptr, io->conf == nullptr, &b);
+             io->pred == nullptr, io->conf == nullptr, paged == nullptr, &b);
   PagedBuffers pb{};
   if (paged) carve_paged(cv, md, *paged->pages, &pb);
   if (!cv.ok) return NMDLM_ERR_WORKSPACE;

@@ -201,3 +201,26 @@ def test_constants_match_the_header():
                  "NMDLM_MAX_POOL", "NMDLM_STATUS_PAGES_SHORT", "NMDLM_STATUS_BAD_REQUEST"):
         m = re.search(r"#define\s+%s\s+([0-9xXa-fA-F]+)" % name, text)
         assert getattr(B, name) == int(m.group(1), 0), name
+
+
+def step_sizes(rows, ctx_pages, flags, T=4, d=2048, H=16):
+    """Bytes of a step over pages without the head's outputs, and of the
+    contiguous step over as many rows."""
+    m = B.Model(2, d, H, 4 * d, 300, T, 0, 10, None, FAKE, FAKE, None, None)
+    p = pages(n_seq=2, max_rows=rows, max_pages=ctx_pages, pool=ctx_pages)
+    lib = B.load()
+    return (lib.nmdlm_block_step_paged_workspace_size(C.byref(m), C.byref(p), flags),
+            lib.nmdlm_block_step_workspace_size(C.byref(m), rows, flags))
+
+
+@pytest.mark.parametrize("rows", [32, 4096])
+def test_step_over_pages_holds_no_currents(rows):
+    """Over pages the rows' keys and values and, for 64 pages, a word and 64
+    scores a row and head come to a contiguous step's needs; the currents of
+    its attention (4 bytes a row, timestep and channel) do not."""
+    T, d, H = 4, 2048, 16
+    paged, contiguous = step_sizes(rows, 64, B.NMDLM_NO_HEAD, T, d, H)
+    more = 2 * T * rows * d // 8 + rows * H * (8 + 64 * 4)
+    more += B.load().nmdlm_bbm_attn_paged_workspace_size(C.byref(pages(n_seq=2, max_rows=rows, max_pages=64)),
+                                                         T, H, d // H)
+    assert paged <= contiguous + more - 4 * T * rows * d + 8 * 256
