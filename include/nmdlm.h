@@ -51,6 +51,9 @@ typedef enum nmdlm_status {
                                     grid and the context decide between one
                                     kernel and two.  Results do not depend on
                                     it.                                         */
+#define NMDLM_ALL_PAGES   0x8u   /* block step over pages: no selection (n_sel
+                                    below 0), whose room the workspace then
+                                    lacks                                       */
 /* bits 8..15 of the flags of nmdlm_qbsm: force the number of K splits
  * (0 = automatic).  Results do not depend on it. */
 #define NMDLM_SPLIT_SHIFT 8u
@@ -661,7 +664,9 @@ size_t nmdlm_bbm_attn_paged_workspace_size(const nmdlm_pages* pages, int T, int 
  *               v_pages; cache_cap and max_seq are not read
  *   key_counts  HOST array [n_layers] of the layers' key_counts
  *   n_sel       context pages that a row and head sees besides its own request's
- *               last ones, or below 0: all pages
+ *               last ones, or below 0: all pages.  A workspace sized with
+ *               NMDLM_ALL_PAGES in the flags serves steps without a selection
+ *               only; the flag with n_sel >= 0 is NMDLM_ERR_INVALID_ARG
  *   io          token-indexed buffers have max_rows rows (x_in, y_out
  *               [T][max_rows][d/64], tokens, masked, pred, conf [max_rows], logits
  *               [max_rows][V]), unmasked_pos [n_seq][k_unmask] holds positions

@@ -28,6 +28,7 @@ NMDLM_NO_HEAD = 0x2
 NMDLM_SPLIT_SHIFT = 8
 NMDLM_ROWTILE_SHIFT = 16
 NMDLM_ATTN_FUSED = 0x4
+NMDLM_ALL_PAGES = 0x8
 NMDLM_MAX_HEAD_M = 4096   # block tokens of a step that runs the head
 NMDLM_MAX_KEYS = 1 << 23   # attention keys C+M per sequence
 NMDLM_STATUS_TOKEN_CLAMPED = 0x1

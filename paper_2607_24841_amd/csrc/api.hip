@@ -529,6 +529,7 @@ nmdlm_status nmdlm_block_step_paged(const nmdlm_model* md, const nmdlm_pages* pa
   if ((rc = paged_call_ok(pages, md->T, md->H, md->d / md->H)) != NMDLM_OK) return rc;
   if ((rc = layers_ok(md, io->flags)) != NMDLM_OK) return rc;
   if (md->n_layers > 0 && !key_counts) return NMDLM_ERR_INVALID_ARG;
+  if (n_sel >= 0 && (io->flags & NMDLM_ALL_PAGES)) return NMDLM_ERR_INVALID_ARG;
   for (int l = 0; l < md->n_layers; ++l)
     for (const void* p : {(const void*)md->layers[l].k_cache, (const void*)md->layers[l].vt_cache,
                           (const void*)key_counts[l]})
@@ -538,7 +539,8 @@ nmdlm_status nmdlm_block_step_paged(const nmdlm_model* md, const nmdlm_pages* pa
     if (!io->tokens && !io->masked) return NMDLM_ERR_INVALID_ARG;
   }
   if ((rc = head_ok(md, io)) != NMDLM_OK) return rc;
-  if (!ws || !aligned(ws, 256) || ws_bytes < block_step_paged_ws_size(md, *pages, io->flags))
+  const unsigned ws_flags = io->flags | (n_sel < 0 ? NMDLM_ALL_PAGES : 0u);
+  if (!ws || !aligned(ws, 256) || ws_bytes < block_step_paged_ws_size(md, *pages, ws_flags))
     return NMDLM_ERR_WORKSPACE;
   if ((rc = events_ok(io, stream)) != NMDLM_OK) return rc;
   const PagedStep paged{pages, key_counts, n_sel};

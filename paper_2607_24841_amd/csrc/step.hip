@@ -370,12 +370,13 @@ struct PagedBuffers {
   uint64_t *K, *V, *sel;
   char *ws_select, *ws_attn;
 };
-static void carve_paged(Carver& cv, const nmdlm_model* md, const nmdlm_pages& pg, PagedBuffers* b) {
+static void carve_paged(Carver& cv, const nmdlm_model* md, const nmdlm_pages& pg, bool select,
+                        PagedBuffers* b) {
   const size_t sp = (size_t)md->T * pg.max_rows * (md->d / 64);
   b->K = cv.take<uint64_t>(sp);
   b->V = cv.take<uint64_t>(sp);
-  b->sel = cv.take<uint64_t>((size_t)pg.max_rows * md->H * ((pg.max_pages + 63) / 64));
-  b->ws_select = cv.take<char>(page_select_ws(pg, md->H));
+  b->sel = select ? cv.take<uint64_t>((size_t)pg.max_rows * md->H * ((pg.max_pages + 63) / 64)) : nullptr;
+  b->ws_select = select ? cv.take<char>(page_select_ws(pg, md->H)) : nullptr;
   b->ws_attn = cv.take<char>(paged_attn_ws(pg, md->T, md->H, md->d / md->H));
 }
 
@@ -384,7 +385,7 @@ size_t block_step_paged_ws_size(const nmdlm_model* md, const nmdlm_pages& pg, un
   StepBuffers b;
   PagedBuffers pb;
   carve_step(cv, md, pg.max_rows, flags, true, true, true, true, false, &b);
-  carve_paged(cv, md, pg, &pb);
+  carve_paged(cv, md, pg, !(flags & NMDLM_ALL_PAGES), &pb);
   return align_up(cv.off, 256);
 }
 
@@ -476,7 +477,7 @@ nmdlm_status block_step_impl(const nmdlm_model* md, nmdlm_step_io* io, void* ws,
   carve_step(cv, md, M, io->flags, io->x_in == nullptr, io->logits == nullptr,
              io->pred == nullptr, io->conf == nullptr, paged == nullptr, &b);
   PagedBuffers pb{};
-  if (paged) carve_paged(cv, md, *paged->pages, &pb);
+  if (paged) carve_paged(cv, md, *paged->pages, paged->n_sel >= 0, &pb);
   if (!cv.ok) return NMDLM_ERR_WORKSPACE;
 
   nmdlm_status rc = NMDLM_OK;

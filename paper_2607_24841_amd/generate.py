@@ -107,9 +107,10 @@ class PagedGenerator:
         self.prompt_pages = self.pages.view(max_prompt_rows or max_len)
         self.model = B.PagedModel(dm, self.pages)
         self.prompt_model = self.model.view(self.prompt_pages, head=False)
+        # a prompt has no context pages to choose from: its step sees all there are
         self.ws = B.workspace(max(
-            B.nmdlm_block_step_paged_workspace_size(self.model, 0),
-            B.nmdlm_block_step_paged_workspace_size(self.prompt_model, B.NMDLM_NO_HEAD)))
+            B.nmdlm_block_step_paged_workspace_size(self.model, 0 if self.n_sel >= 0 else B.NMDLM_ALL_PAGES),
+            B.nmdlm_block_step_paged_workspace_size(self.prompt_model, B.NMDLM_NO_HEAD | B.NMDLM_ALL_PAGES)))
         self.ctx = np.zeros(n_seq, dtype=np.int32)      # positions that a request holds
         self.live = np.zeros(n_seq, dtype=bool)
         rows = n_seq * block
@@ -159,7 +160,7 @@ class PagedGenerator:
             self._plan(self.prompt_pages, new)
             tokens = torch.from_numpy(ids).cuda()
             io = B.step_io(0, 0, flags=B.NMDLM_NO_HEAD, tokens=tokens, status=self.status)
-            B.nmdlm_block_step_paged(self.prompt_model, io, self.ws, n_sel=self.n_sel)
+            B.nmdlm_block_step_paged(self.prompt_model, io, self.ws)
             self._check_status()
         except (RuntimeError, ValueError):   # what they were given goes back
             B.nmdlm_page_plan(self.prompt_pages, torch.from_numpy(self.ctx).cuda(),

@@ -244,3 +244,44 @@ def test_generator_refuses_ids_outside_the_table(bad):
     g.admit({1: ps[1]})
     b = g.run_block(2, 4)
     assert_same(b[1].cpu().numpy(), O.generate(m, ps[1], 1, 8, 2, 4)[0], "the second")
+
+
+def test_workspace_of_a_step_without_a_selection():
+    """As large as such a step needs: what lies behind is left alone, and the
+    spikes are those of a step that selects every page."""
+    torch, B = need_gpu()
+    m = small_model()
+    step, y, want, (dm, pages, pre, pm, pmv, ws, xb) = run_paged(torch, B, m, [200, 64, 30, 129], 16, 100)
+    need = B.nmdlm_block_step_paged_workspace_size(pm, B.NMDLM_NO_HEAD | B.NMDLM_ALL_PAGES)
+    assert need < B.nmdlm_block_step_paged_workspace_size(pm, B.NMDLM_NO_HEAD)
+    room = torch.full((need + 4096,), 85, dtype=torch.uint8, device="cuda")
+    room[:need] = 0
+    io = B.step_io(0, 0, flags=B.NMDLM_NO_HEAD | B.NMDLM_ALL_PAGES, x_in=xb, y_out=y)
+    B.nmdlm_block_step_paged(pm, io, room[:need])
+    torch.cuda.synchronize()
+    assert (room[need:] == 85).all()
+    got = synth.unpack_bits(B.from_dev_bits(y), m.d)[:, :want.shape[1]]
+    assert_same(got, want, "spikes")
+
+
+def test_generator_with_a_selection():
+    """A context of more pages than are selected: prompts see all of theirs, a
+    block's rows choose.  Taking every page is the generator without selection."""
+    torch, B = need_gpu()
+    from paper_2607_24841_amd.generate import PagedGenerator
+
+    m = small_model()
+    ps = prompts_of([200, 70], m.V)
+    ids = {}
+    for n_sel in (None, 3, 1):
+        g = PagedGenerator(device_model(B, m), 2, 8, max_len=320, pool=9, n_sel=n_sel)
+        g.admit({0: ps[0], 1: ps[1]})
+        keys = [k.clone() for k, _, _ in g.model.pools]
+        out = g.run_block(2, 4)
+        ids[n_sel] = out[0], out[1], keys
+    assert_same(ids[None][0].cpu().numpy(), O.generate(m, ps[0], 1, 8, 2, 4)[0], "all pages")
+    assert_same(ids[None][1].cpu().numpy(), O.generate(m, ps[1], 1, 8, 2, 4)[0], "the other")
+    assert torch.equal(ids[3][0], ids[None][0]) and torch.equal(ids[3][1], ids[None][1])
+    for n_sel in (3, 1):
+        for a, b in zip(ids[n_sel][2], ids[None][2]):
+            assert torch.equal(a, b)

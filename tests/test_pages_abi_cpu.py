@@ -224,3 +224,28 @@ def test_step_over_pages_holds_no_currents(rows):
     more += B.load().nmdlm_bbm_attn_paged_workspace_size(C.byref(pages(n_seq=2, max_rows=rows, max_pages=64)),
                                                          T, H, d // H)
     assert paged <= contiguous + more - 4 * T * rows * d + 8 * 256
+
+
+def test_steps_without_a_selection_need_no_room_for_one():
+    rows, ctx_pages, H, flags = 4096, 512, 16, B.NMDLM_NO_HEAD
+    with_sel, _ = step_sizes(rows, ctx_pages, flags)
+    without, _ = step_sizes(rows, ctx_pages, flags | B.NMDLM_ALL_PAGES)
+    p = pages(n_seq=2, max_rows=rows, max_pages=ctx_pages)
+    scores = B.load().nmdlm_page_select_workspace_size(C.byref(p), 4, H, 128)
+    assert with_sel - without >= scores + rows * H * ctx_pages // 8
+
+    lib = B.load()
+    arr = (B.Layer * 1)(B.Layer(*([FAKE] * 4 + [200] * 7 + [4] + [FAKE] * 4)))
+    m = B.Model(1, 128, 2, 256, 300, 4, 0, 10, arr, FAKE, FAKE, None, None)
+    counts = (C.c_void_p * 1)(FAKE)
+    size = lambda fl: lib.nmdlm_block_step_paged_workspace_size(C.byref(m), C.byref(pages()), fl)  # noqa: E731
+
+    def call(n_sel, fl, nbytes):
+        io = B.step_io(0, 0, flags=fl, tokens=FAKE)
+        return lib.nmdlm_block_step_paged(C.byref(m), C.byref(pages()), counts, n_sel, C.byref(io), FAKE, nbytes, None)
+    less = size(flags | B.NMDLM_ALL_PAGES)
+    assert less < size(flags)
+    assert call(2, flags, less) == WORKSPACE                          # a selection needs its room
+    assert call(-1, flags, less - 1) == WORKSPACE
+    assert call(-1, flags | B.NMDLM_ALL_PAGES, less - 1) == WORKSPACE
+    assert call(2, flags | B.NMDLM_ALL_PAGES, 1 << 40) == INVALID
