@@ -622,7 +622,8 @@ nmdlm_status nmdlm_page_store(const nmdlm_pages* pages, const uint64_t* k,
  *   sel    device [max_rows][H][ceil(max_pages/64)] words: bit p%64 of word
  *          p/64 is set when logical page p is selected; rows without a page
  *          keep their words
- *   ws     workspace of nmdlm_page_select_workspace_size() bytes
+ *   ws     workspace of nmdlm_page_select_workspace_size() bytes: at most 1 GiB
+ *          (or 4 bytes a row and page, where that is more)
  * ------------------------------------------------------------------------ */
 nmdlm_status nmdlm_page_select(const nmdlm_pages* pages, const uint64_t* q, int T,
                                int H, int dh, const uint8_t* key_counts, int n_sel,

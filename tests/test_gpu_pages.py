@@ -568,3 +568,17 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for d, c in zip(ds, cs):
         check_all(d, c, 4)
+
+
+@pytest.mark.parametrize("H,heads", [(7, 4), (3, 3)])
+def test_select_by_groups_of_heads(H, heads):
+    """A plan of so many rows that the scores of its heads are held in turn (four
+    and three of them, or all three): a few of its rows are there, with a context
+    of several hundred pages."""
+    c = P.make_case(26, [64 * 300 + 5, 700], [20, 3], T=1, H=H, dh=64, spare_rows=64000, spare_pages=700)
+    d = device(c)
+    assert d.ws_sel.numel() == -(-c.max_rows * heads * -(-c.max_pages // 16) * 16 * 4 // 256) * 256
+    d.plan()
+    d.select(9)
+    sync()
+    assert_same(d.selection(), P.select(c, P.plan(c), 9), "selected pages")

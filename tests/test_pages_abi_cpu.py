@@ -249,3 +249,14 @@ def test_steps_without_a_selection_need_no_room_for_one():
     assert call(-1, flags, less - 1) == WORKSPACE
     assert call(-1, flags | B.NMDLM_ALL_PAGES, less - 1) == WORKSPACE
     assert call(2, flags | B.NMDLM_ALL_PAGES, 1 << 40) == INVALID
+
+
+def test_scores_of_a_selection_are_bounded():
+    """1 GiB, or the scores of one head where those are more."""
+    size = lambda rows, ctx_pages, H: B.load().nmdlm_page_select_workspace_size(  # noqa: E731
+        C.byref(pages(n_seq=8, max_rows=rows, max_pages=ctx_pages)), 4, H, 128)
+    assert size(32, 2047, 16) == 32 * 16 * 2048 * 4
+    assert size(8192, 2048, 16) == 1 << 30
+    for rows, ctx_pages, H in ((8193, 2048, 16), (8192, 8192, 16), (32768, 2048, 16)):
+        assert size(rows, ctx_pages, H) <= 1 << 30
+    assert size(131072, 4096, 16) == 131072 * 4096 * 4
