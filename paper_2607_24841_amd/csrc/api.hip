@@ -426,7 +426,8 @@ nmdlm_status nmdlm_page_plan(const nmdlm_pages* pg, const int32_t* ctx, const in
                              int32_t* status, void* stream) {
   const nmdlm_status rc = pages_ok(pg);
   if (rc != NMDLM_OK) return rc;
-  if (!ctx || !new_rows) return NMDLM_ERR_INVALID_ARG;
+  if (!ctx || !new_rows || !aligned(ctx, 4) || !aligned(new_rows, 4) || !aligned(status, 4))
+    return NMDLM_ERR_INVALID_ARG;
   return launch_page_plan(*pg, ctx, new_rows, status, static_cast<hipStream_t>(stream));
 }
 
@@ -451,7 +452,8 @@ nmdlm_status nmdlm_page_select(const nmdlm_pages* pg, const uint64_t* q, int T, 
                                size_t ws_bytes, void* stream) {
   const nmdlm_status rc = paged_call_ok(pg, T, H, dh);
   if (rc != NMDLM_OK) return rc;
-  if (!q || !aligned(q, 16) || !key_counts || !aligned(key_counts, 16) || !sel || n_sel < 0)
+  if (!q || !aligned(q, 16) || !key_counts || !aligned(key_counts, 16) || !sel || !aligned(sel, 8) ||
+      n_sel < 0)
     return NMDLM_ERR_INVALID_ARG;
   const size_t need = page_select_ws(*pg, H);
   if (need > 0 && (!ws || !aligned(ws, 256) || ws_bytes < need)) return NMDLM_ERR_WORKSPACE;
@@ -472,6 +474,7 @@ nmdlm_status nmdlm_bbm_attn_paged(const nmdlm_pages* pg, const uint64_t* q, int 
   for (const void* p : {(const void*)q, (const void*)k_pages, (const void*)v_pages})
     if (!p || !aligned(p, 16)) return NMDLM_ERR_INVALID_ARG;
   if (!lut_att || (!a_out && !s_out) || (s_out && theta_a <= 0)) return NMDLM_ERR_INVALID_ARG;
+  if (!aligned(sel, 8) || !aligned(a_out, 4) || !aligned(s_out, 8)) return NMDLM_ERR_INVALID_ARG;
   const size_t need = paged_attn_ws(*pg, T, H, dh);
   if (need > 0 && (!ws || !aligned(ws, 256) || ws_bytes < need)) return NMDLM_ERR_WORKSPACE;
   const PagedAttnCall c{q, k_pages, v_pages, T, H, dh, lut_att, sel, a_out, theta_a, s_out, nullptr, ws};
@@ -530,6 +533,7 @@ nmdlm_status nmdlm_block_step_paged(const nmdlm_model* md, const nmdlm_pages* pa
   if ((rc = layers_ok(md, io->flags)) != NMDLM_OK) return rc;
   if (md->n_layers > 0 && !key_counts) return NMDLM_ERR_INVALID_ARG;
   if (n_sel >= 0 && (io->flags & NMDLM_ALL_PAGES)) return NMDLM_ERR_INVALID_ARG;
+  if (!aligned(io->status, 4) || !aligned(io->unmasked_pos, 4)) return NMDLM_ERR_INVALID_ARG;
   for (int l = 0; l < md->n_layers; ++l)
     for (const void* p : {(const void*)md->layers[l].k_cache, (const void*)md->layers[l].vt_cache,
                           (const void*)key_counts[l]})

@@ -260,3 +260,20 @@ def test_scores_of_a_selection_are_bounded():
     for rows, ctx_pages, H in ((8193, 2048, 16), (8192, 8192, 16), (32768, 2048, 16)):
         assert size(rows, ctx_pages, H) <= 1 << 30
     assert size(131072, 4096, 16) == 131072 * 4096 * 4
+
+
+def test_misaligned_outputs():
+    """A status word is written by an atomic, which faults between words."""
+    run = lambda ctx, new, status: B.load().nmdlm_page_plan(C.byref(pages()), ctx, new, status, None)  # noqa: E731
+    for i in range(3):
+        for off in (1, 2):
+            assert run(*[FAKE + off * (j == i) for j in range(3)]) == INVALID, (i, off)
+    assert select(sel=FAKE + 4) == INVALID
+    for name, off in (("sel", 4), ("a_out", 2), ("s_out", 4)):
+        assert attn(**{name: FAKE + off}) == INVALID, name
+    arr = (B.Layer * 1)(B.Layer(*([FAKE] * 4 + [200] * 7 + [4] + [FAKE] * 4)))
+    m = B.Model(1, 128, 2, 256, 300, 4, 0, 10, arr, FAKE, FAKE, None, None)
+    for kw in (dict(status=FAKE + 2), dict(unmasked_pos=FAKE + 1)):
+        io = B.step_io(0, 0, flags=B.NMDLM_NO_HEAD, tokens=FAKE, **kw)
+        assert B.load().nmdlm_block_step_paged(C.byref(m), C.byref(pages()), (C.c_void_p * 1)(FAKE), 2, C.byref(io),
+                                               FAKE, 1 << 40, None) == INVALID, kw
