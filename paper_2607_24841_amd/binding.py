@@ -601,6 +601,16 @@ class PagedModel:
         self.pools = pools or [pages.pools(parent.T, parent.H, parent.d // parent.H)
                                for _ in parent.layers]
         n = len(parent.layers)
+        # the step follows the plan's page numbers into these
+        if len(self.pools) != n:
+            raise NmdlmError(NMDLM_ERR_INVALID_ARG, f"PagedModel: {len(self.pools)} pools for {n} layers")
+        size = pages.pool * parent.d * parent.T
+        for pool in self.pools:
+            for name, t, nbytes in zip(("k_pages", "v_pages", "key_counts"), pool, (8, 8, 1)):
+                pages._arg("PagedModel", name, t, size, nbytes)
+        for l in parent.layers:
+            if l.w_qkv.get_device() != pages._index:
+                raise NmdlmError(NMDLM_ERR_INVALID_ARG, f"PagedModel: the layers are not on {pages.device}")
         self._c_layers = (Layer * max(1, n))(*[l.c for l in parent.layers])
         self.key_counts = (C.c_void_p * max(1, n))()
         for i, (k, v, counts) in enumerate(self.pools):

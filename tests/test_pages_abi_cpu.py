@@ -277,3 +277,25 @@ def test_misaligned_outputs():
         io = B.step_io(0, 0, flags=B.NMDLM_NO_HEAD, tokens=FAKE, **kw)
         assert B.load().nmdlm_block_step_paged(C.byref(m), C.byref(pages()), (C.c_void_p * 1)(FAKE), 2, C.byref(io),
                                                FAKE, 1 << 40, None) == INVALID, kw
+
+
+def test_a_model_and_a_plan_that_do_not_fit():
+    """The step reads no tensor's size: pools of fewer pages than the plan's, or
+    of other types or layers, and layers elsewhere are refused beforehand."""
+    from types import SimpleNamespace as S
+
+    layer = S(w_qkv=torch.zeros(1, dtype=torch.int8), c=B.Layer())
+    parent = S(T=4, H=2, d=128, layers=[layer], c=B.Model())
+    p, wider = (B.Pages(2, 10, 3, n, device="cpu") for n in (7, 8))
+    pm = B.PagedModel(parent, p)
+    assert pm.view(p.view(20), head=False).pools is pm.pools
+    k, v, counts = pm.pools[0]
+    with pytest.raises(B.NmdlmError, match="k_pages"):
+        pm.view(wider, head=False)
+    for bad, name in (([(k.int(), v, counts)], "k_pages"), ([(k, v[:6], counts)], "v_pages"),
+                      ([(k, v, counts.transpose(1, 2))], "key_counts"), ([(k, v, counts)] * 2, "layers")):
+        with pytest.raises(B.NmdlmError, match=name):
+            B.PagedModel(parent, p, pools=bad)
+    parent.layers = [S(w_qkv=S(get_device=lambda: 1), c=B.Layer())]
+    with pytest.raises(B.NmdlmError, match="layers"):
+        B.PagedModel(parent, p)
