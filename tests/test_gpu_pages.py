@@ -582,3 +582,61 @@ def test_select_by_groups_of_heads(H, heads):
     d.select(9)
     sync()
     assert_same(d.selection(), P.select(c, P.plan(c), 9), "selected pages")
+
+
+def run_attention(c, share, seed=4):
+    d = device(c)
+    d.plan()
+    p = P.plan(c)
+    sel = None if share is None else some_selection(c, p, seed, share)
+    d.attention(sel=None if sel is None else d.put_selection(sel))
+    sync()
+    cur, spk = P.attention(c, p, sel)
+    assert_same(d.cur.cpu().numpy(), cur, "currents")
+    assert_same(d.spikes(), spk, "spikes")
+
+
+@pytest.mark.parametrize("T,dh", [(1, 64), (4, 128)])
+@pytest.mark.parametrize("share", [None, 0.3, 0.9, 0.0])
+def test_attention_rows_over_many_lists(T, dh, share):
+    """Single rows whose one workgroup lists its pages in three pieces (256, 256
+    and the rest), beside short requests."""
+    n, H = 70, 8
+    c = P.make_case(90, [64 * 531 + 5] + [20 + 3 * i for i in range(n - 1)], [1] * n, T=T, H=H, dh=dh, spare_pages=0)
+    r = P.case_route(c)
+    assert r.token and r.splits == 1 and c.max_pages > 512
+    run_attention(c, share)
+
+
+@pytest.mark.parametrize("pages", [256, 257, 512, 513])
+def test_attention_rows_at_the_list_end(pages):
+    n = 70
+    c = P.make_case(91, [64 * pages - 1] + [9] * (n - 1), [1] * n, T=2, H=8, dh=64, spare_pages=0)
+    r = P.case_route(c)
+    assert r.token and r.splits == 1 and c.max_pages == pages
+    run_attention(c, None)
+    run_attention(c, 0.5)
+
+
+@pytest.mark.parametrize("share", [None, 0.2, 0.005])
+def test_attention_wide_tiles_over_many_lists(share):
+    """Tiles of 32 rows over more pages than are listed at once."""
+    c = P.make_case(92, [64 * 300 + 30] + [0] * 7, [37] + [32] * 7, T=8, H=8, dh=64, spare_rows=0, spare_pages=0)
+    r = P.case_route(c)
+    assert r.groups == 2 and c.max_pages > 256
+    run_attention(c, share)
+
+
+@pytest.mark.parametrize("name", SHAPES)
+@pytest.mark.parametrize("share", [None, 0.3])
+def test_attention_six_timesteps(name, share):
+    run_attention(P.make_case(93, *SHAPES[name], T=6, H=2, dh=128), share)
+
+
+def test_attention_single_rows_six_timesteps():
+    """Two parts a timestep: twelve waves."""
+    c = P.make_case(94, [1000 + i for i in range(16)], [2] * 16, T=6, H=4, dh=128)
+    r = P.case_route(c)
+    assert r.token and r.parts == 2
+    run_attention(c, None)
+    run_attention(c, 0.3)
