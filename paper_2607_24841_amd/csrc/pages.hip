@@ -591,10 +591,16 @@ __device__ void pick_row_long(const int32_t* sc, int P, int nP, int n_sel, int w
   }
 }
 
-__device__ __forceinline__ void pick_any(const int32_t* sc, int P, int nP, int n_sel, int words,
+// P at most 128.
+__device__ __forceinline__ void pick_few(const int32_t* sc, int P, int nP, int n_sel, int words,
                                          uint64_t* __restrict__ out, int lane) {
   if (P <= 64) pick_row<1>(sc, P, nP, n_sel, words, out, lane);
-  else if (P <= 128) pick_row<2>(sc, P, nP, n_sel, words, out, lane);
+  else pick_row<2>(sc, P, nP, n_sel, words, out, lane);
+}
+
+__device__ __forceinline__ void pick_any(const int32_t* sc, int P, int nP, int n_sel, int words,
+                                         uint64_t* __restrict__ out, int lane) {
+  if (P <= 128) pick_few(sc, P, nP, n_sel, words, out, lane);
   else if (P <= 512) pick_row<8>(sc, P, nP, n_sel, words, out, lane);
   else if (P <= 2048) pick_row<32>(sc, P, nP, n_sel, words, out, lane);
   else pick_row_long(sc, P, nP, n_sel, words, out, lane);
@@ -615,6 +621,8 @@ static int select_ld(const nmdlm_pages& pg) { return (pg.max_pages + 15) / 16 * 
 // Scores and choice in one kernel, for a tile of 16 rows and a head: the scores
 // of at most kSelectPages pages meet in LDS; a wave per row.
 constexpr int kSelectWaves = 8;
+constexpr int kSelectPages = 128;
+static_assert(kSelectPages <= 128, "pick_few");
 template <int DHW>
 __global__ __launch_bounds__(64 * kSelectWaves) void k_page_select(SelectArgs a) {
   touch_kernargs<sizeof(SelectArgs)>();
@@ -640,15 +648,14 @@ __global__ __launch_bounds__(64 * kSelectWaves) void k_page_select(SelectArgs a)
   __syncthreads();
   for (int r = wave; r < nr; r += kSelectWaves) {
     const size_t at = (size_t)(tl.row + r) * a.H + h;
-    pick_any(sScores + r * a.ld, P, (tl.keys + 63) / 64, a.n_sel, a.words, a.sel + at * a.words, lane);
+    pick_few(sScores + r * a.ld, P, (tl.keys + 63) / 64, a.n_sel, a.words, a.sel + at * a.words, lane);
   }
 }
 
 // One kernel where the table is narrow and its workgroups, which choose after
-// they score, fill the chip: 32 requests of 16 rows, 93 context pages, 12.7 us
-// against 14.2 in two kernels; one such request 9.2 against 7.4; 187 pages, one
-// request 13.2 against 9.0, eight 13.2 against 10.1.
-constexpr int kSelectPages = 128;
+// they score, fill the chip: requests of 16 rows, 93 context pages, 16 heads, T = 4,
+// 32 of them 10.1 us against 13.6 in two kernels, 16 of them 9.2 against 8.9, one 6.8
+// in both; 256 with 125 pages 68 against 97.
 bool select_fused(const nmdlm_pages& pg, int H) {
   return pg.max_pages <= kSelectPages && std::max(pg.max_rows / 16, pg.n_seq) * H >= 256;
 }
