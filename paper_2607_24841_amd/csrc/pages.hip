@@ -388,10 +388,9 @@ struct SelectArgs {
   const uint64_t* q;
   const uint8_t* counts;
   uint64_t* sel;
-  int32_t* scores;  // [max_rows][heads][ld], where they do not stay in LDS
+  int32_t* scores;  // [head of the launch][max_rows][ld], where they do not stay in LDS
   int max_pages, pool, max_rows, words;
   int T, H, n_sel, ld;
-  int h0, heads;    // first head of the launch, and how many
 };
 
 // k-steps (of 64 channels) staged at once, and the 16-byte units between a wave's
@@ -465,7 +464,7 @@ __global__ __launch_bounds__(256) void k_page_scores(SelectArgs a) {
   extern __shared__ v4i sStage[];  // of the four waves
   __shared__ uint64_t sQ[NMDLM_MAX_T * 32 * DHW];
   const PageTile tl = a.tiles[blockIdx.x];
-  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, h = a.h0 + (int)blockIdx.y;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, h = blockIdx.y;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int nr = tl.n_full & 63, P = tl.n_full >> 6;
   if (nr == 0 || (int)blockIdx.z * 64 >= P) return;  // uniform
@@ -481,7 +480,7 @@ __global__ __launch_bounds__(256) void k_page_scores(SelectArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int r = 16 * u + 4 * g + e;
-      if (r < nr) a.scores[((size_t)(tl.row + r) * a.heads + blockIdx.y) * a.ld + p0 + c] = s[u][e];
+      if (r < nr) a.scores[((size_t)h * a.max_rows + tl.row + r) * a.ld + p0 + c] = s[u][e];
     }
 }
 
@@ -611,9 +610,9 @@ __global__ __launch_bounds__(256) void k_page_pick(SelectArgs a) {
   const PageTile tl = a.tiles[blockIdx.x];
   const int r = __builtin_amdgcn_readfirstlane((int)blockIdx.z * 4 + ((int)threadIdx.x >> 6));
   if (r >= (tl.n_full & 63)) return;  // wave-uniform
-  const size_t at = (size_t)(tl.row + r) * a.H + a.h0 + blockIdx.y;
-  pick_any(a.scores + ((size_t)(tl.row + r) * a.heads + blockIdx.y) * a.ld, tl.n_full >> 6, (tl.keys + 63) / 64, a.n_sel, a.words, a.sel + at * a.words,
-           threadIdx.x & 63);
+  const int row = tl.row + r;
+  pick_any(a.scores + ((size_t)blockIdx.y * a.max_rows + row) * a.ld, tl.n_full >> 6, (tl.keys + 63) / 64,
+           a.n_sel, a.words, a.sel + ((size_t)row * a.H + blockIdx.y) * a.words, threadIdx.x & 63);
 }
 
 static int select_ld(const nmdlm_pages& pg) { return (pg.max_pages + 15) / 16 * 16; }
@@ -662,8 +661,8 @@ bool select_fused(const nmdlm_pages& pg, int H) {
 
 // Heads that are scored before their pages are chosen: all, or an even share of
 // them whose scores take at most this many bytes (one head's take what they need).
-// 8192 rows, 16 heads, 2046 pages, T = 4, 1 GiB of scores: 1156 us at once, 1180 in
-// four shares; 4096 rows 586 at once, 618 in two.
+// 8192 rows, 16 heads, 2046 pages, T = 4, 1 GiB of scores: 1108 us at once, 1128 in
+// four shares; 4096 rows 560 at once, 567 in two.
 constexpr size_t kScoreBytes = (size_t)1 << 30;
 static int select_heads(const nmdlm_pages& pg, int H) {
   const size_t head = (size_t)pg.max_rows * select_ld(pg) * sizeof(int32_t);
@@ -686,7 +685,7 @@ static nmdlm_status launch_select(const nmdlm_pages& pg, const uint64_t* q, int 
   PageIndex ix;
   page_index_layout(pg.n_seq, pg.max_rows, pg.index, &ix);
   SelectArgs a{ix.t16, pg.table, q, counts, sel, static_cast<int32_t*>(ws), pg.max_pages, pg.pool,
-               pg.max_rows, (pg.max_pages + 63) / 64, T, H, n_sel, select_ld(pg), 0, H};
+               pg.max_rows, (pg.max_pages + 63) / 64, T, H, n_sel, select_ld(pg)};
   const size_t stage = 16 * score_ld(T * DHW) * sizeof(v4i);  // of a wave
   if (select_fused(pg, H)) {
     a.ld += 1;  // a row's bank past the row before's
@@ -700,13 +699,16 @@ static nmdlm_status launch_select(const nmdlm_pages& pg, const uint64_t* q, int 
   }
   a.tiles = ix.t32;
   const int heads = select_heads(pg, H);
-  for (; a.h0 < H; a.h0 += heads) {
-    a.heads = std::min(heads, H - a.h0);
-    hipLaunchKernelGGL(k_page_scores<DHW>, dim3(ix.n32, a.heads, (pg.max_pages + 63) / 64), dim3(256), 4 * stage,
-                       st, a);
+  for (int h0 = 0; h0 < H; h0 += heads) {
+    const int n = std::min(heads, H - h0);
+    // the kernels count heads from the launch's first
+    a.q = q + (size_t)h0 * DHW;
+    a.counts = counts + (size_t)h0 * T * 64 * DHW;
+    a.sel = sel + (size_t)h0 * a.words;
+    hipLaunchKernelGGL(k_page_scores<DHW>, dim3(ix.n32, n, (pg.max_pages + 63) / 64), dim3(256), 4 * stage, st, a);
     nmdlm_status rc = hip_status();
     if (rc != NMDLM_OK) return rc;
-    hipLaunchKernelGGL(k_page_pick, dim3(ix.n32, a.heads, 8), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_page_pick, dim3(ix.n32, n, 8), dim3(256), 0, st, a);
     if ((rc = hip_status()) != NMDLM_OK) return rc;
   }
   return NMDLM_OK;
