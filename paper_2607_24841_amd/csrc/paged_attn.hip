@@ -448,7 +448,11 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T * DHW) void k_paged_join(PagedArgs
 // About 100 vector instructions a page of 128 channels, no exchange between
 // lanes, and few registers: the loads of kTokenAhead pages are in flight in each
 // of many waves.  Bound by HBM: T = 4, 16 heads of 128, 64 requests x 2048 keys, 268 MB,
-// 46 us or 5.9 TB/s (64 in tiles).
+// 45 us or 6.0 TB/s (64 us in tiles; a plain read reaches 6.3); with a selection of 8
+// of the 31 pages, 75 MB 20 us, of 16 of 255 pages, 143 MB 30 us, the list and the table
+// read one after the other before the pages.  A request has one workgroup a head where
+// the plan has rows enough: 64 requests x 1 to 4000 keys, 271 MB, 52 us, the longest
+// last; one of 100 thousand keys among 63 of a thousand 410 us.
 // ---------------------------------------------------------------------------
 // Two pages in flight in each of up to twelve waves a workgroup, at most four a
 // timestep, against four in each of eight: 64 requests x 1 to 4000 keys 60.9 us
@@ -588,7 +592,9 @@ __global__ __launch_bounds__(64 * kTokenWaves) void k_paged_token(PagedArgs a) {
 //  * The token kernel up to 2 rows a request (and 8 rows more, a plan's spare
 //    ones): 64 requests x 1 row x 4001 keys 100 us against 133 in tiles, x 501 keys 20
 //    against 30; 2 rows 136 against 132 and 30 against 31; 3 rows 181 against 133.  One
-//    request of 8 rows x 508 keys 6.9 against 10.7, x 4008 keys 18.0 against 15.1.
+//    request of 8 rows x 508 keys 6.2 against 9.8, x 4008 keys 18.1 against 12.6, x 64008
+//    keys 104 against 36; of 4 rows 6.3 against 9.9, 12.1 against 12.4 and 79 against 35:
+//    the spare rows pay for short contexts only.
 //  * 32 rows a wave (QG = 2) where the tiles give 1024 such waves: 4 x 200 rows x
 //    500 keys 24 us against 29 with 16, 1 x 2048 x 2348 109 against 135, T = 1, 16 x
 //    100 x 400 17.0 against 18.5; below, T = 4, 1 x 300 x 600 19.5 against 17.6, T = 1,
@@ -600,7 +606,8 @@ __global__ __launch_bounds__(64 * kTokenWaves) void k_paged_token(PagedArgs a) {
 //    64016 keys 391 us whole, 109 in 4, 42 in 16, 43 in 32; 4 x 16 x 16016 105 whole, 42 in
 //    4 (one a CU), 47 in 6 (some CUs two), 42 in 8; 64 selected of 2047 pages, 32
 //    rows, 70 whole, 25 in 8 (one a CU), 31 in 10 or 16.  16 x 16 x 2016 keys, a
-//    workgroup a CU without: 23 whole, 40 in 2.
+//    workgroup a CU without: 23 whole, 40 in 2.  Idle slots count as if they had
+//    rows: the 1 x 16 rows x 64016 keys in a plan of 64 blocks of 16 355 us, 36 in its own.
 // ---------------------------------------------------------------------------
 PagedRoute paged_route(const nmdlm_pages& pg, int T, int H) {
   PagedRoute r{pg.max_rows <= 2LL * pg.n_seq + 8, 1, T <= 2 ? 4 : (T <= 4 ? 2 : 1), 1};
