@@ -99,7 +99,7 @@ class PagedGenerator:
         if not 1 <= block <= B.NMDLM_MAX_HEAD_M:
             raise ValueError(f"a block of {block} rows: 1 to {B.NMDLM_MAX_HEAD_M}")
         self.block, self.n, self.n_sel = block, n_seq, -1 if n_sel is None else int(n_sel)
-        self.limit = min(max_len, dm.max_pos)           # positions of a request
+        self.limit = min(max_len, dm.c.max_pos)         # positions of a request
         max_pages = -(-max_len // B.NMDLM_PAGE)
         # prompts go through a plan of their own over the same tables: a step's
         # rows are as many as its plan has room for

@@ -285,3 +285,17 @@ def test_generator_with_a_selection():
     for n_sel in (3, 1):
         for a, b in zip(ids[n_sel][2], ids[None][2]):
             assert torch.equal(a, b)
+
+
+def test_generator_over_a_view_of_a_model():
+    """Some of a model's layers, with its tables and head."""
+    torch, B = need_gpu()
+    from paper_2607_24841_amd.generate import PagedGenerator
+
+    m = small_model(n_layers=3)
+    dm = device_model(B, m)
+    ps = prompts_of([70], m.V)
+    g = PagedGenerator(dm.view(0, 2, head=True), 1, 8, max_len=128, pool=2)
+    g.admit({0: ps[0]})
+    m.layers = m.layers[:2]
+    assert_same(g.run_block(2, 4)[0].cpu().numpy(), O.generate(m, ps[0], 1, 8, 2, 4)[0], "ids")
