@@ -155,8 +155,7 @@ class PagedGenerator:
         self._check_lengths(new)
         ids = np.zeros(self.prompt_pages.max_rows, dtype=np.int32)
         # ids beyond 32 bits stay outside the table
-        wide = np.concatenate([np.asarray(prompts[s]).astype(np.int64) for s in sorted(prompts)])
-        ids[:rows] = np.clip(wide, -1, 2**31 - 1)
+        ids[:rows] = np.clip(np.concatenate([np.asarray(prompts[s]) for s in sorted(prompts)]), -1, 2**31 - 1)
         try:
             self._plan(self.prompt_pages, new)
             tokens = torch.from_numpy(ids).cuda()

@@ -39,16 +39,3 @@ def test_requests_past_their_last_position():
 def test_blocks_that_a_step_cannot_unmask(block):
     with pytest.raises(ValueError, match="block"):
         G.PagedGenerator(SimpleNamespace(max_pos=1 << 20), 1, block, max_len=1 << 14, pool=256)
-
-
-@pytest.mark.parametrize("dtype", [np.uint8, np.int16, np.uint16, np.uint32, np.int64, np.uint64])
-def test_prompts_of_other_integer_types(dtype):
-    """They get as far as the plan, also beside one of another type."""
-    with pytest.raises(AssertionError, match="planned"):
-        bare().admit({0: np.arange(5, dtype=dtype), 1: [3, 4], 2: np.arange(4, dtype=np.int32)})
-
-
-@pytest.mark.parametrize("dtype", [np.uint8, np.int16, np.uint16, np.uint32, np.uint64])
-def test_prompts_that_are_all_of_another_type(dtype):
-    with pytest.raises(AssertionError, match="planned"):
-        bare().admit({0: np.arange(5, dtype=dtype)})
