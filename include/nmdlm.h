@@ -686,6 +686,124 @@ nmdlm_status nmdlm_block_step_paged(const nmdlm_model* model, const nmdlm_pages*
 size_t nmdlm_block_step_paged_workspace_size(const nmdlm_model* model,
                                              const nmdlm_pages* pages, unsigned flags);
 
+/* ------------------------------------------------------------------------
+ * Drafted decoding.  A block drafted by a cheaper model is checked in one pass
+ * of the target: the drafted tokens and, for every position after them, a
+ * masked row that sees the tokens before its position.  The target's logits at
+ * the masked rows then say which drafts stand.  The pass needs rows that see
+ * different keys (nmdlm_bbm_attn_masked, nmdlm_block_step_masked), the choice
+ * draws from distributions (nmdlm_token_sample, nmdlm_draft_verify).
+ *
+ * nmdlm_mask — which cache rows a row sees, and the positions that a bias goes
+ * by:
+ *   ranges    device int32 [M][4], 16-byte aligned: row m sees the cache rows j
+ *             with r0 <= j < r1 or r2 <= j < r3 (ends outside the keys count as
+ *             the nearest end; a range with r1 <= r0 is empty).  Documents,
+ *             prefixes, blocks, windows and drafted rows are such pairs
+ *   q_pos     device int32 [M]: positions of the rows, or NULL
+ *   k_pos     device int32 [n_keys]: positions of the cache rows, or NULL
+ *   max_dist  0 .. NMDLM_MAX_DIST: distances beyond count as this
+ * ------------------------------------------------------------------------ */
+#define NMDLM_MAX_DIST 1024
+typedef struct nmdlm_mask {
+  const int32_t* ranges;
+  const int32_t* q_pos;
+  const int32_t* k_pos;
+  int max_dist;
+} nmdlm_mask;
+
+/* ------------------------------------------------------------------------
+ * nmdlm_bbm_attn_masked — nmdlm_bbm_attn (its sums, weights and neuron) of rows
+ * that see the keys of their ranges, with a bias of the scores by distance:
+ *     s = popcount(Q[t,i,head h] AND K[t,j,head h])
+ *     x = s + bias[h][clamp(q_pos[i] - k_pos[j], -max_dist, max_dist) + max_dist]
+ *     p = lut_att[clamp(x, 0, 255)] for the keys that row i sees
+ *     a[t,i,c] = floor(256 * sum_j p * V[t,j,c] / sum_j p)   (0 if sum_j p = 0)
+ * A cap of the scores is a matter of the table.  A row that sees nothing gets
+ * a = 0.  The integers are exact and do not depend on how the work is split.
+ *
+ *   q, k_cache, vt_cache, cache_cap, T, M, H, dh, lut_att, a_out, theta_a, s_out
+ *           as nmdlm_bbm_attn
+ *   n_keys  cache rows that can be seen: 1 .. NMDLM_MAX_KEYS, at most cache_cap
+ *   mask    HOST struct of device pointers
+ *   bias    device int8 [H][2*max_dist + 1] or NULL (no bias; positions and
+ *           max_dist are not read)
+ *   ws      workspace of nmdlm_bbm_attn_masked_workspace_size() bytes
+ * Errors: NMDLM_ERR_INVALID_ARG for a missing or misaligned pointer (positions
+ * with a bias among them), a size below 1, max_dist outside its bounds, n_keys
+ * past the cache; NMDLM_ERR_UNSUPPORTED as for nmdlm_bbm_attn.
+ * ------------------------------------------------------------------------ */
+nmdlm_status nmdlm_bbm_attn_masked(const uint64_t* q, const uint64_t* k_cache,
+                                   const uint64_t* vt_cache, int64_t cache_cap, int T,
+                                   int M, int n_keys, int H, int dh, const uint8_t* lut_att,
+                                   const nmdlm_mask* mask, const int8_t* bias,
+                                   int32_t* a_out, int32_t theta_a, uint64_t* s_out,
+                                   void* ws, size_t ws_bytes, void* stream);
+size_t nmdlm_bbm_attn_masked_workspace_size(int T, int M, int n_keys, int H, int dh);
+
+/* ------------------------------------------------------------------------
+ * nmdlm_token_sample — a token of each row of logits.  With the row's largest
+ * logit l_max, temperature tau and w_v = exp((l_v - l_max) / tau) (float64; 0 for
+ * exponents below -700 and for NaN, 1 where l_v = l_max), the token is the first
+ * v with
+ *     w_0 + ... + w_v > u * sum_j w_j
+ * (the last of positive weight when none is); at tau = 0 the first of the
+ * largest logits.  conf is w_token / sum_j w_j, at tau = 0 with tau = 1 in the
+ * weights, as the block step has it.  A row of -inf and NaN alone: token -1,
+ * conf 0.
+ *
+ *   logits  device float [M][V], 1 <= V <= NMDLM_MAX_SAMPLE_V
+ *   u       device float [M] in [0, 1) (not read at tau = 0; may then be NULL)
+ *   tokens  device int32 [M]
+ *   conf    device double [M] or NULL
+ * Errors: NMDLM_ERR_INVALID_ARG for a missing or misaligned pointer, a size below
+ * 1, a temperature that is negative, infinite or NaN.
+ * ------------------------------------------------------------------------ */
+#define NMDLM_MAX_SAMPLE_V 16777216
+nmdlm_status nmdlm_token_sample(const float* logits, int M, int V, double temperature,
+                                const float* u, int32_t* tokens, double* conf, void* stream);
+
+/* ------------------------------------------------------------------------
+ * nmdlm_draft_verify — which drafted tokens stand, and what replaces the first
+ * that does not.  Row m has a draft x = draft[m] drawn from q (the
+ * draft's distribution), and the target's distribution p, both as in
+ * nmdlm_token_sample (at temperature 0: all on the first of the largest).  The
+ * draft is taken when
+ *     u[m][0] * q(x) < p(x);
+ * else the token is drawn by u[m][1], as in nmdlm_token_sample, with the
+ * weights max(p_v - q_v, 0) (p where these sum to 0).  Tokens that come out so
+ * are distributed as p.  A row without a draft (an id outside [0, V)) is drawn
+ * from p.
+ *
+ * Rows [cu_rows[s], cu_rows[s+1]) are request s's, in order: the rows up to its
+ * first that takes no draft count, that one included (a row without a draft
+ * behind the drafts gives the token that follows them all).  The rows after it
+ * get token -1, accepted 0 and conf 0.  With NMDLM_VERIFY_EACH every row counts
+ * (positions that were drafted independently).  Rows outside [cu_rows[0],
+ * cu_rows[n_seq]) are left as they were.
+ *
+ *   logits        device float [M][V], the target's
+ *   draft_logits  device float [M][V], the draft's, or NULL: drafts were certain
+ *                 (q is 1 at the draft).  Not read in rows without a draft
+ *   draft         device int32 [M]
+ *   u             device float [M][2] in [0, 1)
+ *   cu_rows       device int32 [n_seq + 1], not decreasing, within [0, M], or NULL:
+ *                 one request of all M rows (n_seq = 1)
+ *   tokens        device int32 [M];  accepted  device uint8 [M]
+ *   n_accepted    device int32 [n_seq] or NULL: drafts taken that count
+ *   conf          device double [M] or NULL: the target's probability of the
+ *                 token, as in nmdlm_token_sample
+ *   flags         0 or NMDLM_VERIFY_EACH
+ * Errors: as nmdlm_token_sample; NMDLM_ERR_INVALID_ARG for other flags and for
+ * n_seq other than 1 without cu_rows.
+ * ------------------------------------------------------------------------ */
+#define NMDLM_VERIFY_EACH 0x1u
+nmdlm_status nmdlm_draft_verify(const float* logits, const float* draft_logits, int M, int V,
+                                const int32_t* draft, const float* u, double temperature,
+                                double draft_temperature, const int32_t* cu_rows, int n_seq,
+                                unsigned flags, int32_t* tokens, uint8_t* accepted,
+                                int32_t* n_accepted, double* conf, void* stream);
+
 /* Clears a workspace region with a fill kernel on the stream (use once on a
  * new workspace). */
 nmdlm_status nmdlm_workspace_clear(void* ws, size_t ws_bytes, void* stream);

@@ -665,3 +665,117 @@ def paged_attention(Q, K, V, lut, see) -> np.ndarray:
             live = den > 0
             a[t, live, h] = 256 * num[live] // den[live, None]
     return a.reshape(T, M, H * dh)
+
+
+# ----------------------------------------------------------------------------
+# drafted decoding: attention of rows that see different keys, tokens drawn from
+# logits, verification of drafts
+# ----------------------------------------------------------------------------
+def seen_keys(ranges, n_keys: int) -> np.ndarray:
+    """0/1 [M][n_keys]: key j is seen when r0 <= j < r1 or r2 <= j < r3."""
+    r = np.asarray(ranges, dtype=np.int64)[:, :, None]
+    j = np.arange(n_keys)
+    return (((j >= r[:, 0]) & (j < r[:, 1])) | ((j >= r[:, 2]) & (j < r[:, 3]))).astype(np.uint8)
+
+
+def masked_attention(Q, K, V, H: int, lut, ranges, bias=None, q_pos=None, k_pos=None,
+                     max_dist: int = 0) -> np.ndarray:
+    """Currents: Q 0/1 [T][M][d]; K, V 0/1 [T][J][d]; the formulas of
+    bbm_attention over the keys of a row's ranges, the score plus
+    bias[h][clamp(q_pos - k_pos, -max_dist, max_dist) + max_dist], clamped to
+    [0, 255], in the table.  int64 [T][M][d]."""
+    T, M, d = Q.shape
+    J, dh = K.shape[1], d // H
+    lut = np.asarray(lut, dtype=np.int64)
+    see = seen_keys(ranges, J).astype(np.int64)
+    a = np.zeros((T, M, d), dtype=np.int64)
+    for h in range(H):
+        c = slice(h * dh, (h + 1) * dh)
+        add = 0
+        if bias is not None:
+            off = np.asarray(q_pos, dtype=np.int64)[:, None] - np.asarray(k_pos, dtype=np.int64)[None, :J]
+            add = np.asarray(bias, dtype=np.int64)[h][np.clip(off, -max_dist, max_dist) + max_dist]
+        for t in range(T):
+            s = np.clip(_exact_matmul(Q[t, :, c], K[t, :, c].T) + add, 0, 255)
+            p = lut[s] * see
+            num, den = _exact_matmul(p, V[t, :, c]), p.sum(1)
+            live = den > 0
+            a[t, live, c] = 256 * num[live] // den[live, None]
+    return a
+
+
+def token_weights(l, tau: float):
+    """Weights of a row of logits at a temperature (float64), those of the draw and
+    those of the confidence: exp((l - max) / tau), 0 for exponents below -700 and
+    for NaN; at temperature 0 the draw has all on the first of the largest, the
+    confidence temperature 1.  Zeros for a row of -inf and NaN."""
+    l = np.where(np.isnan(l), -np.inf, np.asarray(l, dtype=np.float64))
+    top = l.max()
+    if top == -np.inf:
+        return np.zeros(len(l)), np.zeros(len(l))
+    with np.errstate(invalid="ignore", over="ignore"):
+        e = np.where(l == top, 0.0, (l - top) / (tau if tau > 0 else 1.0))
+    w = np.where(e >= -700.0, np.exp(e), 0.0)
+    if tau > 0:
+        return w, w
+    one = np.zeros(len(l))
+    one[np.argmax(l == top)] = 1.0
+    return one, w
+
+
+def draw_token(w, u: float) -> int:
+    """First id whose running sum exceeds u times the sum (the last of positive
+    weight when none does); -1 when all are 0."""
+    cs = np.cumsum(w)
+    if not cs[-1] > 0:
+        return -1
+    over = np.flatnonzero(cs > u * cs[-1])
+    last = int(np.flatnonzero(w > 0)[-1])
+    return min(int(over[0]), last) if len(over) else last
+
+
+def token_sample(logits, tau: float, u):
+    """Tokens and confidences of rows of logits."""
+    tok, conf = np.full(len(logits), -1, dtype=np.int32), np.zeros(len(logits))
+    for m, l in enumerate(logits):
+        w, w1 = token_weights(l, tau)
+        tok[m] = draw_token(w, float(u[m]) if u is not None else 0.0)
+        if tok[m] >= 0:
+            conf[m] = w1[tok[m]] / w1.sum()
+    return tok, conf
+
+
+def draft_verify(logits, draft_logits, draft, u, tau: float, draft_tau: float, cu, chain: bool = True):
+    """tokens, accepted, conf of the rows [cu[0], cu[-1]) (-9, 9, -9.0 elsewhere) and
+    n_accepted of the requests: the draft x is taken when u0 q(x) < p(x), else the
+    token is drawn by u1 from max(p - q, 0), or from p where that is 0."""
+    M, V = logits.shape
+    tok, acc = np.full(M, -9, dtype=np.int32), np.full(M, 9, dtype=np.uint8)
+    conf, n_acc = np.full(M, -9.0), np.zeros(len(cu) - 1, dtype=np.int32)
+    for s in range(len(cu) - 1):
+        ended = False
+        for m in range(cu[s], cu[s + 1]):
+            tok[m], acc[m], conf[m] = -1, 0, 0.0
+            if ended:
+                continue
+            w, w1 = token_weights(logits[m], tau)
+            p = w / w.sum() if w.any() else w
+            x, left = int(draft[m]), p
+            if 0 <= x < V:
+                q = np.zeros(V)
+                if draft_logits is None:
+                    q[x] = 1.0
+                else:
+                    wq = token_weights(draft_logits[m], draft_tau)[0]
+                    q = wq / wq.sum() if wq.any() else wq
+                if float(u[m][0]) * q[x] < p[x]:
+                    tok[m], acc[m] = x, 1
+                    n_acc[s] += 1
+                left = np.maximum(p - q, 0.0)
+                left = left if left.any() else p
+            if not acc[m]:
+                tok[m] = draw_token(left, float(u[m][1]))
+                ended = chain
+            if tok[m] >= 0:
+                conf[m] = w1[tok[m]] / w1.sum()
+    return tok, acc, conf, n_acc

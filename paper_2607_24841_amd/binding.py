@@ -39,6 +39,9 @@ NMDLM_MAX_REQUESTS = 16384
 NMDLM_MAX_PLAN_ROWS = 1 << 19
 NMDLM_MAX_PAGES = 1 << 17   # pages of a request
 NMDLM_MAX_POOL = 1 << 25
+NMDLM_MAX_DIST = 1024     # distance of positions that a bias tells apart
+NMDLM_MAX_SAMPLE_V = 1 << 24
+NMDLM_VERIFY_EACH = 0x1
 NMDLM_NOALLOC_SCRATCH_BYTES = 16 << 20   # static scratch of nmdlm_qbsm_noalloc per GPU
 NMDLM_MAX_THR_DEN = 1 << 24
 NMDLM_PATH_SHIFT = 20
@@ -62,7 +65,8 @@ EXPORTS = (
     "nmdlm_page_index_bytes", "nmdlm_page_plan", "nmdlm_page_store", "nmdlm_page_select",
     "nmdlm_page_select_workspace_size", "nmdlm_bbm_attn_paged",
     "nmdlm_bbm_attn_paged_workspace_size", "nmdlm_block_step_paged",
-    "nmdlm_block_step_paged_workspace_size",
+    "nmdlm_block_step_paged_workspace_size", "nmdlm_bbm_attn_masked",
+    "nmdlm_bbm_attn_masked_workspace_size", "nmdlm_token_sample", "nmdlm_draft_verify",
 )
 
 
@@ -118,6 +122,11 @@ class PagesC(C.Structure):
         ("ring_state", C.c_void_p), ("cu_rows", C.c_void_p), ("slot", C.c_void_p),
         ("pos", C.c_void_p), ("index", C.c_void_p), ("index_bytes", C.c_size_t),
     ]
+
+
+class MaskC(C.Structure):
+    _fields_ = [("ranges", C.c_void_p), ("q_pos", C.c_void_p), ("k_pos", C.c_void_p),
+                ("max_dist", C.c_int)]
 
 
 _lib = None
@@ -185,6 +194,13 @@ def load(path: str = LIB_PATH):
                                            C.POINTER(StepIO), vp, sz, vp]
     lib.nmdlm_block_step_paged_workspace_size.argtypes = [C.POINTER(Model), pg, u]
     lib.nmdlm_block_step_paged_workspace_size.restype = sz
+    lib.nmdlm_bbm_attn_masked.argtypes = [vp, vp, vp, i64, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int,
+                                          vp, C.POINTER(MaskC), vp, vp, i32, vp, vp, sz, vp]
+    lib.nmdlm_bbm_attn_masked_workspace_size.argtypes = [C.c_int] * 5
+    lib.nmdlm_bbm_attn_masked_workspace_size.restype = sz
+    lib.nmdlm_token_sample.argtypes = [vp, C.c_int, C.c_int, C.c_double, vp, vp, vp, vp]
+    lib.nmdlm_draft_verify.argtypes = [vp, vp, C.c_int, C.c_int, vp, vp, C.c_double, C.c_double, vp,
+                                       C.c_int, u, vp, vp, vp, vp, vp]
     lib.nmdlm_workspace_clear.argtypes = [vp, sz, vp]
     lib.nmdlm_status_string.argtypes = [C.c_int]
     lib.nmdlm_status_string.restype = C.c_char_p
@@ -476,6 +492,115 @@ def nmdlm_bbm_attn_paged(pages: Pages, q, T, H, dh, k_pages, v_pages, lut_att, a
 
 def nmdlm_bbm_attn_paged_workspace_size(pages: Pages, T, H, dh) -> int:
     return load().nmdlm_bbm_attn_paged_workspace_size(C.byref(pages.c), T, H, dh)
+
+
+# ----------------------------------------------------------------------------
+# drafted decoding
+# ----------------------------------------------------------------------------
+def _arg(what: str, name: str, t, n: int, size: int, index: int) -> int | None:
+    """The address of a tensor (None for None) that has to lie on GPU `index`,
+    contiguous, with n or more elements of `size` bytes."""
+    if t is None:
+        return None
+    if t.numel() < n or t.element_size() != size or t.get_device() != index or not t.is_contiguous():
+        raise NmdlmError(NMDLM_ERR_INVALID_ARG,
+                         f"{what}: {name} needs {n} contiguous elements of {size} bytes on GPU {index}")
+    return t.data_ptr()
+
+
+def _on(index: int, what: str, call, stream) -> None:
+    """call(stream handle) on GPU `index` and, by default, its current stream."""
+    if index < 0:
+        raise NmdlmError(NMDLM_ERR_INVALID_ARG, f"{what}: the tensors are not on a GPU")
+    handle = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if torch.cuda.current_device() == index:
+        st = call(handle)
+    else:
+        with torch.cuda.device(index):
+            st = call(handle)
+    if st != NMDLM_OK:
+        check(st, what)
+
+
+class Mask:
+    """Which cache rows a row sees (nmdlm_mask): int32 tensors ranges [M][4], a row
+    seeing the rows [r0, r1) and [r2, r3), and for a bias the positions q_pos [M]
+    of the rows and k_pos [n_keys] of the cache rows, distances beyond max_dist
+    counting as max_dist.  The tensors are kept and read at each call."""
+
+    def __init__(self, ranges, q_pos=None, k_pos=None, max_dist: int = 0):
+        self._index = ranges.get_device()
+        self.rows = ranges.numel() // 4
+        self.keys = 0 if k_pos is None else k_pos.numel()
+        self.ranges, self.q_pos, self.k_pos, self.max_dist = ranges, q_pos, k_pos, int(max_dist)
+        arg = lambda name, t, n: _arg("Mask", name, t, n, 4, self._index)  # noqa: E731
+        for t in (ranges, q_pos, k_pos):
+            if t is not None and t.dtype != torch.int32:
+                raise NmdlmError(NMDLM_ERR_INVALID_ARG, "Mask: ranges and positions are int32")
+        if ranges.dim() != 2 or ranges.shape[1] != 4:
+            raise NmdlmError(NMDLM_ERR_INVALID_ARG, "Mask: ranges are [rows][4]")
+        self.c = MaskC(arg("ranges", ranges, 4), arg("q_pos", q_pos, self.rows), arg("k_pos", k_pos, 1),
+                       self.max_dist)
+        self._ref = C.byref(self.c)
+
+    def check(self, what: str, M: int, n_keys: int, biased: bool) -> None:
+        """The mask has M rows and, for a bias, positions of n_keys cache rows."""
+        if self.rows < M or (biased and (self.q_pos is None or self.keys < n_keys)):
+            raise NmdlmError(NMDLM_ERR_INVALID_ARG, f"{what}: the mask is for fewer rows or keys")
+
+
+def nmdlm_bbm_attn_masked(q, k_cache, vt_cache, cache_cap, T, M, n_keys, H, dh, lut_att, mask: Mask,
+                          bias=None, a_out=None, theta_a=0, s_out=None, ws=None, stream=None) -> None:
+    what, ix = "nmdlm_bbm_attn_masked", q.get_device()
+    mask.check(what, M, n_keys, bias is not None)
+    if mask._index != ix:
+        raise NmdlmError(NMDLM_ERR_INVALID_ARG, f"{what}: the mask is on another device")
+    rows, cache = T * M * (H * dh // 64), T * cache_cap * (H * dh // 64)
+    args = (_arg(what, "q", q, rows, 8, ix), _arg(what, "k_cache", k_cache, cache, 8, ix),
+            _arg(what, "vt_cache", vt_cache, cache, 8, ix), cache_cap, T, M, n_keys, H, dh,
+            _arg(what, "lut_att", lut_att, 256, 1, ix), mask._ref,
+            _arg(what, "bias", bias, H * (2 * mask.max_dist + 1), 1, ix),
+            _arg(what, "a_out", a_out, rows * 64, 4, ix), theta_a, _arg(what, "s_out", s_out, rows, 8, ix),
+            _arg(what, "ws", ws, 1, 1, ix), 0 if ws is None else ws.numel())
+    fn = load().nmdlm_bbm_attn_masked
+    _on(ix, what, lambda st: fn(*args, st), stream)
+
+
+def nmdlm_bbm_attn_masked_workspace_size(T, M, n_keys, H, dh) -> int:
+    return load().nmdlm_bbm_attn_masked_workspace_size(T, M, n_keys, H, dh)
+
+
+def _floats(what: str, *named) -> None:
+    for name, t, dtype in named:
+        if t is not None and t.dtype != dtype:
+            raise NmdlmError(NMDLM_ERR_INVALID_ARG, f"{what}: {name} is {t.dtype}, not {dtype}")
+
+
+def nmdlm_token_sample(logits, M, V, temperature, u, tokens, conf=None, stream=None) -> None:
+    what, ix = "nmdlm_token_sample", logits.get_device()
+    _floats(what, ("logits", logits, torch.float32), ("u", u, torch.float32), ("conf", conf, torch.float64))
+    args = (_arg(what, "logits", logits, M * V, 4, ix), M, V, float(temperature),
+            _arg(what, "u", u, M, 4, ix), _arg(what, "tokens", tokens, M, 4, ix),
+            _arg(what, "conf", conf, M, 8, ix))
+    fn = load().nmdlm_token_sample
+    _on(ix, what, lambda st: fn(*args, st), stream)
+
+
+def nmdlm_draft_verify(logits, draft_logits, M, V, draft, u, temperature, draft_temperature, tokens,
+                       accepted, cu_rows=None, n_seq=1, n_accepted=None, conf=None, chain=True,
+                       stream=None) -> None:
+    """chain False: every row counts (NMDLM_VERIFY_EACH)."""
+    what, ix = "nmdlm_draft_verify", logits.get_device()
+    _floats(what, ("logits", logits, torch.float32), ("draft_logits", draft_logits, torch.float32),
+            ("u", u, torch.float32), ("conf", conf, torch.float64))
+    args = (_arg(what, "logits", logits, M * V, 4, ix), _arg(what, "draft_logits", draft_logits, M * V, 4, ix),
+            M, V, _arg(what, "draft", draft, M, 4, ix), _arg(what, "u", u, 2 * M, 4, ix), float(temperature),
+            float(draft_temperature), _arg(what, "cu_rows", cu_rows, n_seq + 1, 4, ix), n_seq,
+            0 if chain else NMDLM_VERIFY_EACH, _arg(what, "tokens", tokens, M, 4, ix),
+            _arg(what, "accepted", accepted, M, 1, ix), _arg(what, "n_accepted", n_accepted, n_seq, 4, ix),
+            _arg(what, "conf", conf, M, 8, ix))
+    fn = load().nmdlm_draft_verify
+    _on(ix, what, lambda st: fn(*args, st), stream)
 
 
 def nmdlm_block_step(model: "DeviceModel", io: StepIO, ws: torch.Tensor, stream=None) -> None:

@@ -1,9 +1,11 @@
 // C ABI of libnmdlm: argument validation (before any HIP call), workspace
 // sizing and dispatch to the launchers.
 #include <algorithm>
+#include <cfloat>
 #include <climits>
 
 #include "common.h"
+#include "masked.h"
 #include "pages.h"
 
 namespace nmdlm {
@@ -121,6 +123,24 @@ nmdlm_status model_ok(const nmdlm_model* md) {
   if (md->d > NMDLM_MAX_K || md->F > NMDLM_MAX_K) return NMDLM_ERR_UNSUPPORTED;
   return NMDLM_OK;
 }
+
+// the sizes of a masked attention
+nmdlm_status masked_sizes_ok(int T, int M, int n_keys, int H, int dh) {
+  if (T < 1 || M < 1 || n_keys < 1 || H < 1 || dh < 1) return NMDLM_ERR_INVALID_ARG;
+  if (T > NMDLM_MAX_T || (dh != 64 && dh != 128) || n_keys > NMDLM_MAX_KEYS) return NMDLM_ERR_UNSUPPORTED;
+  if ((int64_t)T * M > (1 << 19) || (int64_t)H * dh > NMDLM_MAX_K) return NMDLM_ERR_UNSUPPORTED;
+  return NMDLM_OK;
+}
+
+// the mask's pointers; with a bias the positions too
+nmdlm_status mask_ok(const nmdlm_mask* m, bool bias) {
+  if (!m || !m->ranges || !aligned(m->ranges, 16)) return NMDLM_ERR_INVALID_ARG;
+  if (!bias) return NMDLM_OK;
+  if (!m->q_pos || !m->k_pos || !aligned(m->q_pos, 4) || !aligned(m->k_pos, 4)) return NMDLM_ERR_INVALID_ARG;
+  return m->max_dist >= 0 && m->max_dist <= NMDLM_MAX_DIST ? NMDLM_OK : NMDLM_ERR_INVALID_ARG;
+}
+
+bool temperature_ok(double t) { return t >= 0.0 && t <= DBL_MAX; }
 
 }  // namespace
 
@@ -479,6 +499,63 @@ nmdlm_status nmdlm_bbm_attn_paged(const nmdlm_pages* pg, const uint64_t* q, int 
   if (need > 0 && (!ws || !aligned(ws, 256) || ws_bytes < need)) return NMDLM_ERR_WORKSPACE;
   const PagedAttnCall c{q, k_pages, v_pages, T, H, dh, lut_att, sel, a_out, theta_a, s_out, nullptr, ws};
   return launch_paged_attn(*pg, c, static_cast<hipStream_t>(stream));
+}
+
+size_t nmdlm_bbm_attn_masked_workspace_size(int T, int M, int n_keys, int H, int dh) {
+  return masked_sizes_ok(T, M, n_keys, H, dh) == NMDLM_OK ? masked_attn_ws(T, M, n_keys, H, dh) : 0;
+}
+
+nmdlm_status nmdlm_bbm_attn_masked(const uint64_t* q, const uint64_t* k_cache, const uint64_t* vt_cache,
+                                   int64_t cache_cap, int T, int M, int n_keys, int H, int dh,
+                                   const uint8_t* lut_att, const nmdlm_mask* mask, const int8_t* bias,
+                                   int32_t* a_out, int32_t theta_a, uint64_t* s_out, void* ws,
+                                   size_t ws_bytes, void* stream) {
+  if (!lut_att || (!a_out && !s_out) || (s_out && theta_a <= 0)) return NMDLM_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)q, (const void*)k_cache, (const void*)vt_cache})
+    if (!p || !aligned(p, 8)) return NMDLM_ERR_INVALID_ARG;
+  if (!aligned(a_out, 4) || !aligned(s_out, 8)) return NMDLM_ERR_INVALID_ARG;
+  nmdlm_status rc = masked_sizes_ok(T, M, n_keys, H, dh);
+  if (rc != NMDLM_OK) return rc;
+  if ((rc = mask_ok(mask, bias != nullptr)) != NMDLM_OK) return rc;
+  if (cache_cap % 64 != 0 || cache_cap < n_keys) return NMDLM_ERR_INVALID_ARG;
+  if (cache_cap / 64 > INT_MAX) return NMDLM_ERR_UNSUPPORTED;
+  const size_t need = masked_attn_ws(T, M, n_keys, H, dh);
+  if (need > 0 && (!ws || !aligned(ws, 256) || ws_bytes < need)) return NMDLM_ERR_WORKSPACE;
+  const MaskedAttnCall c{q, k_cache, vt_cache, cache_cap, T, M, n_keys, H, dh, lut_att, *mask, bias, a_out,
+                         theta_a, s_out, nullptr, ws};
+  return launch_masked_attn(c, static_cast<hipStream_t>(stream));
+}
+
+nmdlm_status nmdlm_token_sample(const float* logits, int M, int V, double temperature, const float* u,
+                                int32_t* tokens, double* conf, void* stream) {
+  if (!logits || !tokens || M < 1 || V < 1 || !temperature_ok(temperature) || (temperature > 0.0 && !u))
+    return NMDLM_ERR_INVALID_ARG;
+  if (!aligned(logits, 4) || !aligned(u, 4) || !aligned(tokens, 4) || !aligned(conf, 8))
+    return NMDLM_ERR_INVALID_ARG;
+  if (V > NMDLM_MAX_SAMPLE_V) return NMDLM_ERR_UNSUPPORTED;
+  const VerifyCall c{logits, nullptr, nullptr, u, M, V, temperature, 0.0, nullptr, 1, true, tokens, nullptr,
+                     nullptr, conf};
+  return launch_verify(c, static_cast<hipStream_t>(stream));
+}
+
+nmdlm_status nmdlm_draft_verify(const float* logits, const float* draft_logits, int M, int V,
+                                const int32_t* draft, const float* u, double temperature,
+                                double draft_temperature, const int32_t* cu_rows, int n_seq, unsigned flags,
+                                int32_t* tokens, uint8_t* accepted, int32_t* n_accepted, double* conf,
+                                void* stream) {
+  if (!logits || !draft || !u || !tokens || !accepted || M < 1 || V < 1 || n_seq < 1 ||
+      !temperature_ok(temperature) || (flags & ~NMDLM_VERIFY_EACH))
+    return NMDLM_ERR_INVALID_ARG;
+  if ((draft_logits && !temperature_ok(draft_temperature)) || (!cu_rows && n_seq != 1))
+    return NMDLM_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)logits, (const void*)draft_logits, (const void*)draft, (const void*)u,
+                        (const void*)cu_rows, (const void*)tokens, (const void*)n_accepted})
+    if (!aligned(p, 4)) return NMDLM_ERR_INVALID_ARG;
+  if (!aligned(conf, 8)) return NMDLM_ERR_INVALID_ARG;
+  if (V > NMDLM_MAX_SAMPLE_V) return NMDLM_ERR_UNSUPPORTED;
+  const VerifyCall c{logits, draft_logits, draft, u, M, V, temperature, draft_temperature, cu_rows, n_seq,
+                     (flags & NMDLM_VERIFY_EACH) != 0, tokens, accepted, n_accepted, conf};
+  return launch_verify(c, static_cast<hipStream_t>(stream));
 }
 
 size_t nmdlm_block_step_workspace_size(const nmdlm_model* model, int M, unsigned flags) {

@@ -400,4 +400,28 @@ __device__ __forceinline__ int keys_of(int jc0, int step, int nch, int J) {
   return n * 64 - (((nch - 1 - jc0) % step == 0) ? nch * 64 - J : 0);
 }
 
+// ---------------------------------------------------------------------------
+// The neuron of one row and head: num(t) is the channel's sum, den(t) the
+// weights' sum; one wave per 64 channels.  Rows of the outputs are max_rows a timestep.
+// ---------------------------------------------------------------------------
+template <int DHW, typename Args, typename N, typename D>
+__device__ __forceinline__ void fire_row(const Args& a, int row, int h, int w, int lane, bool small, N num,
+                                         D den) {
+  const int dw = a.H * DHW;
+  int V = 0;
+  uint64_t uor = 0;
+  for (int t = 0; t < a.T; ++t) {
+    const int x = attn_norm1(num(t), den(t), small);
+    const size_t at = ((size_t)t * a.max_rows + row) * dw + h * DHW + w;
+    if (a.a_out) a.a_out[at * 64 + lane] = x;
+    V += x;
+    const bool s = V >= a.theta;
+    if (s) V -= a.theta;
+    const uint64_t word = __builtin_amdgcn_ballot_w64(s);
+    uor |= word;
+    if (a.s_out && lane == 0) a.s_out[at] = word;
+  }
+  if (a.u_out && lane == 0) a.u_out[(size_t)row * dw + h * DHW + w] = uor;
+}
+
 }  // namespace nmdlm

@@ -1,0 +1,48 @@
+// Internal declarations of the masked attention and of drawing tokens (not installed).
+#pragma once
+
+#include "common.h"
+
+namespace nmdlm {
+
+struct MaskedAttnCall {
+  const uint64_t* q;
+  const uint64_t* k_cache;
+  const uint64_t* vt_cache;
+  int64_t cap;
+  int T, M, n_keys, H, dh;
+  const uint8_t* lut;
+  nmdlm_mask mask;
+  const int8_t* bias;  // or null
+  int32_t* a_out;      // or null
+  int32_t theta;
+  uint64_t* s_out;     // or null
+  uint64_t* u_out;     // or null: per-row union over t
+  void* ws;
+};
+// Waves a timestep and most splits of a call's rows.
+struct MaskedRoute {
+  int parts, splits;
+};
+MaskedRoute masked_route(int T, int M, int n_keys, int H);
+size_t masked_attn_ws(int T, int M, int n_keys, int H, int dh);
+nmdlm_status launch_masked_attn(const MaskedAttnCall& c, hipStream_t st);
+
+struct VerifyCall {
+  const float* logits;
+  const float* draft_logits;  // or null
+  const int32_t* draft;       // null: every row is drawn from its logits
+  const float* u;             // [M][2], or [M] without drafts
+  int M, V;
+  double tau, draft_tau;
+  const int32_t* cu;          // or null
+  int n_seq;
+  bool each;
+  int32_t* tokens;
+  uint8_t* accepted;
+  int32_t* n_accepted;
+  double* conf;
+};
+nmdlm_status launch_verify(const VerifyCall& c, hipStream_t st);
+
+}  // namespace nmdlm

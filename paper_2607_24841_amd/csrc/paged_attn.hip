@@ -373,29 +373,6 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_paged_att
 }
 
 // ---------------------------------------------------------------------------
-// The neuron of one row and head: num(t) is the channel's sum, den(t) the
-// weights' sum; one wave per 64 channels.
-// ---------------------------------------------------------------------------
-template <int DHW, typename N, typename D>
-__device__ __forceinline__ void fire_row(const PagedArgs& a, int row, int h, int w, int lane, bool small, N num,
-                                         D den) {
-  const int dw = a.H * DHW;
-  int V = 0;
-  uint64_t uor = 0;
-  for (int t = 0; t < a.T; ++t) {
-    const int x = attn_norm1(num(t), den(t), small);
-    const size_t at = ((size_t)t * a.max_rows + row) * dw + h * DHW + w;
-    if (a.a_out) a.a_out[at * 64 + lane] = x;
-    V += x;
-    const bool s = V >= a.theta;
-    if (s) V -= a.theta;
-    const uint64_t word = __builtin_amdgcn_ballot_w64(s);
-    uor |= word;
-    if (a.s_out && lane == 0) a.s_out[at] = word;
-  }
-  if (a.u_out && lane == 0) a.u_out[(size_t)row * dw + h * DHW + w] = uor;
-}
-
 // k_paged_join: the sums of a row's splits (integers: any order gives the same)
 // and the neuron.  A workgroup per row and head, a wave per timestep and 64
 // channels: 5 us for 32 rows of 16 heads in 8 splits, a chain of three loads (18 us
