@@ -400,6 +400,77 @@ __device__ __forceinline__ int keys_of(int jc0, int step, int nch, int J) {
   return n * 64 - (((nch - 1 - jc0) % step == 0) ? nch * 64 - J : 0);
 }
 
+// The neuron of 16 rows over their sums: sNum [part][t][tile][lane] (row lane%16,
+// channels 16n + 4(lane/16) + e) and sDen [part][t][row].  Waves share the NT
+// tiles of 16 channels; a timestep's weights are summed and inverted once for
+// all tiles of a wave.  All threads of the workgroup call it.
+template <int DHW, typename Args>
+__device__ __forceinline__ void fire_rows(const Args& a, const v4i* sNum, const int (*sDen)[16],
+                                          uint32_t (*sWord)[16][2 * DHW], int row0, int nr, int h, bool small,
+                                          int tid, int nth) {
+  constexpr int NT = DHW * 4, DH = DHW * 64;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nwaves = nth >> 6;
+  const int g = lane >> 4, c = lane & 15;
+  const int d = a.H * DH, dw = d / 64;
+  const bool vec = (reinterpret_cast<uintptr_t>(a.a_out) & 15) == 0;
+  for (int i = tid; i < a.T * 32 * DHW; i += nth) (&sWord[0][0][0])[i] = 0u;
+  __syncthreads();
+  v4i V[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) V[j] = v4i{0, 0, 0, 0};
+  for (int t = 0; t < a.T; ++t) {
+    int den = 0;
+    for (int p = 0; p < a.parts; ++p) den += sDen[p * a.T + t][c];
+    const float den_f = (float)max(den, 1), k = attn_factor(den_f);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int n = wave + j * nwaves;
+      if (n >= NT) break;  // wave-uniform
+      v4i x = sNum[(t * NT + n) * 64 + lane];
+      for (int p = 1; p < a.parts; ++p) x += sNum[((p * a.T + t) * NT + n) * 64 + lane];
+      if (small) {  // uniform
+        x = attn_norm4(x, den_f, k);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = attn_norm(x[e], den);
+      }
+      if (a.a_out && c < nr) {
+        int32_t* o = a.a_out + ((size_t)t * a.max_rows + row0 + c) * d + h * DH + n * 16 + 4 * g;
+        if (vec) {
+          *reinterpret_cast<v4i*>(o) = x;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = x[e];
+        }
+      }
+      uint32_t bits = 0u;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        V[j][e] += x[e];
+        const bool s = V[j][e] >= a.theta;
+        if (s) V[j][e] -= a.theta;
+        bits |= (uint32_t)s << e;
+      }
+      atomicOr(&sWord[t][c][n >> 1], bits << (16 * (n & 1) + 4 * g));
+    }
+  }
+  if (!a.s_out) return;  // uniform
+  __syncthreads();
+  for (int i = tid; i < 16 * DHW * a.T; i += nth) {
+    const int k = i % DHW, m = (i / DHW) % 16, t = i / (16 * DHW);
+    if (m < nr)
+      a.s_out[((size_t)t * a.max_rows + row0 + m) * dw + h * DHW + k] =
+          sWord[t][m][2 * k] | (uint64_t)sWord[t][m][2 * k + 1] << 32;
+  }
+  if (a.u_out)
+    for (int i = tid; i < 16 * DHW; i += nth) {
+      const int k = i % DHW, m = i / DHW;
+      uint64_t uor = 0ull;
+      for (int t = 0; t < a.T; ++t) uor |= sWord[t][m][2 * k] | (uint64_t)sWord[t][m][2 * k + 1] << 32;
+      if (m < nr) a.u_out[(size_t)(row0 + m) * dw + h * DHW + k] = uor;
+    }
+}
+
 // ---------------------------------------------------------------------------
 // The neuron of one row and head: num(t) is the channel's sum, den(t) the
 // weights' sum; one wave per 64 channels.  Rows of the outputs are max_rows a timestep.

@@ -20,9 +20,10 @@ struct MaskedAttnCall {
   uint64_t* u_out;     // or null: per-row union over t
   void* ws;
 };
-// Waves a timestep and most splits of a call's rows.
+// Rows of a workgroup (1: the row kernel; 16 or 32: tiles), waves a timestep, most
+// splits.
 struct MaskedRoute {
-  int parts, splits;
+  int tile, parts, splits;
 };
 MaskedRoute masked_route(int T, int M, int n_keys, int H);
 size_t masked_attn_ws(int T, int M, int n_keys, int H, int dh);

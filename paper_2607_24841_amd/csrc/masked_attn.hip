@@ -1,5 +1,7 @@
 // Attention on spike operands whose rows see the keys of two ranges each, with a
 // bias of the scores by distance (the formulas: attn_device.h and nmdlm.h).
+#include <limits.h>
+
 #include <algorithm>
 
 #include "attn_device.h"
@@ -22,6 +24,7 @@ struct MaskedArgs {
   uint64_t* u_out;
   int32_t* part;  // sums of the splits [row][head][split][T][64 DHW + kMaskedDen]
   int n_keys, max_rows, T, H, parts, splits, max_dist;
+  int tile;       // rows that a workgroup takes: 1, 16 or 32
   int32_t theta;
 };
 constexpr int kMaskedDen = 4;    // the weights' sum behind the channels' sums, and padding
@@ -56,6 +59,30 @@ __device__ __forceinline__ ChunkList chunk_list(const KeyRanges& k) {
     b = b1 = 0;
   }
   return ChunkList{a, a1 - a, b, a1 - a + b1 - b};
+}
+// The rows of a tile together: the hulls of their two ranges, and the keys that all
+// of them see by the first or by the second.  Every lane of the wave gets the same.
+struct TileKeys {
+  KeyRanges hull, all;
+};
+__device__ __forceinline__ int wave_min(int x) {
+  for (int o = 32; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ int wave_max(int x) { return ~wave_min(~x); }
+__device__ __forceinline__ TileKeys tile_keys(const MaskedArgs& a, int row0, int lane) {
+  const int row = row0 + lane % a.tile;
+  KeyRanges k = key_ranges(a.ranges[min(row, a.max_rows - 1)], a.n_keys);
+  const bool there = row < a.max_rows, in_a = there && k.a1 > 0, in_b = there && k.b1 > 0;
+  TileKeys t;
+  t.hull = KeyRanges{wave_min(in_a ? k.a0 : INT_MAX), wave_max(in_a ? k.a1 : 0),
+                     wave_min(in_b ? k.b0 : INT_MAX), wave_max(in_b ? k.b1 : 0)};
+  if (t.hull.a1 == 0) t.hull.a0 = 0;
+  if (t.hull.b1 == 0) t.hull.b0 = 0;
+  // a row that is not there asks for nothing; one whose range is empty sees nothing by it
+  t.all = KeyRanges{wave_max(there ? k.a0 : 0), wave_min(there ? k.a1 : INT_MAX),
+                    wave_max(there ? k.b0 : 0), wave_min(there ? k.b1 : INT_MAX)};
+  return t;
 }
 // Splits of a list of n chunks, and the part of split z.
 __device__ __forceinline__ int split_count(const MaskedArgs& a, int n) {
@@ -160,6 +187,274 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_masked_rows(MaskedArgs a) {
                   [&](int tt) { return sDen[tt]; });
 }
 
+// ---------------------------------------------------------------------------
+// k_masked_tiles: a tile of 16*QG rows, a head and one of the tile's splits; wave =
+// (timestep, part), the sums and the pipeline of attn_device.h over the chunks
+// that any row of the tile sees.  A chunk that not all of them see whole is
+// masked: a lane (one row, 16 keys) makes the bits of its keys from the row's
+// ranges, and the weights of the others become 0 (byte -128).  The values of the
+// keys past n_keys in the last chunk then count with weight 0 too.
+//
+// Bias: the scores' sums begin with 8 * bias, so it costs no instruction behind the
+// products; the table is extended by 128 entries below and above, which clamps.  A
+// chunk whose keys are all at least max_dist before (or behind) all rows of the tile
+// has one bias for all pairs.
+// ---------------------------------------------------------------------------
+constexpr int kWideEntries = 384;  // scores -128 .. 255
+struct WideLut {
+  int e[2][kWideEntries][2];
+};
+template <bool BIAS>
+struct MaskedLut {
+  AttnLut lut;
+};
+template <>
+struct MaskedLut<true> {
+  WideLut lut;
+};
+
+template <int DHW, int QG>
+__device__ __forceinline__ void add_scores(const v4i (&q)[QG][DHW], const uint32_t (&k)[4], v4i (&s)[QG][4]) {
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    v4i k0, k1;
+    if constexpr (DHW == 2) {
+      k0 = key_bytes(k[u]);
+      k1 = key_bytes(k[u] >> 4);
+    } else {
+      k0 = key_bytes(k[u] | (k[u] << 12));
+    }
+#pragma unroll
+    for (int w = 0; w < QG; ++w) s[w][u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k0, q[w][0], s[w][u], 0, 0, 0);
+    if constexpr (DHW == 2) {
+#pragma unroll
+      for (int w = 0; w < QG; ++w) s[w][u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k1, q[w][1], s[w][u], 0, 0, 0);
+    }
+  }
+}
+
+// bits [lo, hi) of 16
+__device__ __forceinline__ uint32_t bits16(int lo, int hi) {
+  return ((1u << min(max(hi, 0), 16)) - 1u) & ~((1u << min(max(lo, 0), 16)) - 1u);
+}
+
+template <int DHW, int QG, bool BIAS>
+__global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_masked_tiles(MaskedArgs a) {
+  constexpr int NT = DHW * 4, DH = DHW * 64;
+  constexpr int kHalf = (BIAS ? kWideEntries : kLutEntries) * 8;  // bytes of half a table
+  __shared__ MaskedLut<BIAS> sLut;
+  __shared__ int sDen[NMDLM_MAX_T][16];  // [part][T], at most eight waves
+  __shared__ uint32_t sWord[NMDLM_MAX_T][16][2 * DHW];
+  __shared__ int sPos[BIAS ? NMDLM_MAX_T * kAttnStages : 1][64];  // positions of the staged keys
+  // the waves' stages, then their sums [part][T][NT][64]; behind them 8 * bias
+  extern __shared__ v4i sNum[];
+  AttnStage<DHW>* sStage = reinterpret_cast<AttnStage<DHW>*>(sNum);
+
+  const int nth = blockDim.x, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nwaves = nth >> 6;
+  const int g = lane >> 4, c = lane & 15;
+  // neighbouring heads share key lines: consecutive logical ids, head fastest; the
+  // last tiles first, which see most keys where rows see what is before them
+  const int lid = xcd_order(blockIdx.x, gridDim.x);
+  const int h = lid % a.H, z = (lid / a.H) % a.splits;
+  const int n_tiles = (a.max_rows + 16 * QG - 1) / (16 * QG);
+  const int row0 = (n_tiles - 1 - lid / (a.H * a.splits)) * 16 * QG;
+  const int nr = min(a.max_rows - row0, 16 * QG);
+  const int np = a.parts, t = wave / np, part = wave - t * np;
+  const int d = a.H * DH, dw = d / 64, D = a.max_dist;
+  const uint64_t* kb = a.kc + (size_t)t * a.cap * dw + h * DHW;
+  const uint64_t* vb = a.vt + (size_t)t * (a.cap / 64) * d + h * DH;
+
+  uint32_t qraw[QG];
+  AttnWave<DHW, QG>::load_queries(qraw, a.q + ((size_t)t * a.max_rows + row0) * dw + h * DHW, dw, 0, nr - 1, g, c);
+  KeyRanges kr[QG];
+  int qp[QG];
+#pragma unroll
+  for (int u = 0; u < QG; ++u) {
+    const int row = min(row0 + 16 * u + c, a.max_rows - 1);
+    kr[u] = key_ranges(a.ranges[row], a.n_keys);
+    qp[u] = BIAS ? a.q_pos[row] : 0;
+  }
+  const TileKeys tk = tile_keys(a, row0, lane);
+  const ChunkList cl = chunk_list(tk.hull);
+  const int splits = split_count(a, cl.n);
+  if (z >= splits) return;  // uniform
+  const int i0 = split_at(cl.n, z, splits), i1 = split_at(cl.n, z + 1, splits);
+  int* const sBias = reinterpret_cast<int*>(sNum + nwaves * NT * 64);
+  int q_lo = 0, q_hi = 0;
+  if constexpr (BIAS) {
+    q_lo = q_hi = qp[0];
+#pragma unroll
+    for (int u = 1; u < QG; ++u) {
+      q_lo = min(q_lo, qp[u]);
+      q_hi = max(q_hi, qp[u]);
+    }
+    q_lo = wave_min(q_lo);
+    q_hi = wave_max(q_hi);
+    for (int i = tid; i < 2 * D + 1; i += nth) sBias[i] = 8 * a.bias[(size_t)h * (2 * D + 1) + i];
+    for (int i = tid; i < kWideEntries; i += nth) {
+      const uint32_t v = (uint32_t)a.lut[min(max(i - 128, 0), 255)] ^ 0x80u;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) sLut.lut.e[b >> 1][i][b & 1] = (int)(v << (8 * b));
+    }
+  } else {
+    fill_lut(sLut.lut, load_lut(a.lut, tid, nth), tid, nth);
+  }
+  AttnWave<DHW, QG> w;
+  w.init(qraw);
+  __syncthreads();
+
+  const char* lb = reinterpret_cast<const char*>(&sLut) + (BIAS ? 128 * 8 : 0);
+  AttnStage<DHW>* const st = &sStage[kAttnStages * wave];
+  int keys = 0;
+  if (i0 + part < i1) {  // wave-uniform
+    // as AttnWave::run: the weighted sum of one chunk while the table reads of the
+    // next are in flight, and the loads of the one after that
+    auto chunk_at = [&](int i) { return cl.at(min(i, i1 - 1)); };
+    int kp = 0;  // the position of key `lane` of the chunk in `next`
+    auto load = [&](AttnChunk<DHW>& ch, int jc) {
+      AttnWave<DHW, QG>::load(ch, kb, vb, dw, d, jc, lane);
+      if constexpr (BIAS) kp = a.k_pos[min(64 * jc + lane, a.n_keys - 1)];
+    };
+    // returns the side of the chunk: 1 all keys max_dist or more before the rows, -1
+    // behind, 0 between
+    auto put = [&](const AttnChunk<DHW>& ch, AttnStage<DHW>& s, int slot) {
+      int side = 0;
+      if constexpr (BIAS) {
+        const bool before = __builtin_elementwise_sub_sat(q_lo, kp) >= D;
+        const bool behind = __builtin_elementwise_sub_sat(q_hi, kp) <= -D;
+        side = __builtin_amdgcn_ballot_w64(before) == ~0ull ? 1
+               : __builtin_amdgcn_ballot_w64(behind) == ~0ull ? -1 : 0;
+        sPos[kAttnStages * wave + slot][lane] = kp;
+      }
+      w.put(ch, s, lane);
+      return side;
+    };
+    v4i s[QG][4], p[QG];
+    auto biased = [&](int slot, int side) {  // what the scores begin with
+      if constexpr (BIAS) {
+        if (side != 0) {  // wave-uniform
+          const int b = sBias[side > 0 ? 2 * D : 0];
+#pragma unroll
+          for (int u = 0; u < QG; ++u)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[u][k] = v4i{b, b, b, b};
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const v4i pos = *reinterpret_cast<const v4i*>(&sPos[kAttnStages * wave + slot][16 * g + 4 * k]);
+#pragma unroll
+            for (int u = 0; u < QG; ++u)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int off = __builtin_elementwise_sub_sat(qp[u], pos[e]);
+                s[u][k][e] = sBias[min(max(off, -D), D) + D];
+              }
+          }
+        }
+      }
+    };
+    auto score = [&](const uint32_t (&k)[4], int slot, int side) {
+      if constexpr (BIAS) {
+        biased(slot, side);
+        add_scores<DHW, QG>(w.q, k, s);
+      } else {
+        w.scores(k, s);
+      }
+    };
+    auto lookup = [&]() {
+#pragma unroll
+      for (int u = 0; u < QG; ++u)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int b = k == 1 ? 2 : (k == 2 ? 1 : k);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            s[u][k][e] = *reinterpret_cast<const int*>(lb + kHalf * (b >> 1) + 4 * (b & 1) + s[u][k][e]);
+        }
+    };
+    auto masked = [&](int jc) {  // weight 0 for the keys that a row does not see
+      const int j0 = 64 * jc, j1 = j0 + 64;
+      if ((j0 >= tk.all.a0 && j1 <= tk.all.a1) || (j0 >= tk.all.b0 && j1 <= tk.all.b1)) return;  // uniform
+      const int j = j0 + 16 * g;
+#pragma unroll
+      for (int u = 0; u < QG; ++u) {
+        const uint32_t vm = bits16(kr[u].a0 - j, kr[u].a1 - j) | bits16(kr[u].b0 - j, kr[u].b1 - j);
+        const v4i m = bytes16(vm | (vm << 12)) * 0xFF;
+        p[u] = (p[u] & m) | (~m & (int)0x80808080u);
+      }
+    };
+    uint32_t k[4], v[NT];
+    AttnChunk<DHW> first, next;
+    int i = i0 + part, s0 = 0, s1 = 1, s2 = 2;  // the stages of chunks i - np, i, i + np
+    load(first, chunk_at(i));
+    int d0 = put(first, st[s0], s0), d1, d2;  // their sides
+    load(next, chunk_at(i + np));
+    w.key_pieces(st[s0], k, g, c);
+    d1 = put(next, st[s1], s1);
+    load(next, chunk_at(i + 2 * np));
+    score(k, s0, d0);
+    lookup();
+    w.key_pieces(st[s1], k, g, c);
+    w.pack(s, p);
+    masked(cl.at(i));
+    for (i += np; i < i1; i += np) {  // wave-uniform
+      w.value_pieces(st[s0], v, g, c);
+      score(k, s1, d1);
+      __builtin_amdgcn_sched_barrier(0);
+      lookup();
+      d2 = put(next, st[s2], s2);
+      load(next, chunk_at(i + 2 * np));
+      w.key_pieces(st[s2], k, g, c);
+      keys += 64;
+      w.weigh(v, p);
+      __builtin_amdgcn_sched_barrier(0);
+      w.pack(s, p);
+      masked(cl.at(i));
+      const int tmp = s0;
+      s0 = s1;
+      s1 = s2;
+      s2 = tmp;
+      d1 = d2;
+    }
+    w.value_pieces(st[s0], v, g, c);
+    keys += 64;
+    w.weigh(v, p);
+  }
+  w.finish(reinterpret_cast<char*>(st), lane, g, c);
+  __syncthreads();  // the stages are read
+
+#pragma unroll
+  for (int u = 0; u < QG; ++u) {
+    if (u > 0) __syncthreads();  // the sums and words of the group before are read
+    const int rows = nr - 16 * u, pt = part * a.T + t;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) sNum[(pt * NT + n) * 64 + lane] = w.acc[u][n];
+    if (g == 0) sDen[pt][c] = w.den[u] + 128 * keys;
+    __syncthreads();
+    if (splits > 1) {  // uniform
+      for (int i = tid; i < a.T * NT * 64; i += nth) {
+        const int tt = i / (NT * 64), n = (i >> 6) % NT, r = i & 15, lg = (i >> 4) & 3;
+        if (r < rows) {
+          v4i x = sNum[i];
+          for (int p = 1; p < np; ++p) x += sNum[p * a.T * NT * 64 + i];
+          *reinterpret_cast<v4i*>(split_sums<DHW>(a, row0 + 16 * u + r, h, z) +
+                                  (size_t)tt * (DH + kMaskedDen) + 16 * n + 4 * lg) = x;
+        }
+      }
+      for (int i = tid; i < a.T * 16; i += nth)
+        if (i % 16 < rows) {
+          int den = 0;
+          for (int p = 0; p < np; ++p) den += sDen[p * a.T + i / 16][i % 16];
+          split_sums<DHW>(a, row0 + 16 * u + i % 16, h, z)[(size_t)(i / 16) * (DH + kMaskedDen) + DH] = den;
+        }
+      continue;
+    }
+    if (rows <= 0) continue;  // uniform
+    fire_rows<DHW>(a, sNum, sDen, sWord, row0 + 16 * u, min(rows, 16), h, a.n_keys < 65536, tid, nth);
+  }
+}
+
 // k_masked_join: the sums of a row's splits (integers: any order gives the same)
 // and the neuron.  A workgroup per row and head, a wave per timestep and 64
 // channels.
@@ -169,9 +464,10 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T * DHW) void k_masked_join(MaskedAr
   __shared__ int sNum[NMDLM_MAX_T][64 * DHW];
   __shared__ int sDen[NMDLM_MAX_T];
   const int h = blockIdx.x % a.H, row = blockIdx.x / a.H;
-  const int n = split_count(a, chunk_list(key_ranges(a.ranges[row], a.n_keys)).n);
+  const int lane = threadIdx.x & 63;
+  const int n = split_count(a, chunk_list(tile_keys(a, row - row % a.tile, lane).hull).n);
   if (n == 1) return;  // uniform; a single split fired by itself
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int t = wave / DHW, w = wave - t * DHW;
   const int32_t* base = split_sums<DHW>(a, row, h, 0) + (size_t)t * LD;
   const size_t ld = (size_t)a.T * LD;
@@ -189,8 +485,13 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T * DHW) void k_masked_join(MaskedAr
 }
 
 MaskedRoute masked_route(int T, int M, int n_keys, int H) {
-  MaskedRoute r{std::max(std::min(kRowWaves / T, 4), 1), 1};
-  r.splits = (int)std::max(1LL, std::min<long long>({512 / ((long long)M * H), 64, n_keys / (64 * kSplitChunks)}));
+  MaskedRoute r{1, T <= 2 ? 4 : (T <= 4 ? 2 : 1), 1};
+  if (M > 2) r.tile = M >= 32 && (long long)(M / 32) * H * T >= 1024 ? 32 : 16;
+  if (r.tile == 1) r.parts = std::max(std::min(kRowWaves / T, 4), 1);
+  if (r.tile == 32) r.parts = 1;
+  const long long units = (long long)((M + r.tile - 1) / r.tile) * H;
+  r.splits = (int)std::max(1LL, std::min<long long>({(r.tile == 1 ? 512 : 256) / units, 64,
+                                                     n_keys / (64 * kSplitChunks)}));
   return r;
 }
 
@@ -200,15 +501,37 @@ size_t masked_attn_ws(int T, int M, int n_keys, int H, int dh) {
   return align_up((size_t)M * H * r.splits * T * (dh + kMaskedDen) * sizeof(int32_t), 256);
 }
 
+constexpr size_t kMaskedPlainLds = 32768;  // dynamic LDS that needs no attribute beside the static
+
+template <int DHW, int QG, bool BIAS>
+static nmdlm_status launch_tiles(const MaskedArgs& a, unsigned grid, hipStream_t st) {
+  size_t dyn = (size_t)a.T * a.parts * std::max(DHW * 4 * 64 * sizeof(v4i), kAttnStages * sizeof(AttnStage<DHW>));
+  if (BIAS) dyn += (2 * a.max_dist + 1) * sizeof(int);
+  if (dyn > kMaskedPlainLds &&
+      hipFuncSetAttribute(reinterpret_cast<const void*>(&k_masked_tiles<DHW, QG, BIAS>),
+                          hipFuncAttributeMaxDynamicSharedMemorySize, (int)dyn) != hipSuccess)
+    return NMDLM_ERR_HIP;
+  hipLaunchKernelGGL((k_masked_tiles<DHW, QG, BIAS>), dim3(grid), dim3(64 * a.T * a.parts), (uint32_t)dyn, st, a);
+  return hip_status();
+}
+
 template <int DHW>
 static nmdlm_status launch_masked_dh(const MaskedAttnCall& c, hipStream_t st) {
   const MaskedRoute r = masked_route(c.T, c.M, c.n_keys, c.H);
   const MaskedArgs a{c.q, c.k_cache, c.vt_cache, c.cap, reinterpret_cast<const int4*>(c.mask.ranges),
                      c.mask.q_pos, c.mask.k_pos, c.bias, c.lut, c.a_out, c.s_out, c.u_out,
                      static_cast<int32_t*>(c.ws), c.n_keys, c.M, c.T, c.H, r.parts, r.splits,
-                     c.bias ? c.mask.max_dist : 0, c.theta};
-  hipLaunchKernelGGL(k_masked_rows<DHW>, dim3((unsigned)c.M * c.H * r.splits), dim3(64 * c.T * r.parts), 0, st, a);
-  const nmdlm_status rc = hip_status();
+                     c.bias ? c.mask.max_dist : 0, r.tile, c.theta};
+  const unsigned grid = (unsigned)((c.M + r.tile - 1) / r.tile) * c.H * r.splits;
+  nmdlm_status rc;
+  if (r.tile == 1) {
+    hipLaunchKernelGGL(k_masked_rows<DHW>, dim3(grid), dim3(64 * c.T * r.parts), 0, st, a);
+    rc = hip_status();
+  } else if (r.tile == 16) {
+    rc = c.bias ? launch_tiles<DHW, 1, true>(a, grid, st) : launch_tiles<DHW, 1, false>(a, grid, st);
+  } else {
+    rc = c.bias ? launch_tiles<DHW, 2, true>(a, grid, st) : launch_tiles<DHW, 2, false>(a, grid, st);
+  }
   if (rc != NMDLM_OK || r.splits == 1) return rc;
   hipLaunchKernelGGL(k_masked_join<DHW>, dim3((unsigned)c.M * c.H), dim3(64 * c.T * DHW), 0, st, a);
   return hip_status();

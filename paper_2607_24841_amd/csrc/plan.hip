@@ -3,6 +3,7 @@
 // is stored channel-major.  Not part of the installed header; nothing is
 // launched and no GPU is needed.
 #include "common.h"
+#include "masked.h"
 #include "pages.h"
 
 using namespace nmdlm;
@@ -84,6 +85,15 @@ void nmdlm_internal_paged_route(int n_seq, int max_rows, int max_pages, int T, i
   out[2] = r.parts;
   out[3] = r.splits;
   out[4] = select_fused(pg, H) ? 1 : 0;
+}
+
+// The route of a masked attention call: rows of a workgroup (1: the row kernel),
+// waves per timestep, most splits.
+void nmdlm_internal_masked_route(int T, int M, int n_keys, int H, int32_t* out) {
+  const MaskedRoute r = masked_route(T, M, n_keys, H);
+  out[0] = r.tile;
+  out[1] = r.parts;
+  out[2] = r.splits;
 }
 
 // The runs of row block y of M tokens into out[4 i ..]: sequence, first position,

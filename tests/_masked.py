@@ -61,6 +61,18 @@ def make_case(seed, ranges, q_pos, n_keys, T=4, H=2, dh=64, max_dist=None, rate=
     return c
 
 
+def route(T, M, n_keys, H):
+    """The kernel a call takes (a host-side query): rows of a workgroup (1: the row
+    kernel), waves per timestep, most splits."""
+    import ctypes as C
+
+    from paper_2607_24841_amd import binding as B
+
+    out = (C.c_int32 * 3)()
+    B.load().nmdlm_internal_masked_route(T, M, n_keys, H, out)
+    return SimpleNamespace(tile=out[0], parts=out[1], splits=out[2])
+
+
 def attention(c):
     a = O.masked_attention(c.q, c.k[:, :c.n_keys], c.v[:, :c.n_keys], c.H, c.lut, np.clip(c.ranges, 0, c.n_keys),
                            c.bias, c.q_pos, c.k_pos, c.max_dist)

@@ -55,6 +55,27 @@ def test_blocks(S):
     check(K.make_case(S, r, pos, 300, T=3, H=2, dh=128, max_dist=30, k_pos=pos))
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("max_dist", [None, 20])
+def test_tiles_of_32_rows(dh, max_dist):
+    """Rows enough for 32 a wave: drafted, ragged, empty and unordered ones."""
+    rng = np.random.default_rng(dh)
+    r, pos = K.docs_mask([100, 3, 77], 93)
+    r[150:200], pos[150:200] = K.random_mask(rng, 50, 400)
+    assert K.route(8, len(r), 400, 16).tile == 32
+    check(K.make_case(dh, r, pos, 400, T=8, H=16, dh=dh, max_dist=max_dist))
+
+
+@pytest.mark.parametrize("T, M, n_keys, H, tile, split", [(4, 1, 300, 2, 1, False), (4, 2, 3000, 2, 1, True),
+                                                          (4, 3, 300, 2, 16, False), (2, 40, 5000, 1, 16, True)])
+def test_routes_of_small_calls(T, M, n_keys, H, tile, split):
+    """The kernels that the sizes of these tests reach."""
+    r = K.route(T, M, n_keys, H)
+    assert (r.tile, r.splits > 1) == (tile, split)
+    pos = n_keys - M + np.arange(M)
+    check(K.make_case(M, np.stack([0 * pos, pos + 1, 0 * pos, 0 * pos], 1), pos, n_keys, T=T, H=H, max_dist=33))
+
+
 def test_documents_and_rows_of_none():
     r, pos = K.docs_mask([1, 64, 63, 65, 2, 130, 7], 20)
     c = K.make_case(1, r, pos, len(r), H=5, max_dist=10, k_pos=pos)
