@@ -21,130 +21,441 @@ struct VerifyArgs {
   bool chain;
 };
 
-constexpr int kRowThreads = 256;
+// ---------------------------------------------------------------------------
+// A workgroup takes a row (of the target, and of the draft): a thread holds
+// kQuads groups of four consecutive logits in registers, group k of thread i being
+// ids 4 (k nth + i) on, less the row's offset from a 16-byte address, so that a
+// wave reads 1 KB runs.  Up to kQuads * 4 * 1024 ids the row is read once; longer rows go
+// in tiles of that size and are read again for each step.
+// ---------------------------------------------------------------------------
+constexpr int kQuads = 8;
+constexpr int kMaxThreads = 1024;
+constexpr int kSegs = kQuads * kMaxThreads / 16;  // of 64 ids: the sums of 16 lanes
+constexpr int kMaxTiles = NMDLM_MAX_SAMPLE_V / (kQuads * 4 * kMaxThreads) + 1;
 constexpr double kExpFloor = -700.0;  // exponents below weigh nothing
 
-// A row of logits at a temperature: its largest value, that value's first id and
-// the sum of the weights.
-struct Row {
+// 2^(j/32), correctly rounded
+__device__ const double kPow[32] = {
+    0x1.0000000000000p+0, 0x1.059b0d3158574p+0, 0x1.0b5586cf9890fp+0, 0x1.11301d0125b51p+0,
+    0x1.172b83c7d517bp+0, 0x1.1d4873168b9aap+0, 0x1.2387a6e756238p+0, 0x1.29e9df51fdee1p+0,
+    0x1.306fe0a31b715p+0, 0x1.371a7373aa9cbp+0, 0x1.3dea64c123422p+0, 0x1.44e086061892dp+0,
+    0x1.4bfdad5362a27p+0, 0x1.5342b569d4f82p+0, 0x1.5ab07dd485429p+0, 0x1.6247eb03a5585p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.71f75e8ec5f74p+0, 0x1.7a11473eb0187p+0, 0x1.82589994cce13p+0,
+    0x1.8ace5422aa0dbp+0, 0x1.93737b0cdc5e5p+0, 0x1.9c49182a3f090p+0, 0x1.a5503b23e255dp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0,
+    0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0,
+};
+
+struct Quads {
+  float x[kQuads][4];
+};
+
+struct RowShared {
+  double seg[kSegs];
+  double tile[kMaxTiles];
+  double part[2][kMaxThreads / 16];
+  double pow[32];  // 2^(j/32)
+  float top[2][kMaxThreads / 64];
+  int first[kMaxThreads / 64];
+};
+
+// A row and where a thread's groups of it lie: the target's from the 16-byte address
+// at or before the row on, the draft's the same ids.
+struct RowAt {
   const float* l;
+  int V, shift;  // ids before the row's first
+  bool vec;      // the groups are 16-byte aligned
+  __device__ __forceinline__ static int shift_of(const float* row) {
+    return (int)((reinterpret_cast<uintptr_t>(row) >> 2) & 3);
+  }
+  __device__ __forceinline__ RowAt(const float* row, int V_, int shift_)
+      : l(row), V(V_), shift(shift_), vec(shift_of(row) == shift_) {}
+  __device__ __forceinline__ int tile_ids() const { return kQuads * 4 * blockDim.x; }
+  __device__ __forceinline__ int tiles() const { return (V + shift + tile_ids() - 1) / tile_ids(); }
+  __device__ __forceinline__ int id(int tile, int k) const {
+    return tile * tile_ids() + 4 * (int)(k * blockDim.x + threadIdx.x) - shift;
+  }
+  // any id of the workgroup in group k
+  __device__ __forceinline__ bool has(int tile, int k) const {
+    return tile * tile_ids() + 4 * (int)(k * blockDim.x) - shift < V;
+  }
+  // NaN and ids outside the row become -inf
+  __device__ __forceinline__ void load(Quads& q, int tile) const {
+#pragma unroll
+    for (int k = 0; k < kQuads; ++k) {
+      const int v = id(tile, k);
+      if (vec && v >= 0 && v + 3 < V) {
+        const float4 f = *reinterpret_cast<const float4*>(l + v);
+        q.x[k][0] = f.x;
+        q.x[k][1] = f.y;
+        q.x[k][2] = f.z;
+        q.x[k][3] = f.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q.x[k][e] = v + e >= 0 && v + e < V ? l[v + e] : -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) q.x[k][e] = fmaxf(q.x[k][e], -INFINITY);
+  }
+};
+
+// exp(e) for -700 <= e <= 0, else 0 (NaN too), relative error below 2^-48: with n =
+// round(32 e / ln 2), exp(e) = 2^(n / 32) exp(r), r = e - n ln 2 / 32, |r| <= 0.0109, the
+// powers from a table of 32 and exp(r) by its series to r^5 (r^6 / 720 < 2.4e-15).  The
+// table fills each LDS bank once, so its reads do not conflict.
+__device__ __forceinline__ double exp_weight(double e, const double* pow) {
+  constexpr double kMagic = 6755399441055744.0;  // 1.5 * 2^52: the sum's low bits are the integer
+  const double big = __builtin_fma(e, 46.16624130844682903, kMagic);
+  const int n = (int)__double_as_longlong(big);
+  const double r = __builtin_fma(big - kMagic, -0.02166084939249829091, e);
+  double p = __builtin_fma(r, 1.0 / 120, 1.0 / 24);
+  p = __builtin_fma(p, r, 1.0 / 6);
+  p = __builtin_fma(p, r, 0.5);
+  p = __builtin_fma(p, r, 1.0);
+  p = __builtin_fma(p, r, 1.0);
+  p *= pow[n & 31];
+  const long long bits = __double_as_longlong(p) + ((long long)((n >> 5) << 20) << 32);
+  return e >= kExpFloor ? __longlong_as_double(bits) : 0.0;
+}
+
+// What the weights of a row go by.
+struct Dist {
   float top;
-  int first;
   double inv, sum;
   bool some, sharp;  // any weight; temperature 0
-  __device__ __forceinline__ double weight(int v) const {
-    const float x = l[v];
-    if (!some || x != x) return 0.0;
-    if (x == top) return 1.0;
-    const double e = ((double)x - (double)top) * inv;
-    return e >= kExpFloor ? exp(e) : 0.0;
-  }
-  // probability in the draw (temperature 0: all on the first)
-  __device__ __forceinline__ double prob(int v) const {
-    if (!some) return 0.0;
-    return sharp ? (v == first ? 1.0 : 0.0) : weight(v) / sum;
+  int first;         // id of the largest (temperature 0 only)
+  __device__ __forceinline__ double weight(float x, const double* pow) const {
+    return x == top ? 1.0 : exp_weight(((double)x - (double)top) * inv, pow);
   }
 };
 
-struct Shared {
-  double sum[kRowThreads];
-  float top[kRowThreads];
-  int id[kRowThreads];
-};
-
-// Thread i's ids are [i n / 256, (i + 1) n / 256).
-__device__ __forceinline__ int part_of(int V, int i) { return (int)((long long)V * i / kRowThreads); }
-
-__device__ Row read_row(const float* l, int V, double tau, Shared& s) {
-  const int tid = threadIdx.x, v0 = part_of(V, tid), v1 = part_of(V, tid + 1);
-  Row r{l, -INFINITY, 0, tau > 0.0 ? 1.0 / tau : 1.0, 0.0, false, tau == 0.0};
-  for (int v = v0; v < v1; ++v)
-    if (l[v] > r.top) {
-      r.top = l[v];
-      r.first = v;
-    }
-  __syncthreads();
-  s.top[tid] = r.top;
-  s.id[tid] = r.first;
-  __syncthreads();
-  for (int i = 0; i < kRowThreads; ++i)  // in the order of the ids
-    if (i == 0 || s.top[i] > r.top) {
-      r.top = s.top[i];
-      r.first = s.id[i];
-    }
-  r.some = r.top > -INFINITY;
-  double sum = 0.0;
-  for (int v = v0; v < v1; ++v) sum += r.weight(v);
-  s.sum[tid] = sum;
-  __syncthreads();
-  for (int i = 0; i < kRowThreads; ++i) r.sum += s.sum[i];
-  return r;
+// Sums over the 16 lanes of a row of lanes, inclusive from its first lane.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_add(double x) {
+  const long long b = __double_as_longlong(x);
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)b, CTRL, ROWS, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROWS, 0xf, false);
+  return x + __longlong_as_double((long long)hi << 32 | (uint32_t)lo);
+}
+__device__ __forceinline__ double row_scan(double x) {
+  x = dpp_add<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  return dpp_add<0x118, 0xf>(x);
+}
+__device__ __forceinline__ double lane_scan(double x) {
+  x = row_scan(x);
+  x = dpp_add<0x142, 0xa>(x);    // row_bcast 15
+  return dpp_add<0x143, 0xc>(x);  // row_bcast 31
+}
+__device__ __forceinline__ double read_lane(double x, int lane) {
+  const long long b = __double_as_longlong(x);
+  return __longlong_as_double((long long)__builtin_amdgcn_readlane((int)(b >> 32), lane) << 32 |
+                              (uint32_t)__builtin_amdgcn_readlane((int)b, lane));
 }
 
-// First id whose running sum of w exceeds u times the sum of all (the last of
-// positive weight when none does); -1 when the sum is 0.
+__device__ __forceinline__ float thread_top(const Quads& q) {
+  float t = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t = fmaxf(t, q.x[k][e]);
+  return t;
+}
+__device__ __forceinline__ float wave_top(float t) {
+  for (int o = 32; o > 0; o >>= 1) t = fmaxf(t, __shfl_xor(t, o));
+  return t;
+}
+
+// Where the running sum of a tile passes a target: a segment of 64 ids (16 lanes of
+// wave `wave`, group k), the sum before it, found by every wave alike.
+struct Spot {
+  int k, wave, lanes;
+  double before;
+};
+
+// A tile's segments: the sums of 16 lanes' groups of four ids, by group, wave and
+// lanes, which is the order of the ids.  w4(k, out) gives the weights of the thread's
+// group k.  All threads; two barriers.  The sums then lie in LDS such that lane i of
+// a wave reads segments i n .. i n + n - 1 (n = a 64th of them) without conflicts.
 template <typename W>
-__device__ int pick(int V, float u, Shared& s, W w) {
-  const int tid = threadIdx.x, v0 = part_of(V, tid), v1 = part_of(V, tid + 1);
-  double sum = 0.0;
-  for (int v = v0; v < v1; ++v) sum += w(v);
-  __syncthreads();
-  s.sum[tid] = sum;
-  __syncthreads();
-  double total = 0.0;
-  for (int i = 0; i < kRowThreads; ++i) total += s.sum[i];
-  if (!(total > 0.0)) return -1;
-  const double target = u < 1.0f ? (double)u * total : INFINITY;  // 1 and beyond: no sum exceeds it
-  double before = 0.0;
-  int at = -1, last = -1;  // the thread whose ids hold the token
-  for (int i = 0; i < kRowThreads; ++i) {
-    if (s.sum[i] > 0.0) last = i;
-    if (before + s.sum[i] > target) {
-      at = i;
-      break;
+__device__ __forceinline__ void fill_segments(RowShared& s, const RowAt& at, int tile, W w4) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = blockDim.x / 16;
+  const int per = kQuads * rows / 64;
+  __syncthreads();  // the segments before are read
+#pragma unroll
+  for (int k = 0; k < kQuads; ++k) {
+    double x = 0.0;
+    if (at.has(tile, k)) {  // uniform
+      double w[4];
+      w4(k, w);
+      x = row_scan((w[0] + w[1]) + (w[2] + w[3]));
     }
-    before += s.sum[i];
-  }
-  if (at < 0) at = last;
-  if (tid == at) {
-    int id = v0;
-    for (int v = v0; v < v1; ++v) {
-      const double x = w(v);
-      if (x > 0.0) id = v;
-      before += x;
-      if (x > 0.0 && before > target) break;
-    }
-    s.id[0] = id;
+    const int seg = k * rows + wave * 4 + (lane >> 4);
+    if ((lane & 15) == 15) s.seg[(seg % per) * 64 + seg / per] = x;
   }
   __syncthreads();
-  return s.id[0];
+}
+// The sum of the tile's segments; pre: that of the lanes before.
+__device__ __forceinline__ double segment_sum(const RowShared& s, double& pre) {
+  const int lane = threadIdx.x & 63, per = kQuads * (blockDim.x / 16) / 64;
+  double x = 0.0;
+  for (int i = 0; i < per; ++i) x += s.seg[i * 64 + lane];
+  const double in = lane_scan(x);
+  pre = in - x;
+  return read_lane(in, 63);
+}
+// First segment whose running sum, from `before` on, exceeds the target; the last of
+// positive sum when none does.
+__device__ __forceinline__ Spot find_segment(const RowShared& s, double before, double target) {
+  const int lane = threadIdx.x & 63, rows = blockDim.x / 16, per = kQuads * rows / 64;
+  double x = 0.0;
+  for (int i = 0; i < per; ++i) x += s.seg[i * 64 + lane];
+  const double in = lane_scan(x);
+  double run = before + __shfl_up(in, 1);
+  if (lane == 0) run = before;
+  int over = -1, last = -1;
+  double run_over = 0.0, run_last = 0.0;
+  for (int i = 0; i < per; ++i) {
+    const double y = s.seg[i * 64 + lane];
+    if (y > 0.0) {
+      last = i;
+      run_last = run;
+      if (over < 0 && run + y > target) {
+        over = i;
+        run_over = run;
+      }
+    }
+    run += y;
+  }
+  const uint64_t has_over = __builtin_amdgcn_ballot_w64(over >= 0), has_last = __builtin_amdgcn_ballot_w64(last >= 0);
+  const int L = has_over ? (int)__builtin_ctzll(has_over) : 63 - (int)__builtin_clzll(has_last | 1ull);
+  const int i = __builtin_amdgcn_readlane(has_over ? over : max(last, 0), L);
+  const int seg = L * per + i;
+  return Spot{seg / rows, (seg % rows) / 4, seg % 4, read_lane(has_over ? run_over : run_last, L)};
+}
+// In the spot's wave: the lane that holds the token returns its id, the others -1.
+template <typename W>
+__device__ __forceinline__ int find_id(const Spot& sp, double target, const RowAt& at, int tile, W w4) {
+  const int lane = threadIdx.x & 63;
+  double w[4];
+  w4(sp.k, w);
+  const double x = (w[0] + w[1]) + (w[2] + w[3]);
+  const double in = row_scan(x);
+  const bool mine = (lane >> 4) == sp.lanes;
+  const uint64_t over = __builtin_amdgcn_ballot_w64(mine && x > 0.0 && sp.before + in > target);
+  const uint64_t some = __builtin_amdgcn_ballot_w64(mine && x > 0.0);
+  const int L = over ? (int)__builtin_ctzll(over) : 63 - (int)__builtin_clzll(some | 1ull);
+  if (lane != L) return -1;
+  double run = sp.before + (in - x);
+  int id = -1;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const bool past = id >= 0 && run > target;
+    if (!past && w[e] > 0.0) id = at.id(tile, sp.k) + e;
+    run += past ? 0.0 : w[e];
+  }
+  return id;
 }
 
-// k_verify_rows: a workgroup a row: the draft is taken or a token is drawn.
-__global__ __launch_bounds__(kRowThreads) void k_verify_rows(VerifyArgs a) {
-  __shared__ Shared s;
-  const int m = blockIdx.x, V = a.V;
+// Group k of the registers, k uniform.
+__device__ __forceinline__ void take_group(const Quads& q, int k, float (&x)[4]) {
+#pragma unroll
+  for (int j = 0; j < kQuads; ++j)
+    if (j == k) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = q.x[j][e];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// k_verify_rows: a workgroup a row: its draft is taken or a token is drawn.  DRAFT:
+// with drafts; ONE: the row fits the registers.
+// ---------------------------------------------------------------------------
+template <bool DRAFT, bool ONE>
+__global__ __launch_bounds__(kMaxThreads) void k_verify_rows(VerifyArgs a) {
+  __shared__ RowShared s;
+  const int m = blockIdx.x, V = a.V, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int nwaves = blockDim.x / 64;
   if (a.cu && (m < a.cu[0] || m >= a.cu[a.n_seq])) return;  // uniform
-  const Row p = read_row(a.logits + (size_t)m * V, V, a.tau, s);
-  const int x = a.draft ? a.draft[m] : -1;
-  const bool real = x >= 0 && x < V;
+  const float* const row = a.logits + (size_t)m * V;
+  const RowAt pa(row, V, RowAt::shift_of(row));
+  const int x = DRAFT ? a.draft[m] : -1;
+  const bool real = x >= 0 && x < V, has_q = DRAFT && real && a.draft_logits;
+  const RowAt qa(has_q ? a.draft_logits + (size_t)m * V : row, V, pa.shift);
+  const int tiles = ONE ? 1 : pa.tiles();
+  Quads P, Q;
+  const double* pow = s.pow;
+  if (tid < 32) s.pow[tid] = kPow[tid];
+
+  // the largest
+  Dist p{-INFINITY, a.tau > 0.0 ? 1.0 / a.tau : 1.0, 0.0, false, a.tau == 0.0, 0};
+  Dist q{-INFINITY, a.draft_tau > 0.0 ? 1.0 / a.draft_tau : 1.0, 0.0, false, a.draft_tau == 0.0, 0};
+  for (int t = 0; t < tiles; ++t) {
+    pa.load(P, t);
+    if (has_q) qa.load(Q, t);
+    p.top = fmaxf(p.top, thread_top(P));
+    if (has_q) q.top = fmaxf(q.top, thread_top(Q));
+  }
+  p.top = wave_top(p.top);
+  if (DRAFT) q.top = wave_top(q.top);
+  if (lane == 0) {
+    s.top[0][wave] = p.top;
+    s.top[1][wave] = q.top;
+  }
+  __syncthreads();
+  for (int i = 0; i < nwaves; ++i) {
+    p.top = fmaxf(p.top, s.top[0][i]);
+    q.top = fmaxf(q.top, s.top[1][i]);
+  }
+  p.some = p.top > -INFINITY;
+  q.some = q.top > -INFINITY;
+
+  // at temperature 0, the first of the largest
+  auto first_id = [&](Dist& d, const RowAt& at, Quads& r) {
+    int id = V;
+    for (int t = 0; t < tiles; ++t) {
+      if (!ONE) at.load(r, t);
+#pragma unroll
+      for (int k = kQuads - 1; k >= 0; --k)
+#pragma unroll
+        for (int e = 3; e >= 0; --e)
+          if (r.x[k][e] == d.top && d.some) id = min(id, at.id(t, k) + e);
+    }
+    for (int o = 32; o > 0; o >>= 1) id = min(id, __shfl_xor(id, o));
+    __syncthreads();
+    if (lane == 0) s.first[wave] = id;
+    __syncthreads();
+    for (int i = 0; i < nwaves; ++i) id = min(id, s.first[i]);
+    d.first = id;
+  };
+  if (p.sharp) first_id(p, pa, P);
+  if (has_q && q.sharp) first_id(q, qa, Q);
+
+  // the sums of the weights
+  auto weights_p = [&](int k, double (&w)[4]) {
+    float v[4];
+    take_group(P, k, v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = p.weight(v[e], pow);
+  };
+  auto thread_sum = [&](const Dist& d, const Quads& r, const RowAt& at, int t) {
+    double w = 0.0;
+#pragma unroll
+    for (int k = 0; k < kQuads; ++k)
+      if (at.has(t, k)) {  // uniform
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w += d.weight(r.x[k][e], pow);
+      }
+    return w;
+  };
   int tok = -1;
-  bool take = false;
-  if (real) {
-    const bool certain = a.draft_logits == nullptr;
-    const Row q = certain ? Row{} : read_row(a.draft_logits + (size_t)m * V, V, a.draft_tau, s);
-    auto q_of = [&](int v) { return certain ? (v == x ? 1.0 : 0.0) : q.prob(v); };
-    take = (double)a.u[2 * m] * q_of(x) < p.prob(x);
-    if (take) tok = x;
-    else if (p.some) tok = pick(V, a.u[2 * m + 1], s, [&](int v) { return fmax(p.prob(v) - q_of(v), 0.0); });
+  bool take = false, mine = tid == 0;  // the thread that writes
+  float logit = -INFINITY;            // the token's
+  if (real && p.some) {
+    double wp = 0.0, wq = 0.0;
+    for (int t = 0; t < tiles; ++t) {
+      if (!ONE) pa.load(P, t);
+      wp += thread_sum(p, P, pa, t);
+      if (has_q && q.some) {
+        if (!ONE) qa.load(Q, t);
+        wq += thread_sum(q, Q, qa, t);
+      }
+    }
+    wp = row_scan(wp);
+    wq = row_scan(wq);
+    if ((lane & 15) == 15) {
+      s.part[0][tid >> 4] = wp;
+      s.part[1][tid >> 4] = wq;
+    }
+    __syncthreads();
+    p.sum = read_lane(lane_scan(lane < nwaves * 4 ? s.part[0][lane] : 0.0), 63);
+    q.sum = read_lane(lane_scan(lane < nwaves * 4 ? s.part[1][lane] : 0.0), 63);
+    const float px = fmaxf(pa.l[x], -INFINITY), qx = fmaxf(qa.l[x], -INFINITY);
+    const double pr = p.sharp ? (x == p.first ? 1.0 : 0.0) : p.weight(px, pow) / p.sum;
+    double qr = 1.0;
+    if (has_q) qr = !q.some ? 0.0 : q.sharp ? (x == q.first ? 1.0 : 0.0) : q.weight(qx, pow) / q.sum;
+    take = (double)a.u[2 * m] * qr < pr;
+    if (take) {
+      tok = x;
+      logit = px;
+    }
   }
-  if (tok < 0 && p.some)
-    tok = p.sharp ? p.first : pick(V, a.draft ? a.u[2 * m + 1] : a.u[m], s, [&](int v) { return p.weight(v); });
-  if (threadIdx.x == 0) {
-    a.tokens[m] = tok;
-    if (a.accepted) a.accepted[m] = take ? 1 : 0;
-    if (a.conf) a.conf[m] = tok >= 0 ? p.weight(tok) / p.sum : 0.0;
+
+  // a token: from max(p - q, 0) where a draft was refused, else from p
+  if (!take && p.some) {
+    const float u = DRAFT ? a.u[2 * m + 1] : (p.sharp ? 0.0f : a.u[m]);
+    const double ip = 1.0 / p.sum, iq = 1.0 / q.sum;  // of the sums above (not read without a draft)
+    auto weights_left = [&](int k, int t, double (&w)[4]) {
+      float v[4], y[4];
+      take_group(P, k, v);
+      if (has_q) take_group(Q, k, y);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int id = pa.id(t, k) + e;
+        const double pv = p.sharp ? (id == p.first ? 1.0 : 0.0) : p.weight(v[e], pow) * ip;
+        double qv = id == x ? 1.0 : 0.0;
+        if (has_q) qv = !q.some ? 0.0 : q.sharp ? (id == q.first ? 1.0 : 0.0) : q.weight(y[e], pow) * iq;
+        w[e] = id >= 0 && id < V ? fmax(pv - qv, 0.0) : 0.0;
+      }
+    };
+    // draws from the weights of all tiles: false when they sum to 0
+    auto draw = [&](auto w4, double& total) {
+      int at = 0;
+      double before = 0.0, pre;
+      if (ONE) {
+        fill_segments(s, pa, 0, [&](int k, double (&w)[4]) { w4(k, 0, w); });
+        total = segment_sum(s, pre);
+      } else {
+        total = 0.0;
+        int last = 0;
+        for (int t = 0; t < tiles; ++t) {
+          pa.load(P, t);
+          if (has_q) qa.load(Q, t);
+          fill_segments(s, pa, t, [&](int k, double (&w)[4]) { w4(k, t, w); });
+          const double sum = segment_sum(s, pre);
+          if (tid == 0) s.tile[t] = sum;
+          total += sum;
+          if (sum > 0.0) last = t;
+        }
+        __syncthreads();
+        const double target = u < 1.0f ? (double)u * total : INFINITY;
+        for (at = 0; at < last && !(before + s.tile[at] > target); ++at) before += s.tile[at];
+      }
+      if (!(total > 0.0)) return false;
+      const double target = u < 1.0f ? (double)u * total : INFINITY;  // 1 and beyond: no sum exceeds it
+      if (!ONE) {
+        pa.load(P, at);
+        if (has_q) qa.load(Q, at);
+        fill_segments(s, pa, at, [&](int k, double (&w)[4]) { w4(k, at, w); });
+      }
+      const Spot sp = find_segment(s, before, target);
+      mine = false;
+      if (wave == sp.wave) {  // wave-uniform
+        tok = find_id(sp, target, pa, at, [&](int k, double (&w)[4]) { w4(k, at, w); });
+        mine = tok >= 0;
+      }
+      return true;
+    };
+    double total;
+    if (DRAFT && real && draw(weights_left, total)) {
+    } else {
+      if (!draw([&](int k, int, double (&w)[4]) { weights_p(k, w); }, total)) total = 1.0;
+      p.sum = total;
+      if (p.sharp) {
+        tok = p.first;
+        mine = tid == 0;
+      }
+    }
+    if (mine) logit = fmaxf(pa.l[tok], -INFINITY);
   }
+  if (!mine) return;
+  a.tokens[m] = tok;
+  if (a.accepted) a.accepted[m] = take ? 1 : 0;
+  if (a.conf) a.conf[m] = tok >= 0 ? p.weight(logit, pow) / p.sum : 0.0;
 }
 
 // k_verify_join: a wave a request: the drafts taken, and in a chain the rows after
@@ -179,7 +490,13 @@ __global__ __launch_bounds__(64) void k_verify_join(VerifyArgs a) {
 nmdlm_status launch_verify(const VerifyCall& c, hipStream_t st) {
   const VerifyArgs a{c.logits, c.draft_logits, c.draft, c.u, c.cu, c.M, c.V, c.n_seq, c.tau, c.draft_tau,
                      c.tokens, c.accepted, c.n_accepted, c.conf, !c.each};
-  hipLaunchKernelGGL(k_verify_rows, dim3((unsigned)c.M), dim3(kRowThreads), 0, st, a);
+  // the fewest threads whose registers hold the row, with up to 3 ids before it
+  int threads = 256;
+  while (threads < kMaxThreads && threads * kQuads * 4 < c.V + 3) threads *= 2;
+  const bool one = threads * kQuads * 4 >= c.V + 3;
+  const auto fn = c.draft ? (one ? k_verify_rows<true, true> : k_verify_rows<true, false>)
+                          : (one ? k_verify_rows<false, true> : k_verify_rows<false, false>);
+  hipLaunchKernelGGL(fn, dim3((unsigned)c.M), dim3(threads), 0, st, a);
   const nmdlm_status rc = hip_status();
   if (rc != NMDLM_OK || !c.draft || (c.each && !c.n_accepted)) return rc;
   hipLaunchKernelGGL(k_verify_join, dim3((unsigned)c.n_seq), dim3(64), 0, st, a);

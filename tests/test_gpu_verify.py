@@ -203,6 +203,32 @@ def test_verify_optional_outputs(counts, conf, chain):
           O.draft_verify(l, ql, draft, u, 0.8, 0.8, cu, chain))
 
 
+@pytest.mark.parametrize("off, qoff", [(0, 1), (1, 0), (2, 3), (3, 3)])
+@pytest.mark.parametrize("V", [64, 1001, 33001])
+def test_verify_logits_at_any_address(V, off, qoff):
+    """Rows that begin at any float, the target's and the draft's at different ones."""
+    torch, B = need_gpu()
+    l, ql, draft, u, cu = make(14, [3, 4], V, spare=(0, 0))
+    M = len(l)
+
+    def put(a, o):
+        t = torch.full((a.size + 8,), float("nan"), device="cuda")
+        t[o:o + a.size] = torch.from_numpy(a.ravel()).cuda()
+        return t[o:o + a.size].view(a.shape)
+
+    g = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+    tok = torch.zeros(M, dtype=torch.int32, device="cuda")
+    acc = torch.zeros(M, dtype=torch.uint8, device="cuda")
+    B.nmdlm_draft_verify(put(l, off), put(ql, qoff), M, V, g(draft.astype(np.int32)), g(u), 0.8, 0.8, tok, acc,
+                         cu_rows=g(cu.astype(np.int32)), n_seq=2)
+    want = O.draft_verify(l, ql, draft, u, 0.8, 0.8, cu, True)
+    assert_same(tok.cpu().numpy(), want[0], "tokens")
+    assert_same(acc.cpu().numpy(), want[1], "accepted")
+    one = torch.zeros(M, dtype=torch.int32, device="cuda")
+    B.nmdlm_token_sample(put(l, off), M, V, 0.8, g(u[:, 0]), one)
+    assert_same(one.cpu().numpy(), O.token_sample(l, 0.8, u[:, 0])[0], "drawn")
+
+
 def test_verified_tokens_follow_the_target():
     """Over many pairs of numbers a token comes as often as the target says,
     whatever the draft: counts within 6 standard deviations."""
