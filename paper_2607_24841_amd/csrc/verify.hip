@@ -1,6 +1,9 @@
 // Tokens drawn from logits and verification of drafted tokens: weights in
 // float64, running sums in the order of the ids (the definitions: nmdlm.h).
+#include <float.h>
 #include <math.h>
+
+#include <type_traits>
 
 #include "masked.h"
 
@@ -102,33 +105,56 @@ struct RowAt {
   }
 };
 
-// exp(e) for -700 <= e <= 0, else 0 (NaN too), relative error below 2^-48: with n =
-// round(32 e / ln 2), exp(e) = 2^(n / 32) exp(r), r = e - n ln 2 / 32, |r| <= 0.0109, the
-// powers from a table of 32 and exp(r) by its series to r^5 (r^6 / 720 < 2.4e-15).  The
-// table fills each LDS bank once, so its reads do not conflict.
-__device__ __forceinline__ double exp_weight(double e, const double* pow) {
-  constexpr double kMagic = 6755399441055744.0;  // 1.5 * 2^52: the sum's low bits are the integer
-  const double big = __builtin_fma(e, 46.16624130844682903, kMagic);
-  const int n = (int)__double_as_longlong(big);
-  const double r = __builtin_fma(big - kMagic, -0.02166084939249829091, e);
-  double p = __builtin_fma(r, 1.0 / 120, 1.0 / 24);
-  p = __builtin_fma(p, r, 1.0 / 6);
-  p = __builtin_fma(p, r, 0.5);
-  p = __builtin_fma(p, r, 1.0);
-  p = __builtin_fma(p, r, 1.0);
-  p *= pow[n & 31];
-  const long long bits = __double_as_longlong(p) + ((long long)((n >> 5) << 20) << 32);
-  return e >= kExpFloor ? __longlong_as_double(bits) : 0.0;
-}
-
-// What the weights of a row go by.
+// The weights of a row.  exp(e), e = (x - top) / tau in [-700, 0], with t = 32 e / ln 2, n =
+// round(t) and r = t - n: 2^(n/32) from a table of 32 powers, whose entries fill each
+// LDS bank once (no conflicts), times exp(r ln 2 / 32) by the polynomial of degree 4
+// that meets it at the five Chebyshev points of [-1/2, 1/2] (0 is one: exp(0) is 1).  Its
+// relative error, 7.9e-14, is 2^-43: a running sum errs by less than what decides
+// between two ids in one draw of 10^9.  Float64 runs at the rate of float32 here, so
+// it is the instructions that count, 17 a weight.
 struct Dist {
-  float top;
-  double inv, sum;
-  bool some, sharp;  // any weight; temperature 0
-  int first;         // id of the largest (temperature 0 only)
+  float top, cut;    // the largest; below cut an exponent may be below -700
+  double inv, scale;  // 1 / tau; 32 / (tau ln 2)
+  double sum;
+  bool some, sharp, lift;  // any weight; temperature 0; the largest is +inf
+  int first;               // id of the largest (temperature 0 only)
+  __device__ __forceinline__ void init(double tau) {
+    sharp = tau == 0.0;
+    inv = sharp ? 1.0 : fmin(1.0 / tau, 1e300);  // finite, so that 0 * inv is 0
+    scale = inv * 46.16624130844683;
+    top = -INFINITY;
+    sum = 0.0;
+    first = 0;
+  }
+  // top is known: with a largest of +inf these logits count as 0, the others as -inf
+  __device__ __forceinline__ void set_top() {
+    some = top > -INFINITY;
+    lift = top == INFINITY;
+    if (lift) top = 0.0f;
+    cut = fmaxf((float)((double)top - 690.0 / inv), -FLT_MAX);
+  }
+  __device__ __forceinline__ float lifted(float x) const { return x == INFINITY ? 0.0f : -INFINITY; }
+  // CLEAN: none below cut
+  template <bool CLEAN>
   __device__ __forceinline__ double weight(float x, const double* pow) const {
-    return x == top ? 1.0 : exp_weight(((double)x - (double)top) * inv, pow);
+    constexpr double kMagic = 6755399441055744.0;  // 1.5 * 2^52: the sum's low bits are the integer
+    const double y = (double)x - (double)top;
+    const double big = __builtin_fma(y, scale, kMagic);
+    const int n = (int)__double_as_longlong(big);
+    const double r = __builtin_fma(y, scale, kMagic - big);
+    double p = __builtin_fma(r, 0x1.3b2b1bee88b09p-27, 0x1.c6b167e571135p-20);
+    p = __builtin_fma(p, r, 0x1.ebfbdff8131c3p-13);
+    p = __builtin_fma(p, r, 0x1.62e42fef6d01ap-6);
+    p = __builtin_fma(p, r, 1.0);
+    p *= pow[n & 31];
+    const long long b = __double_as_longlong(p);
+    const double w = __longlong_as_double((long long)((int)(b >> 32) + ((n & ~31) << 15)) << 32 | (uint32_t)b);
+    return CLEAN || y * inv >= kExpFloor ? w : 0.0;
+  }
+  template <bool CLEAN>
+  __device__ __forceinline__ void weights(const float (&x)[4], double (&w)[4], const double* pow) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = weight<CLEAN>(x[e], pow);
   }
 };
 
@@ -165,6 +191,29 @@ __device__ __forceinline__ float thread_top(const Quads& q) {
     for (int e = 0; e < 4; ++e) t = fmaxf(t, q.x[k][e]);
   return t;
 }
+// none of the wave's logits is below the cut
+__device__ __forceinline__ bool wave_clean(const Quads& q, float cut) {
+  float t = INFINITY;
+#pragma unroll
+  for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t = fminf(t, q.x[k][e]);
+  return __builtin_amdgcn_ballot_w64(t >= cut) == ~0ull;
+}
+__device__ __forceinline__ void lift_all(Quads& q, const Dist& d) {
+#pragma unroll
+  for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q.x[k][e] = d.lifted(q.x[k][e]);
+}
+// Keeps the compiler from carrying what it made of the logits in one pass into the next:
+// the weights of a row would take 128 registers.
+__device__ __forceinline__ void renew(Quads& q) {
+#pragma unroll
+  for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) asm("" : "+v"(q.x[k][e]));
+}
 __device__ __forceinline__ float wave_top(float t) {
   for (int o = 32; o > 0; o >>= 1) t = fmaxf(t, __shfl_xor(t, o));
   return t;
@@ -193,6 +242,7 @@ __device__ __forceinline__ void fill_segments(RowShared& s, const RowAt& at, int
       double w[4];
       w4(k, w);
       x = row_scan((w[0] + w[1]) + (w[2] + w[3]));
+      __builtin_amdgcn_sched_barrier(0);
     }
     const int seg = k * rows + wave * 4 + (lane >> 4);
     if ((lane & 15) == 15) s.seg[(seg % per) * 64 + seg / per] = x;
@@ -271,6 +321,11 @@ __device__ __forceinline__ void take_group(const Quads& q, int k, float (&x)[4])
     }
 }
 
+__device__ __forceinline__ double weight_at(const Dist& d, const RowAt& at, int id, const double* pow) {
+  const float x = fmaxf(at.l[id], -INFINITY);
+  return d.weight<false>(d.lift ? d.lifted(x) : x, pow);
+}
+
 // ---------------------------------------------------------------------------
 // k_verify_rows: a workgroup a row: its draft is taken or a token is drawn.  DRAFT:
 // with drafts; ONE: the row fits the registers.
@@ -287,13 +342,14 @@ __global__ __launch_bounds__(kMaxThreads) void k_verify_rows(VerifyArgs a) {
   const bool real = x >= 0 && x < V, has_q = DRAFT && real && a.draft_logits;
   const RowAt qa(has_q ? a.draft_logits + (size_t)m * V : row, V, pa.shift);
   const int tiles = ONE ? 1 : pa.tiles();
-  Quads P, Q;
+  Quads P, Q = {};
   const double* pow = s.pow;
   if (tid < 32) s.pow[tid] = kPow[tid];
 
   // the largest
-  Dist p{-INFINITY, a.tau > 0.0 ? 1.0 / a.tau : 1.0, 0.0, false, a.tau == 0.0, 0};
-  Dist q{-INFINITY, a.draft_tau > 0.0 ? 1.0 / a.draft_tau : 1.0, 0.0, false, a.draft_tau == 0.0, 0};
+  Dist p, q;
+  p.init(a.tau);
+  q.init(a.draft_tau);
   for (int t = 0; t < tiles; ++t) {
     pa.load(P, t);
     if (has_q) qa.load(Q, t);
@@ -311,19 +367,38 @@ __global__ __launch_bounds__(kMaxThreads) void k_verify_rows(VerifyArgs a) {
     p.top = fmaxf(p.top, s.top[0][i]);
     q.top = fmaxf(q.top, s.top[1][i]);
   }
-  p.some = p.top > -INFINITY;
-  q.some = q.top > -INFINITY;
+  p.set_top();
+  q.set_top();
+  // a tile of the row (and its draft's) into registers; with ONE it is there
+  bool clean_p = false, clean_q = false;  // of the wave
+  auto lift_tile = [&]() __attribute__((always_inline)) {
+    if (p.lift) lift_all(P, p);
+    if (has_q && q.lift) lift_all(Q, q);
+    clean_p = wave_clean(P, p.cut);
+    if (has_q) clean_q = wave_clean(Q, q.cut);
+  };
+  auto tile = [&](int t) __attribute__((always_inline)) {
+    if (ONE) {
+      renew(P);
+      if (DRAFT) renew(Q);
+      return;
+    }
+    pa.load(P, t);
+    if (has_q) qa.load(Q, t);
+    lift_tile();
+  };
+  if (ONE) lift_tile();
 
   // at temperature 0, the first of the largest
-  auto first_id = [&](Dist& d, const RowAt& at, Quads& r) {
+  auto first_id = [&](Dist& d, const Quads& r) __attribute__((always_inline)) {
     int id = V;
     for (int t = 0; t < tiles; ++t) {
-      if (!ONE) at.load(r, t);
+      tile(t);
 #pragma unroll
-      for (int k = kQuads - 1; k >= 0; --k)
+      for (int k = 0; k < kQuads; ++k)
 #pragma unroll
-        for (int e = 3; e >= 0; --e)
-          if (r.x[k][e] == d.top && d.some) id = min(id, at.id(t, k) + e);
+        for (int e = 0; e < 4; ++e)
+          if (r.x[k][e] == d.top && d.some) id = min(id, pa.id(t, k) + e);
     }
     for (int o = 32; o > 0; o >>= 1) id = min(id, __shfl_xor(id, o));
     __syncthreads();
@@ -332,38 +407,33 @@ __global__ __launch_bounds__(kMaxThreads) void k_verify_rows(VerifyArgs a) {
     for (int i = 0; i < nwaves; ++i) id = min(id, s.first[i]);
     d.first = id;
   };
-  if (p.sharp) first_id(p, pa, P);
-  if (has_q && q.sharp) first_id(q, qa, Q);
+  if (p.sharp) first_id(p, P);
+  if (has_q && q.sharp) first_id(q, Q);
 
   // the sums of the weights
-  auto weights_p = [&](int k, double (&w)[4]) {
-    float v[4];
-    take_group(P, k, v);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = p.weight(v[e], pow);
-  };
-  auto thread_sum = [&](const Dist& d, const Quads& r, const RowAt& at, int t) {
-    double w = 0.0;
+  auto thread_sum = [&](auto clean, const Dist& d, const Quads& r, int t) __attribute__((always_inline)) {
+    double sum = 0.0;
 #pragma unroll
     for (int k = 0; k < kQuads; ++k)
-      if (at.has(t, k)) {  // uniform
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w += d.weight(r.x[k][e], pow);
+      if (pa.has(t, k)) {  // uniform
+        double w[4];
+        d.template weights<decltype(clean)::value>(r.x[k], w, pow);
+        sum += (w[0] + w[1]) + (w[2] + w[3]);
+        __builtin_amdgcn_sched_barrier(0);  // four chains at a time: more would spill the rows
       }
-    return w;
+    return sum;
+  };
+  auto tile_sum = [&](bool clean, const Dist& d, const Quads& r, int t) __attribute__((always_inline)) {
+    return clean ? thread_sum(std::true_type{}, d, r, t) : thread_sum(std::false_type{}, d, r, t);
   };
   int tok = -1;
   bool take = false, mine = tid == 0;  // the thread that writes
-  float logit = -INFINITY;            // the token's
   if (real && p.some) {
     double wp = 0.0, wq = 0.0;
     for (int t = 0; t < tiles; ++t) {
-      if (!ONE) pa.load(P, t);
-      wp += thread_sum(p, P, pa, t);
-      if (has_q && q.some) {
-        if (!ONE) qa.load(Q, t);
-        wq += thread_sum(q, Q, qa, t);
-      }
+      tile(t);
+      wp += tile_sum(clean_p, p, P, t);
+      if (has_q && q.some) wq += tile_sum(clean_q, q, Q, t);
     }
     wp = row_scan(wp);
     wq = row_scan(wq);
@@ -374,48 +444,30 @@ __global__ __launch_bounds__(kMaxThreads) void k_verify_rows(VerifyArgs a) {
     __syncthreads();
     p.sum = read_lane(lane_scan(lane < nwaves * 4 ? s.part[0][lane] : 0.0), 63);
     q.sum = read_lane(lane_scan(lane < nwaves * 4 ? s.part[1][lane] : 0.0), 63);
-    const float px = fmaxf(pa.l[x], -INFINITY), qx = fmaxf(qa.l[x], -INFINITY);
-    const double pr = p.sharp ? (x == p.first ? 1.0 : 0.0) : p.weight(px, pow) / p.sum;
+    const double pr = p.sharp ? (x == p.first ? 1.0 : 0.0) : weight_at(p, pa, x, pow) / p.sum;
     double qr = 1.0;
-    if (has_q) qr = !q.some ? 0.0 : q.sharp ? (x == q.first ? 1.0 : 0.0) : q.weight(qx, pow) / q.sum;
+    if (has_q) qr = !q.some ? 0.0 : q.sharp ? (x == q.first ? 1.0 : 0.0) : weight_at(q, qa, x, pow) / q.sum;
     take = (double)a.u[2 * m] * qr < pr;
-    if (take) {
-      tok = x;
-      logit = px;
-    }
+    if (take) tok = x;
   }
 
   // a token: from max(p - q, 0) where a draft was refused, else from p
   if (!take && p.some) {
     const float u = DRAFT ? a.u[2 * m + 1] : (p.sharp ? 0.0f : a.u[m]);
-    const double ip = 1.0 / p.sum, iq = 1.0 / q.sum;  // of the sums above (not read without a draft)
-    auto weights_left = [&](int k, int t, double (&w)[4]) {
-      float v[4], y[4];
-      take_group(P, k, v);
-      if (has_q) take_group(Q, k, y);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int id = pa.id(t, k) + e;
-        const double pv = p.sharp ? (id == p.first ? 1.0 : 0.0) : p.weight(v[e], pow) * ip;
-        double qv = id == x ? 1.0 : 0.0;
-        if (has_q) qv = !q.some ? 0.0 : q.sharp ? (id == q.first ? 1.0 : 0.0) : q.weight(y[e], pow) * iq;
-        w[e] = id >= 0 && id < V ? fmax(pv - qv, 0.0) : 0.0;
-      }
-    };
-    // draws from the weights of all tiles: false when they sum to 0
-    auto draw = [&](auto w4, double& total) {
+    // draws from the weights w4(k, tile, out) of all tiles: false when they sum to 0
+    auto draw = [&](auto w4, double& total) __attribute__((always_inline)) {
       int at = 0;
       double before = 0.0, pre;
       if (ONE) {
-        fill_segments(s, pa, 0, [&](int k, double (&w)[4]) { w4(k, 0, w); });
+        tile(0);
+        fill_segments(s, pa, 0, [&](int k, double (&w)[4]) __attribute__((always_inline)) { w4(k, 0, w); });
         total = segment_sum(s, pre);
       } else {
         total = 0.0;
         int last = 0;
         for (int t = 0; t < tiles; ++t) {
-          pa.load(P, t);
-          if (has_q) qa.load(Q, t);
-          fill_segments(s, pa, t, [&](int k, double (&w)[4]) { w4(k, t, w); });
+          tile(t);
+          fill_segments(s, pa, t, [&](int k, double (&w)[4]) __attribute__((always_inline)) { w4(k, t, w); });
           const double sum = segment_sum(s, pre);
           if (tid == 0) s.tile[t] = sum;
           total += sum;
@@ -428,34 +480,68 @@ __global__ __launch_bounds__(kMaxThreads) void k_verify_rows(VerifyArgs a) {
       if (!(total > 0.0)) return false;
       const double target = u < 1.0f ? (double)u * total : INFINITY;  // 1 and beyond: no sum exceeds it
       if (!ONE) {
-        pa.load(P, at);
-        if (has_q) qa.load(Q, at);
-        fill_segments(s, pa, at, [&](int k, double (&w)[4]) { w4(k, at, w); });
+        tile(at);
+        fill_segments(s, pa, at, [&](int k, double (&w)[4]) __attribute__((always_inline)) { w4(k, at, w); });
       }
       const Spot sp = find_segment(s, before, target);
       mine = false;
       if (wave == sp.wave) {  // wave-uniform
-        tok = find_id(sp, target, pa, at, [&](int k, double (&w)[4]) { w4(k, at, w); });
+        if (ONE) tile(0);
+        tok = find_id(sp, target, pa, at, [&](int k, double (&w)[4]) __attribute__((always_inline)) { w4(k, at, w); });
         mine = tok >= 0;
       }
       return true;
     };
     double total;
-    if (DRAFT && real && draw(weights_left, total)) {
-    } else {
-      if (!draw([&](int k, int, double (&w)[4]) { weights_p(k, w); }, total)) total = 1.0;
-      p.sum = total;
+    bool drawn = false;
+    if constexpr (DRAFT) {
+      if (real) {
+        const double ip = 1.0 / p.sum, iq = 1.0 / q.sum;
+        drawn = draw([&](int k, int t, double (&w)[4]) __attribute__((always_inline)) {
+          float v[4];
+          double y[4] = {};
+          const int id = pa.id(t, k);
+          take_group(P, k, v);
+          if (p.sharp) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = id + e == p.first ? 1.0 : 0.0;
+          } else {
+            p.template weights<false>(v, w, pow);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] *= ip;
+          }
+          if (!has_q || (q.some && q.sharp)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = id + e == (has_q ? q.first : x) ? 1.0 : 0.0;
+          } else if (q.some) {
+            take_group(Q, k, v);
+            q.template weights<false>(v, y, pow);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] *= iq;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = fmax(w[e] - y[e], 0.0);
+        }, total);
+      }
+    }
+    if (!drawn) {
+      auto from_p = [&](auto clean, int k, double (&w)[4]) __attribute__((always_inline)) {
+        float v[4];
+        take_group(P, k, v);
+        p.template weights<decltype(clean)::value>(v, w, pow);
+      };
+      draw([&](int k, int, double (&w)[4]) __attribute__((always_inline)) { clean_p ? from_p(std::true_type{}, k, w) : from_p(std::false_type{}, k, w); },
+           p.sum);
       if (p.sharp) {
         tok = p.first;
         mine = tid == 0;
       }
     }
-    if (mine) logit = fmaxf(pa.l[tok], -INFINITY);
   }
   if (!mine) return;
   a.tokens[m] = tok;
   if (a.accepted) a.accepted[m] = take ? 1 : 0;
-  if (a.conf) a.conf[m] = tok >= 0 ? p.weight(logit, pow) / p.sum : 0.0;
+  if (a.conf) a.conf[m] = tok >= 0 ? weight_at(p, pa, tok, pow) / p.sum : 0.0;
 }
 
 // k_verify_join: a wave a request: the drafts taken, and in a chain the rows after
