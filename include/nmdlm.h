@@ -752,16 +752,21 @@ size_t nmdlm_bbm_attn_masked_workspace_size(int T, int M, int n_keys, int H, int
  * weights, as the block step has it.  A row of -inf and NaN alone: token -1,
  * conf 0.
  *
- *   logits  device float [M][V], 1 <= V <= NMDLM_MAX_SAMPLE_V
+ *   logits  device float [M][V]
  *   u       device float [M] in [0, 1) (not read at tau = 0; may then be NULL)
  *   tokens  device int32 [M]
  *   conf    device double [M] or NULL
- * Errors: NMDLM_ERR_INVALID_ARG for a missing or misaligned pointer, a size below
+ *   ws      workspace of nmdlm_token_sample_workspace_size() bytes (any content)
+ * Limits: M <= NMDLM_MAX_SAMPLE_M, V <= NMDLM_MAX_SAMPLE_V, else
+ * NMDLM_ERR_UNSUPPORTED.  Errors: NMDLM_ERR_INVALID_ARG for a missing or misaligned pointer, a size below
  * 1, a temperature that is negative, infinite or NaN.
  * ------------------------------------------------------------------------ */
 #define NMDLM_MAX_SAMPLE_V 16777216
+#define NMDLM_MAX_SAMPLE_M 65535
 nmdlm_status nmdlm_token_sample(const float* logits, int M, int V, double temperature,
-                                const float* u, int32_t* tokens, double* conf, void* stream);
+                                const float* u, int32_t* tokens, double* conf, void* ws,
+                                size_t ws_bytes, void* stream);
+size_t nmdlm_token_sample_workspace_size(int M, int V);
 
 /* ------------------------------------------------------------------------
  * nmdlm_draft_verify — which drafted tokens stand, and what replaces the first
@@ -794,7 +799,8 @@ nmdlm_status nmdlm_token_sample(const float* logits, int M, int V, double temper
  *   conf          device double [M] or NULL: the target's probability of the
  *                 token, as in nmdlm_token_sample
  *   flags         0 or NMDLM_VERIFY_EACH
- * Errors: as nmdlm_token_sample; NMDLM_ERR_INVALID_ARG for other flags and for
+ *   ws            workspace of nmdlm_draft_verify_workspace_size() bytes (any content)
+ * Limits and errors: as nmdlm_token_sample; n_seq <= NMDLM_MAX_PLAN_ROWS; NMDLM_ERR_INVALID_ARG for other flags and for
  * n_seq other than 1 without cu_rows.
  * ------------------------------------------------------------------------ */
 #define NMDLM_VERIFY_EACH 0x1u
@@ -802,7 +808,9 @@ nmdlm_status nmdlm_draft_verify(const float* logits, const float* draft_logits, 
                                 const int32_t* draft, const float* u, double temperature,
                                 double draft_temperature, const int32_t* cu_rows, int n_seq,
                                 unsigned flags, int32_t* tokens, uint8_t* accepted,
-                                int32_t* n_accepted, double* conf, void* stream);
+                                int32_t* n_accepted, double* conf, void* ws,
+                                size_t ws_bytes, void* stream);
+size_t nmdlm_draft_verify_workspace_size(int M, int V);
 
 /* Clears a workspace region with a fill kernel on the stream (use once on a
  * new workspace). */

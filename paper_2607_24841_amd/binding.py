@@ -41,6 +41,7 @@ NMDLM_MAX_PAGES = 1 << 17   # pages of a request
 NMDLM_MAX_POOL = 1 << 25
 NMDLM_MAX_DIST = 1024     # distance of positions that a bias tells apart
 NMDLM_MAX_SAMPLE_V = 1 << 24
+NMDLM_MAX_SAMPLE_M = 65535
 NMDLM_VERIFY_EACH = 0x1
 NMDLM_NOALLOC_SCRATCH_BYTES = 16 << 20   # static scratch of nmdlm_qbsm_noalloc per GPU
 NMDLM_MAX_THR_DEN = 1 << 24
@@ -66,7 +67,8 @@ EXPORTS = (
     "nmdlm_page_select_workspace_size", "nmdlm_bbm_attn_paged",
     "nmdlm_bbm_attn_paged_workspace_size", "nmdlm_block_step_paged",
     "nmdlm_block_step_paged_workspace_size", "nmdlm_bbm_attn_masked",
-    "nmdlm_bbm_attn_masked_workspace_size", "nmdlm_token_sample", "nmdlm_draft_verify",
+    "nmdlm_bbm_attn_masked_workspace_size", "nmdlm_token_sample",
+    "nmdlm_token_sample_workspace_size", "nmdlm_draft_verify", "nmdlm_draft_verify_workspace_size",
 )
 
 
@@ -198,9 +200,11 @@ def load(path: str = LIB_PATH):
                                           vp, C.POINTER(MaskC), vp, vp, i32, vp, vp, sz, vp]
     lib.nmdlm_bbm_attn_masked_workspace_size.argtypes = [C.c_int] * 5
     lib.nmdlm_bbm_attn_masked_workspace_size.restype = sz
-    lib.nmdlm_token_sample.argtypes = [vp, C.c_int, C.c_int, C.c_double, vp, vp, vp, vp]
+    lib.nmdlm_token_sample.argtypes = [vp, C.c_int, C.c_int, C.c_double, vp, vp, vp, vp, sz, vp]
     lib.nmdlm_draft_verify.argtypes = [vp, vp, C.c_int, C.c_int, vp, vp, C.c_double, C.c_double, vp,
-                                       C.c_int, u, vp, vp, vp, vp, vp]
+                                       C.c_int, u, vp, vp, vp, vp, vp, sz, vp]
+    for fn in (lib.nmdlm_token_sample_workspace_size, lib.nmdlm_draft_verify_workspace_size):
+        fn.argtypes, fn.restype = [C.c_int] * 2, sz
     lib.nmdlm_workspace_clear.argtypes = [vp, sz, vp]
     lib.nmdlm_status_string.argtypes = [C.c_int]
     lib.nmdlm_status_string.restype = C.c_char_p
@@ -576,21 +580,40 @@ def _floats(what: str, *named) -> None:
             raise NmdlmError(NMDLM_ERR_INVALID_ARG, f"{what}: {name} is {t.dtype}, not {dtype}")
 
 
-def nmdlm_token_sample(logits, M, V, temperature, u, tokens, conf=None, stream=None) -> None:
-    what, ix = "nmdlm_token_sample", logits.get_device()
+def _scratch(what: str, ws, nbytes: int, index: int, stream):
+    """The given workspace, or one of torch's allocator for this call."""
+    if ws is None and index >= 0:
+        ws = torch.empty(max(256, nbytes), dtype=torch.uint8, device=torch.device("cuda", index))
+        if stream is not None:
+            ws.record_stream(stream)
+    return ws, _arg(what, "ws", ws, 1, 1, index), 0 if ws is None else ws.numel()
+
+
+def nmdlm_token_sample_workspace_size(M, V) -> int:
+    return load().nmdlm_token_sample_workspace_size(M, V)
+
+
+def nmdlm_token_sample(logits, M, V, temperature, u, tokens, conf=None, ws=None, stream=None) -> None:
+    """ws None: a workspace of torch's allocator for the call."""
+    what, ix, lib = "nmdlm_token_sample", logits.get_device(), load()
     _floats(what, ("logits", logits, torch.float32), ("u", u, torch.float32), ("conf", conf, torch.float64))
     args = (_arg(what, "logits", logits, M * V, 4, ix), M, V, float(temperature),
             _arg(what, "u", u, M, 4, ix), _arg(what, "tokens", tokens, M, 4, ix),
             _arg(what, "conf", conf, M, 8, ix))
-    fn = load().nmdlm_token_sample
-    _on(ix, what, lambda st: fn(*args, st), stream)
+    ws, at, nbytes = _scratch(what, ws, lib.nmdlm_token_sample_workspace_size(M, V), ix, stream)
+    _on(ix, what, lambda st: lib.nmdlm_token_sample(*args, at, nbytes, st), stream)
+
+
+def nmdlm_draft_verify_workspace_size(M, V) -> int:
+    return load().nmdlm_draft_verify_workspace_size(M, V)
 
 
 def nmdlm_draft_verify(logits, draft_logits, M, V, draft, u, temperature, draft_temperature, tokens,
                        accepted, cu_rows=None, n_seq=1, n_accepted=None, conf=None, chain=True,
-                       stream=None) -> None:
-    """chain False: every row counts (NMDLM_VERIFY_EACH)."""
-    what, ix = "nmdlm_draft_verify", logits.get_device()
+                       ws=None, stream=None) -> None:
+    """chain False: every row counts (NMDLM_VERIFY_EACH).  ws None: a workspace of
+    torch's allocator for the call."""
+    what, ix, lib = "nmdlm_draft_verify", logits.get_device(), load()
     _floats(what, ("logits", logits, torch.float32), ("draft_logits", draft_logits, torch.float32),
             ("u", u, torch.float32), ("conf", conf, torch.float64))
     args = (_arg(what, "logits", logits, M * V, 4, ix), _arg(what, "draft_logits", draft_logits, M * V, 4, ix),
@@ -599,8 +622,8 @@ def nmdlm_draft_verify(logits, draft_logits, M, V, draft, u, temperature, draft_
             0 if chain else NMDLM_VERIFY_EACH, _arg(what, "tokens", tokens, M, 4, ix),
             _arg(what, "accepted", accepted, M, 1, ix), _arg(what, "n_accepted", n_accepted, n_seq, 4, ix),
             _arg(what, "conf", conf, M, 8, ix))
-    fn = load().nmdlm_draft_verify
-    _on(ix, what, lambda st: fn(*args, st), stream)
+    ws, at, nbytes = _scratch(what, ws, lib.nmdlm_draft_verify_workspace_size(M, V), ix, stream)
+    _on(ix, what, lambda st: lib.nmdlm_draft_verify(*args, at, nbytes, st), stream)
 
 
 def nmdlm_block_step(model: "DeviceModel", io: StepIO, ws: torch.Tensor, stream=None) -> None:

@@ -140,6 +140,12 @@ nmdlm_status mask_ok(const nmdlm_mask* m, bool bias) {
   return m->max_dist >= 0 && m->max_dist <= NMDLM_MAX_DIST ? NMDLM_OK : NMDLM_ERR_INVALID_ARG;
 }
 
+// rows of logits
+nmdlm_status verify_sizes_ok(int M, int V) {
+  if (M < 1 || V < 1) return NMDLM_ERR_INVALID_ARG;
+  return M <= NMDLM_MAX_SAMPLE_M && V <= NMDLM_MAX_SAMPLE_V ? NMDLM_OK : NMDLM_ERR_UNSUPPORTED;
+}
+
 bool temperature_ok(double t) { return t >= 0.0 && t <= DBL_MAX; }
 
 }  // namespace
@@ -526,25 +532,30 @@ nmdlm_status nmdlm_bbm_attn_masked(const uint64_t* q, const uint64_t* k_cache, c
   return launch_masked_attn(c, static_cast<hipStream_t>(stream));
 }
 
+size_t nmdlm_token_sample_workspace_size(int M, int V) { return verify_sizes_ok(M, V) == NMDLM_OK ? verify_ws(M, V, false) : 0; }
+
 nmdlm_status nmdlm_token_sample(const float* logits, int M, int V, double temperature, const float* u,
-                                int32_t* tokens, double* conf, void* stream) {
-  if (!logits || !tokens || M < 1 || V < 1 || !temperature_ok(temperature) || (temperature > 0.0 && !u))
-    return NMDLM_ERR_INVALID_ARG;
+                                int32_t* tokens, double* conf, void* ws, size_t ws_bytes, void* stream) {
+  if (!logits || !tokens || !temperature_ok(temperature) || (temperature > 0.0 && !u)) return NMDLM_ERR_INVALID_ARG;
   if (!aligned(logits, 4) || !aligned(u, 4) || !aligned(tokens, 4) || !aligned(conf, 8))
     return NMDLM_ERR_INVALID_ARG;
-  if (V > NMDLM_MAX_SAMPLE_V) return NMDLM_ERR_UNSUPPORTED;
+  const nmdlm_status rc = verify_sizes_ok(M, V);
+  if (rc != NMDLM_OK) return rc;
+  if (!ws || !aligned(ws, 256) || ws_bytes < verify_ws(M, V, false)) return NMDLM_ERR_WORKSPACE;
   const VerifyCall c{logits, nullptr, nullptr, u, M, V, temperature, 0.0, nullptr, 1, true, tokens, nullptr,
-                     nullptr, conf};
+                     nullptr, conf, ws};
   return launch_verify(c, static_cast<hipStream_t>(stream));
 }
+
+size_t nmdlm_draft_verify_workspace_size(int M, int V) { return verify_sizes_ok(M, V) == NMDLM_OK ? verify_ws(M, V, true) : 0; }
 
 nmdlm_status nmdlm_draft_verify(const float* logits, const float* draft_logits, int M, int V,
                                 const int32_t* draft, const float* u, double temperature,
                                 double draft_temperature, const int32_t* cu_rows, int n_seq, unsigned flags,
                                 int32_t* tokens, uint8_t* accepted, int32_t* n_accepted, double* conf,
-                                void* stream) {
-  if (!logits || !draft || !u || !tokens || !accepted || M < 1 || V < 1 || n_seq < 1 ||
-      !temperature_ok(temperature) || (flags & ~NMDLM_VERIFY_EACH))
+                                void* ws, size_t ws_bytes, void* stream) {
+  if (!logits || !draft || !u || !tokens || !accepted || n_seq < 1 || !temperature_ok(temperature) ||
+      (flags & ~NMDLM_VERIFY_EACH))
     return NMDLM_ERR_INVALID_ARG;
   if ((draft_logits && !temperature_ok(draft_temperature)) || (!cu_rows && n_seq != 1))
     return NMDLM_ERR_INVALID_ARG;
@@ -552,9 +563,12 @@ nmdlm_status nmdlm_draft_verify(const float* logits, const float* draft_logits, 
                         (const void*)cu_rows, (const void*)tokens, (const void*)n_accepted})
     if (!aligned(p, 4)) return NMDLM_ERR_INVALID_ARG;
   if (!aligned(conf, 8)) return NMDLM_ERR_INVALID_ARG;
-  if (V > NMDLM_MAX_SAMPLE_V) return NMDLM_ERR_UNSUPPORTED;
+  const nmdlm_status rc = verify_sizes_ok(M, V);
+  if (rc != NMDLM_OK) return rc;
+  if (n_seq > NMDLM_MAX_PLAN_ROWS) return NMDLM_ERR_UNSUPPORTED;
+  if (!ws || !aligned(ws, 256) || ws_bytes < verify_ws(M, V, true)) return NMDLM_ERR_WORKSPACE;
   const VerifyCall c{logits, draft_logits, draft, u, M, V, temperature, draft_temperature, cu_rows, n_seq,
-                     (flags & NMDLM_VERIFY_EACH) != 0, tokens, accepted, n_accepted, conf};
+                     (flags & NMDLM_VERIFY_EACH) != 0, tokens, accepted, n_accepted, conf, ws};
   return launch_verify(c, static_cast<hipStream_t>(stream));
 }
 

@@ -43,7 +43,9 @@ struct VerifyCall {
   uint8_t* accepted;
   int32_t* n_accepted;
   double* conf;
+  void* ws;
 };
+size_t verify_ws(int M, int V, bool drafts);
 nmdlm_status launch_verify(const VerifyCall& c, hipStream_t st);
 
 }  // namespace nmdlm

@@ -1,13 +1,27 @@
 // Tokens drawn from logits and verification of drafted tokens: weights in
 // float64, running sums in the order of the ids (the definitions: nmdlm.h).
+//
+// A row's ids go in parts of kPartIds, a wave each, so that one row fills many CUs
+// and many rows stream through small workgroups without a barrier:
+//   k_logit_parts  the largest logit of a part and the sum of its weights against it,
+//                  of the target's rows and of the draft's: the logits' one full read
+//   k_verify_left  (with drafts) whether a row's draft is taken; where not, the parts'
+//                  sums of max(p - q, 0)
+//   k_draw         the part in which the running sum passes the drawn number, then the
+//                  id in it; and a request's count and end
+// Every sum that decides is made in the same way by all waves that need it.
 #include <float.h>
 #include <math.h>
-
-#include <type_traits>
 
 #include "masked.h"
 
 namespace nmdlm {
+
+struct PartStat {
+  float top;     // -inf: no weight
+  int32_t first; // id of the largest
+  double sum;    // of exp((l - top) / tau)
+};
 
 struct VerifyArgs {
   const float* logits;
@@ -15,27 +29,22 @@ struct VerifyArgs {
   const int32_t* draft;
   const float* u;
   const int32_t* cu;
-  int M, V, n_seq;
+  int M, V, n_seq, parts;
   double tau, draft_tau;
   int32_t* tokens;
   uint8_t* accepted;
   int32_t* n_accepted;
   double* conf;
+  PartStat* p_stat;  // [M][parts]
+  PartStat* q_stat;
+  double* left;      // [M][parts]
   bool chain;
 };
 
-// ---------------------------------------------------------------------------
-// A workgroup takes a row (of the target, and of the draft): a thread holds
-// kQuads groups of four consecutive logits in registers, group k of thread i being
-// ids 4 (k nth + i) on, less the row's offset from a 16-byte address, so that a
-// wave reads 1 KB runs.  Up to kQuads * 4 * 1024 ids the row is read once; longer rows go
-// in tiles of that size and are read again for each step.
-// ---------------------------------------------------------------------------
-constexpr int kQuads = 8;
-constexpr int kMaxThreads = 1024;
-constexpr int kSegs = kQuads * kMaxThreads / 16;  // of 64 ids: the sums of 16 lanes
-constexpr int kMaxTiles = NMDLM_MAX_SAMPLE_V / (kQuads * 4 * kMaxThreads) + 1;
-constexpr double kExpFloor = -700.0;  // exponents below weigh nothing
+constexpr int kQuads = 4;                   // groups of four consecutive ids of a lane
+constexpr int kPartIds = 64 * 4 * kQuads;
+constexpr int kPartWaves = 4;               // of a workgroup
+constexpr double kExpFloor = -700.0;        // exponents below weigh nothing
 
 // 2^(j/32), correctly rounded
 __device__ const double kPow[32] = {
@@ -48,62 +57,62 @@ __device__ const double kPow[32] = {
     0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0,
     0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0,
 };
+__device__ __forceinline__ void fill_pow(double* pow) {
+  if (threadIdx.x < 32) pow[threadIdx.x] = kPow[threadIdx.x];
+}
 
-struct Quads {
-  float x[kQuads][4];
-};
-
-struct RowShared {
-  double seg[kSegs];
-  double tile[kMaxTiles];
-  double part[2][kMaxThreads / 16];
-  double pow[32];  // 2^(j/32)
-  float top[2][kMaxThreads / 64];
-  int first[kMaxThreads / 64];
-};
-
-// A row and where a thread's groups of it lie: the target's from the 16-byte address
-// at or before the row on, the draft's the same ids.
+// A row and where a lane's ids of it lie: group k of lane i of part w begins at id 1024 w +
+// 4 (64 k + i) - shift, the target's groups 16-byte aligned; a wave reads runs of 1 KB.
 struct RowAt {
   const float* l;
-  int V, shift;  // ids before the row's first
-  bool vec;      // the groups are 16-byte aligned
+  int V, shift;
+  bool vec;  // the groups are aligned
   __device__ __forceinline__ static int shift_of(const float* row) {
     return (int)((reinterpret_cast<uintptr_t>(row) >> 2) & 3);
   }
   __device__ __forceinline__ RowAt(const float* row, int V_, int shift_)
       : l(row), V(V_), shift(shift_), vec(shift_of(row) == shift_) {}
-  __device__ __forceinline__ int tile_ids() const { return kQuads * 4 * blockDim.x; }
-  __device__ __forceinline__ int tiles() const { return (V + shift + tile_ids() - 1) / tile_ids(); }
-  __device__ __forceinline__ int id(int tile, int k) const {
-    return tile * tile_ids() + 4 * (int)(k * blockDim.x + threadIdx.x) - shift;
-  }
-  // any id of the workgroup in group k
-  __device__ __forceinline__ bool has(int tile, int k) const {
-    return tile * tile_ids() + 4 * (int)(k * blockDim.x) - shift < V;
+  __device__ __forceinline__ int id(int part, int k) const {
+    return part * kPartIds + 4 * (64 * k + (int)(threadIdx.x & 63)) - shift;
   }
   // NaN and ids outside the row become -inf
-  __device__ __forceinline__ void load(Quads& q, int tile) const {
+  __device__ __forceinline__ void load(float (&x)[kQuads][4], int part) const {
+    if (vec && part * kPartIds >= shift && (part + 1) * kPartIds - shift <= V) {  // uniform
 #pragma unroll
-    for (int k = 0; k < kQuads; ++k) {
-      const int v = id(tile, k);
-      if (vec && v >= 0 && v + 3 < V) {
-        const float4 f = *reinterpret_cast<const float4*>(l + v);
-        q.x[k][0] = f.x;
-        q.x[k][1] = f.y;
-        q.x[k][2] = f.z;
-        q.x[k][3] = f.w;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) q.x[k][e] = v + e >= 0 && v + e < V ? l[v + e] : -INFINITY;
+      for (int k = 0; k < kQuads; ++k) {
+        const float4 f = *reinterpret_cast<const float4*>(l + id(part, k));
+        x[k][0] = f.x;
+        x[k][1] = f.y;
+        x[k][2] = f.z;
+        x[k][3] = f.w;
       }
+    } else {
+#pragma unroll
+      for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int v = id(part, k) + e;
+          const float y = l[min(max(v, 0), V - 1)];
+          x[k][e] = v >= 0 && v < V ? y : -INFINITY;
+        }
     }
 #pragma unroll
     for (int k = 0; k < kQuads; ++k)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) q.x[k][e] = fmaxf(q.x[k][e], -INFINITY);
+      for (int e = 0; e < 4; ++e) x[k][e] = fmaxf(x[k][e], -INFINITY);
   }
+  __device__ __forceinline__ float at(int v) const { return fmaxf(l[v], -INFINITY); }
 };
+__device__ __forceinline__ RowAt target_row(const VerifyArgs& a, int m) {
+  const float* l = a.logits + (size_t)m * a.V;
+  return RowAt(l, a.V, RowAt::shift_of(l));
+}
+__device__ __forceinline__ RowAt draft_row(const VerifyArgs& a, int m) {  // at the target's ids
+  return RowAt(a.draft_logits + (size_t)m * a.V, a.V, RowAt::shift_of(a.logits + (size_t)m * a.V));
+}
+__device__ __forceinline__ bool row_counts(const VerifyArgs& a, int m) {
+  return !a.cu || (m >= a.cu[0] && m < a.cu[a.n_seq]);
+}
 
 // The weights of a row.  exp(e), e = (x - top) / tau in [-700, 0], with t = 32 e / ln 2, n =
 // round(t) and r = t - n: 2^(n/32) from a table of 32 powers, whose entries fill each
@@ -113,30 +122,31 @@ struct RowAt {
 // between two ids in one draw of 10^9.  Float64 runs at the rate of float32 here, so
 // it is the instructions that count, 17 a weight.
 struct Dist {
-  float top, cut;    // the largest; below cut an exponent may be below -700
+  float top, cut;     // the largest; below cut an exponent may be below -700
   double inv, scale;  // 1 / tau; 32 / (tau ln 2)
   double sum;
   bool some, sharp, lift;  // any weight; temperature 0; the largest is +inf
-  int first;               // id of the largest (temperature 0 only)
-  __device__ __forceinline__ void init(double tau) {
+  int first;               // id of the largest
+  __device__ __forceinline__ explicit Dist(double tau) {
     sharp = tau == 0.0;
     inv = sharp ? 1.0 : fmin(1.0 / tau, 1e300);  // finite, so that 0 * inv is 0
     scale = inv * 46.16624130844683;
-    top = -INFINITY;
     sum = 0.0;
     first = 0;
+    set_top(-INFINITY);
   }
-  // top is known: with a largest of +inf these logits count as 0, the others as -inf
-  __device__ __forceinline__ void set_top() {
-    some = top > -INFINITY;
-    lift = top == INFINITY;
-    if (lift) top = 0.0f;
+  // with a largest of +inf these logits count as 0, the others as -inf
+  __device__ __forceinline__ void set_top(float t) {
+    some = t > -INFINITY;
+    lift = t == INFINITY;
+    top = lift ? 0.0f : t;
     cut = fmaxf((float)((double)top - 690.0 / inv), -FLT_MAX);
   }
-  __device__ __forceinline__ float lifted(float x) const { return x == INFINITY ? 0.0f : -INFINITY; }
-  // CLEAN: none below cut
-  template <bool CLEAN>
-  __device__ __forceinline__ double weight(float x, const double* pow) const {
+  __device__ __forceinline__ float seen(float x) const {
+    return !lift ? x : x == INFINITY ? 0.0f : -INFINITY;
+  }
+  template <bool CLEAN>  // CLEAN: not below cut
+  __device__ __forceinline__ double weight_of(float x, const double* pow) const {
     constexpr double kMagic = 6755399441055744.0;  // 1.5 * 2^52: the sum's low bits are the integer
     const double y = (double)x - (double)top;
     const double big = __builtin_fma(y, scale, kMagic);
@@ -151,14 +161,37 @@ struct Dist {
     const double w = __longlong_as_double((long long)((int)(b >> 32) + ((n & ~31) << 15)) << 32 | (uint32_t)b);
     return CLEAN || y * inv >= kExpFloor ? w : 0.0;
   }
-  template <bool CLEAN>
-  __device__ __forceinline__ void weights(const float (&x)[4], double (&w)[4], const double* pow) const {
+  __device__ __forceinline__ double weight(float x, const double* pow) const {
+    return weight_of<false>(seen(x), pow);
+  }
+  // the weights of a lane's ids
+  __device__ __forceinline__ void weights(float (&x)[kQuads][4], double (&w)[kQuads][4], const double* pow) const {
+    float least = INFINITY;
+    if (lift) {  // uniform
 #pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = weight<CLEAN>(x[e], pow);
+      for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[k][e] = seen(x[k][e]);
+    }
+#pragma unroll
+    for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) least = fminf(least, x[k][e]);
+    if (__builtin_amdgcn_ballot_w64(least >= cut) == ~0ull) {
+#pragma unroll
+      for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[k][e] = weight_of<true>(x[k][e], pow);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[k][e] = weight_of<false>(x[k][e], pow);
+    }
   }
 };
 
-// Sums over the 16 lanes of a row of lanes, inclusive from its first lane.
+// Sums over the lanes, inclusive from the first.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ double dpp_add(double x) {
   const long long b = __double_as_longlong(x);
@@ -166,15 +199,12 @@ __device__ __forceinline__ double dpp_add(double x) {
   const int hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROWS, 0xf, false);
   return x + __longlong_as_double((long long)hi << 32 | (uint32_t)lo);
 }
-__device__ __forceinline__ double row_scan(double x) {
+__device__ __forceinline__ double lane_scan(double x) {
   x = dpp_add<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8
   x = dpp_add<0x112, 0xf>(x);
   x = dpp_add<0x114, 0xf>(x);
-  return dpp_add<0x118, 0xf>(x);
-}
-__device__ __forceinline__ double lane_scan(double x) {
-  x = row_scan(x);
-  x = dpp_add<0x142, 0xa>(x);    // row_bcast 15
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);     // row_bcast 15
   return dpp_add<0x143, 0xc>(x);  // row_bcast 31
 }
 __device__ __forceinline__ double read_lane(double x, int lane) {
@@ -182,410 +212,355 @@ __device__ __forceinline__ double read_lane(double x, int lane) {
   return __longlong_as_double((long long)__builtin_amdgcn_readlane((int)(b >> 32), lane) << 32 |
                               (uint32_t)__builtin_amdgcn_readlane((int)b, lane));
 }
+__device__ __forceinline__ double wave_total(double x) { return read_lane(lane_scan(x), 63); }
+template <int CTRL>
+__device__ __forceinline__ float dpp_max(float x) {
+  return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(x), __float_as_int(x), CTRL, 0xf, 0xf, false)));
+}
+__device__ __forceinline__ float wave_top(float x) {
+  x = dpp_max<0x111>(x);
+  x = dpp_max<0x112>(x);
+  x = dpp_max<0x114>(x);
+  x = dpp_max<0x118>(x);
+  x = dpp_max<0x142>(x);
+  x = dpp_max<0x143>(x);
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+__device__ __forceinline__ int wave_min(int x) {
+  for (int o = 32; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ double sum4(const double (&w)[4]) { return (w[0] + w[1]) + (w[2] + w[3]); }
 
-__device__ __forceinline__ float thread_top(const Quads& q) {
+// ---------------------------------------------------------------------------
+// k_logit_parts: grid (parts / 4, rows, 1 or 2: the target's and the draft's), a wave a
+// part.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(64 * kPartWaves) void k_logit_parts(VerifyArgs a) {
+  __shared__ double pow[32];
+  const int m = blockIdx.y, lane = threadIdx.x & 63;
+  const int part = blockIdx.x * kPartWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const bool of_draft = blockIdx.z != 0;
+  if (!row_counts(a, m)) return;  // uniform
+  if (of_draft && (uint32_t)a.draft[m] >= (uint32_t)a.V) return;
+  fill_pow(pow);
+  const RowAt row = of_draft ? draft_row(a, m) : target_row(a, m);
+  float x[kQuads][4];
+  if (part < a.parts) row.load(x, part);  // wave-uniform
+  __syncthreads();
+  if (part >= a.parts) return;
   float t = -INFINITY;
 #pragma unroll
   for (int k = 0; k < kQuads; ++k)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) t = fmaxf(t, q.x[k][e]);
-  return t;
-}
-// none of the wave's logits is below the cut
-__device__ __forceinline__ bool wave_clean(const Quads& q, float cut) {
-  float t = INFINITY;
+    for (int e = 0; e < 4; ++e) t = fmaxf(t, x[k][e]);
+  t = wave_top(t);
+  Dist d(of_draft ? a.draft_tau : a.tau);
+  d.set_top(t);
+  int first = a.V;
+  if (d.sharp) {  // uniform
 #pragma unroll
-  for (int k = 0; k < kQuads; ++k)
+    for (int k = 0; k < kQuads; ++k)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) t = fminf(t, q.x[k][e]);
-  return __builtin_amdgcn_ballot_w64(t >= cut) == ~0ull;
-}
-__device__ __forceinline__ void lift_all(Quads& q, const Dist& d) {
+      for (int e = 0; e < 4; ++e)
+        if (x[k][e] == t && d.some) first = min(first, row.id(part, k) + e);
+    first = wave_min(first);
+  }
+  double sum = 0.0;
+  if (d.some) {  // wave-uniform
+    double w[kQuads][4];
+    d.weights(x, w, pow);
 #pragma unroll
-  for (int k = 0; k < kQuads; ++k)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) q.x[k][e] = d.lifted(q.x[k][e]);
-}
-// Keeps the compiler from carrying what it made of the logits in one pass into the next:
-// the weights of a row would take 128 registers.
-__device__ __forceinline__ void renew(Quads& q) {
-#pragma unroll
-  for (int k = 0; k < kQuads; ++k)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) asm("" : "+v"(q.x[k][e]));
-}
-__device__ __forceinline__ float wave_top(float t) {
-  for (int o = 32; o > 0; o >>= 1) t = fmaxf(t, __shfl_xor(t, o));
-  return t;
+    for (int k = 0; k < kQuads; ++k) sum += sum4(w[k]);
+    sum = lane_scan(sum);
+  }
+  if (lane == 63) (of_draft ? a.q_stat : a.p_stat)[(size_t)m * a.parts + part] = PartStat{t, first, sum};
 }
 
-// Where the running sum of a tile passes a target: a segment of 64 ids (16 lanes of
-// wave `wave`, group k), the sum before it, found by every wave alike.
-struct Spot {
-  int k, wave, lanes;
-  double before;
+// The row's distribution from its parts; every lane gets it.
+__device__ __forceinline__ Dist row_dist(const PartStat* st, int parts, double tau, const double* pow) {
+  const int lane = threadIdx.x & 63;
+  Dist d(tau);
+  float top = -INFINITY;
+  for (int i = lane; i < parts; i += 64) top = fmaxf(top, st[i].top);
+  top = wave_top(top);
+  d.set_top(top);
+  double sum = 0.0;
+  int first = INT32_MAX;
+  for (int i = lane; i < parts; i += 64) {
+    const PartStat s = st[i];
+    sum += s.sum * d.weight(s.top, pow);
+    if (s.top == top) first = min(first, s.first);
+  }
+  d.sum = wave_total(sum);
+  if (d.sharp) d.first = wave_min(first);
+  return d;
+}
+
+// The target's and the draft's distribution of a row with a draft x.
+struct Pair {
+  Dist p, q;
+  int x;
+  bool certain;  // q is 1 at x
+  __device__ __forceinline__ Pair(const VerifyArgs& a, int m, int x_, const double* pow)
+      : p(row_dist(a.p_stat + (size_t)m * a.parts, a.parts, a.tau, pow)), q(a.draft_tau), x(x_),
+        certain(!a.draft_logits) {
+    if (!certain) q = row_dist(a.q_stat + (size_t)m * a.parts, a.parts, a.draft_tau, pow);
+  }
+  // max(p - q, 0) of a part's ids
+  __device__ __forceinline__ void left(const VerifyArgs& a, int m, int part, double (&w)[kQuads][4],
+                                       const double* pow) const {
+    const RowAt row = target_row(a, m);
+    float lp[kQuads][4], lq[kQuads][4];
+    row.load(lp, part);
+    if (!certain) draft_row(a, m).load(lq, part);
+    double y[kQuads][4];
+    if (p.sharp) {
+#pragma unroll
+      for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[k][e] = row.id(part, k) + e == p.first ? 1.0 : 0.0;
+    } else {
+      const double ip = 1.0 / p.sum;
+      p.weights(lp, w, pow);
+#pragma unroll
+      for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[k][e] *= ip;
+    }
+    if (certain || q.sharp || !q.some) {
+      const int at = certain ? x : q.some ? q.first : -1 << 30;
+#pragma unroll
+      for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[k][e] = row.id(part, k) + e == at ? 1.0 : 0.0;
+    } else {
+      const double iq = 1.0 / q.sum;
+      q.weights(lq, y, pow);
+#pragma unroll
+      for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[k][e] *= iq;
+    }
+#pragma unroll
+    for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[k][e] = fmax(w[k][e] - y[k][e], 0.0);
+  }
 };
 
-// A tile's segments: the sums of 16 lanes' groups of four ids, by group, wave and
-// lanes, which is the order of the ids.  w4(k, out) gives the weights of the thread's
-// group k.  All threads; two barriers.  The sums then lie in LDS such that lane i of
-// a wave reads segments i n .. i n + n - 1 (n = a 64th of them) without conflicts.
-template <typename W>
-__device__ __forceinline__ void fill_segments(RowShared& s, const RowAt& at, int tile, W w4) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = blockDim.x / 16;
-  const int per = kQuads * rows / 64;
-  __syncthreads();  // the segments before are read
+// ---------------------------------------------------------------------------
+// k_verify_left: grid (parts / 4, rows), a wave a part.  Each decides on its row's draft
+// for itself; part 0 writes what was decided.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(64 * kPartWaves) void k_verify_left(VerifyArgs a) {
+  __shared__ double pow[32];
+  const int m = blockIdx.y, lane = threadIdx.x & 63;
+  const int part = blockIdx.x * kPartWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  if (!row_counts(a, m)) return;  // uniform
+  const int x = a.draft[m];
+  if ((uint32_t)x >= (uint32_t)a.V) {
+    if (part == 0 && lane == 0) a.accepted[m] = 0;
+    return;
+  }
+  fill_pow(pow);
+  __syncthreads();
+  if (part >= a.parts) return;
+  const Pair d(a, m, x, pow);
+  const Dist &p = d.p, &q = d.q;
+  bool take = false;
+  if (p.some) {
+    const double pr = p.sharp ? (x == p.first ? 1.0 : 0.0) : p.weight(target_row(a, m).at(x), pow) / p.sum;
+    double qr = 1.0;
+    if (!d.certain)
+      qr = !q.some ? 0.0 : q.sharp ? (x == q.first ? 1.0 : 0.0) : q.weight(draft_row(a, m).at(x), pow) / q.sum;
+    take = (double)a.u[2 * m] * qr < pr;
+  }
+  if (part == 0 && lane == 0) {
+    a.accepted[m] = take ? 1 : 0;
+    if (take) {
+      a.tokens[m] = x;
+      if (a.conf) a.conf[m] = p.weight(target_row(a, m).at(x), pow) / p.sum;
+    }
+  }
+  if (take || !p.some) return;
+  double w[kQuads][4], sum = 0.0;
+  d.left(a, m, part, w, pow);
+#pragma unroll
+  for (int k = 0; k < kQuads; ++k) sum += sum4(w[k]);
+  sum = lane_scan(sum);
+  if (lane == 63) a.left[(size_t)m * a.parts + part] = sum;
+}
+
+// First part whose running sum exceeds u times the sum of all (the last of positive sum
+// when none does), and the running sum before it.  of(i): part i's sum.
+struct Spot {
+  int part;
+  double before, target, total;
+};
+template <typename F>
+__device__ __forceinline__ Spot find_part(int parts, float u, F of) {
+  const int lane = threadIdx.x & 63;
+  double x = lane < parts ? of(lane) : 0.0, in = lane_scan(x);
+  Spot s{-1, 0.0, 0.0, read_lane(in, 63)};
+  for (int b = 64; b < parts; b += 64) s.total += wave_total(b + lane < parts ? of(b + lane) : 0.0);
+  // 1 and beyond: no sum exceeds it
+  s.target = u < 1.0f ? (double)u * s.total : INFINITY;
+  double run = 0.0;
+  for (int b = 0; b < parts; b += 64) {  // uniform
+    if (b > 0) {
+      x = b + lane < parts ? of(b + lane) : 0.0;
+      in = lane_scan(x);
+    }
+    const uint64_t some = __builtin_amdgcn_ballot_w64(x > 0.0);
+    const uint64_t over = __builtin_amdgcn_ballot_w64(x > 0.0 && run + in > s.target);
+    if (some) {
+      const int L = over ? (int)__builtin_ctzll(over) : 63 - (int)__builtin_clzll(some);
+      s.part = b + L;
+      s.before = run + (read_lane(in, L) - read_lane(x, L));
+      if (over) break;
+    }
+    run += read_lane(in, 63);
+  }
+  return s;
+}
+// The id in the spot's part, from the weights of its ids; every lane gets it.
+__device__ __forceinline__ int find_id(const Spot& s, const double (&w)[kQuads][4], const RowAt& row) {
+  const int lane = threadIdx.x & 63;
+  int id = -1;
+  double run = s.before;
 #pragma unroll
   for (int k = 0; k < kQuads; ++k) {
-    double x = 0.0;
-    if (at.has(tile, k)) {  // uniform
-      double w[4];
-      w4(k, w);
-      x = row_scan((w[0] + w[1]) + (w[2] + w[3]));
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    const int seg = k * rows + wave * 4 + (lane >> 4);
-    if ((lane & 15) == 15) s.seg[(seg % per) * 64 + seg / per] = x;
-  }
-  __syncthreads();
-}
-// The sum of the tile's segments; pre: that of the lanes before.
-__device__ __forceinline__ double segment_sum(const RowShared& s, double& pre) {
-  const int lane = threadIdx.x & 63, per = kQuads * (blockDim.x / 16) / 64;
-  double x = 0.0;
-  for (int i = 0; i < per; ++i) x += s.seg[i * 64 + lane];
-  const double in = lane_scan(x);
-  pre = in - x;
-  return read_lane(in, 63);
-}
-// First segment whose running sum, from `before` on, exceeds the target; the last of
-// positive sum when none does.
-__device__ __forceinline__ Spot find_segment(const RowShared& s, double before, double target) {
-  const int lane = threadIdx.x & 63, rows = blockDim.x / 16, per = kQuads * rows / 64;
-  double x = 0.0;
-  for (int i = 0; i < per; ++i) x += s.seg[i * 64 + lane];
-  const double in = lane_scan(x);
-  double run = before + __shfl_up(in, 1);
-  if (lane == 0) run = before;
-  int over = -1, last = -1;
-  double run_over = 0.0, run_last = 0.0;
-  for (int i = 0; i < per; ++i) {
-    const double y = s.seg[i * 64 + lane];
-    if (y > 0.0) {
-      last = i;
-      run_last = run;
-      if (over < 0 && run + y > target) {
-        over = i;
-        run_over = run;
-      }
-    }
-    run += y;
-  }
-  const uint64_t has_over = __builtin_amdgcn_ballot_w64(over >= 0), has_last = __builtin_amdgcn_ballot_w64(last >= 0);
-  const int L = has_over ? (int)__builtin_ctzll(has_over) : 63 - (int)__builtin_clzll(has_last | 1ull);
-  const int i = __builtin_amdgcn_readlane(has_over ? over : max(last, 0), L);
-  const int seg = L * per + i;
-  return Spot{seg / rows, (seg % rows) / 4, seg % 4, read_lane(has_over ? run_over : run_last, L)};
-}
-// In the spot's wave: the lane that holds the token returns its id, the others -1.
-template <typename W>
-__device__ __forceinline__ int find_id(const Spot& sp, double target, const RowAt& at, int tile, W w4) {
-  const int lane = threadIdx.x & 63;
-  double w[4];
-  w4(sp.k, w);
-  const double x = (w[0] + w[1]) + (w[2] + w[3]);
-  const double in = row_scan(x);
-  const bool mine = (lane >> 4) == sp.lanes;
-  const uint64_t over = __builtin_amdgcn_ballot_w64(mine && x > 0.0 && sp.before + in > target);
-  const uint64_t some = __builtin_amdgcn_ballot_w64(mine && x > 0.0);
-  const int L = over ? (int)__builtin_ctzll(over) : 63 - (int)__builtin_clzll(some | 1ull);
-  if (lane != L) return -1;
-  double run = sp.before + (in - x);
-  int id = -1;
+    const double x = sum4(w[k]), in = lane_scan(x);
+    const uint64_t some = __builtin_amdgcn_ballot_w64(x > 0.0);
+    const uint64_t over = __builtin_amdgcn_ballot_w64(x > 0.0 && run + in > s.target);
+    if (some) {  // uniform
+      const int L = over ? (int)__builtin_ctzll(over) : 63 - (int)__builtin_clzll(some);
+      double r = run + (in - x);
+      int mine = -1;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const bool past = id >= 0 && run > target;
-    if (!past && w[e] > 0.0) id = at.id(tile, sp.k) + e;
-    run += past ? 0.0 : w[e];
+      for (int e = 0; e < 4; ++e) {
+        const bool past = mine >= 0 && r > s.target;
+        if (!past && w[k][e] > 0.0) mine = row.id(s.part, k) + e;
+        r += past ? 0.0 : w[k][e];
+      }
+      id = __builtin_amdgcn_readlane(mine, L);
+      if (over) return id;
+    }
+    run += read_lane(in, 63);
   }
   return id;
 }
 
-// Group k of the registers, k uniform.
-__device__ __forceinline__ void take_group(const Quads& q, int k, float (&x)[4]) {
-#pragma unroll
-  for (int j = 0; j < kQuads; ++j)
-    if (j == k) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = q.x[j][e];
+// ---------------------------------------------------------------------------
+// k_draw: a wave a row that has no token yet, then one a request for its count.  In a
+// chain a row that follows one without an accepted draft is void.  (A void row's flag
+// is cleared while later rows look: they are void by the earlier row's, which stays.)
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(64) void k_draw(VerifyArgs a) {
+  __shared__ double pow[32];
+  const int lane = threadIdx.x;
+  if ((int)blockIdx.x >= a.M) {  // a request's count
+    const int s = blockIdx.x - a.M;
+    const int r0 = a.cu ? min(max(a.cu[s], 0), a.M) : 0, r1 = a.cu ? min(a.cu[s + 1], a.M) : a.M;
+    int n = 0;
+    for (int b = r0; b < r1; b += 64) {
+      const uint64_t there = r1 - b >= 64 ? ~0ull : (1ull << (r1 - b)) - 1;
+      const uint64_t yes = __builtin_amdgcn_ballot_w64(b + lane < r1 && a.accepted[b + lane]), no = there & ~yes;
+      if (a.chain && no) {
+        n += (int)__builtin_ctzll(no);
+        break;
+      }
+      n += (int)__popcll(yes);
     }
-}
-
-__device__ __forceinline__ double weight_at(const Dist& d, const RowAt& at, int id, const double* pow) {
-  const float x = fmaxf(at.l[id], -INFINITY);
-  return d.weight<false>(d.lift ? d.lifted(x) : x, pow);
-}
-
-// ---------------------------------------------------------------------------
-// k_verify_rows: a workgroup a row: its draft is taken or a token is drawn.  DRAFT:
-// with drafts; ONE: the row fits the registers.
-// ---------------------------------------------------------------------------
-template <bool DRAFT, bool ONE>
-__global__ __launch_bounds__(kMaxThreads) void k_verify_rows(VerifyArgs a) {
-  __shared__ RowShared s;
-  const int m = blockIdx.x, V = a.V, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int nwaves = blockDim.x / 64;
-  if (a.cu && (m < a.cu[0] || m >= a.cu[a.n_seq])) return;  // uniform
-  const float* const row = a.logits + (size_t)m * V;
-  const RowAt pa(row, V, RowAt::shift_of(row));
-  const int x = DRAFT ? a.draft[m] : -1;
-  const bool real = x >= 0 && x < V, has_q = DRAFT && real && a.draft_logits;
-  const RowAt qa(has_q ? a.draft_logits + (size_t)m * V : row, V, pa.shift);
-  const int tiles = ONE ? 1 : pa.tiles();
-  Quads P, Q = {};
-  const double* pow = s.pow;
-  if (tid < 32) s.pow[tid] = kPow[tid];
-
-  // the largest
-  Dist p, q;
-  p.init(a.tau);
-  q.init(a.draft_tau);
-  for (int t = 0; t < tiles; ++t) {
-    pa.load(P, t);
-    if (has_q) qa.load(Q, t);
-    p.top = fmaxf(p.top, thread_top(P));
-    if (has_q) q.top = fmaxf(q.top, thread_top(Q));
+    if (lane == 0) a.n_accepted[s] = n;
+    return;
   }
-  p.top = wave_top(p.top);
-  if (DRAFT) q.top = wave_top(q.top);
-  if (lane == 0) {
-    s.top[0][wave] = p.top;
-    s.top[1][wave] = q.top;
-  }
-  __syncthreads();
-  for (int i = 0; i < nwaves; ++i) {
-    p.top = fmaxf(p.top, s.top[0][i]);
-    q.top = fmaxf(q.top, s.top[1][i]);
-  }
-  p.set_top();
-  q.set_top();
-  // a tile of the row (and its draft's) into registers; with ONE it is there
-  bool clean_p = false, clean_q = false;  // of the wave
-  auto lift_tile = [&]() __attribute__((always_inline)) {
-    if (p.lift) lift_all(P, p);
-    if (has_q && q.lift) lift_all(Q, q);
-    clean_p = wave_clean(P, p.cut);
-    if (has_q) clean_q = wave_clean(Q, q.cut);
-  };
-  auto tile = [&](int t) __attribute__((always_inline)) {
-    if (ONE) {
-      renew(P);
-      if (DRAFT) renew(Q);
+  const int m = blockIdx.x;
+  if (!row_counts(a, m)) return;
+  if (a.chain) {
+    int r0 = 0;
+    if (a.cu) {  // the last request that begins at or before the row
+      int lo = 0, hi = a.n_seq;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.cu[mid] <= m) lo = mid;
+        else hi = mid;
+      }
+      r0 = max(a.cu[lo], 0);
+    }
+    bool ended = false;
+    for (int b = r0; b < m && !ended; b += 64)
+      ended = __builtin_amdgcn_ballot_w64(b + lane < m && !a.accepted[b + lane]) != 0;
+    if (ended) {
+      if (lane == 0) {
+        a.tokens[m] = -1;
+        a.accepted[m] = 0;
+        if (a.conf) a.conf[m] = 0.0;
+      }
       return;
     }
-    pa.load(P, t);
-    if (has_q) qa.load(Q, t);
-    lift_tile();
-  };
-  if (ONE) lift_tile();
-
-  // at temperature 0, the first of the largest
-  auto first_id = [&](Dist& d, const Quads& r) __attribute__((always_inline)) {
-    int id = V;
-    for (int t = 0; t < tiles; ++t) {
-      tile(t);
-#pragma unroll
-      for (int k = 0; k < kQuads; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (r.x[k][e] == d.top && d.some) id = min(id, pa.id(t, k) + e);
-    }
-    for (int o = 32; o > 0; o >>= 1) id = min(id, __shfl_xor(id, o));
-    __syncthreads();
-    if (lane == 0) s.first[wave] = id;
-    __syncthreads();
-    for (int i = 0; i < nwaves; ++i) id = min(id, s.first[i]);
-    d.first = id;
-  };
-  if (p.sharp) first_id(p, P);
-  if (has_q && q.sharp) first_id(q, Q);
-
-  // the sums of the weights
-  auto thread_sum = [&](auto clean, const Dist& d, const Quads& r, int t) __attribute__((always_inline)) {
-    double sum = 0.0;
-#pragma unroll
-    for (int k = 0; k < kQuads; ++k)
-      if (pa.has(t, k)) {  // uniform
-        double w[4];
-        d.template weights<decltype(clean)::value>(r.x[k], w, pow);
-        sum += (w[0] + w[1]) + (w[2] + w[3]);
-        __builtin_amdgcn_sched_barrier(0);  // four chains at a time: more would spill the rows
-      }
-    return sum;
-  };
-  auto tile_sum = [&](bool clean, const Dist& d, const Quads& r, int t) __attribute__((always_inline)) {
-    return clean ? thread_sum(std::true_type{}, d, r, t) : thread_sum(std::false_type{}, d, r, t);
-  };
+  }
+  if (a.accepted && a.accepted[m]) return;
+  fill_pow(pow);
+  __syncthreads();
+  const int x = a.draft ? a.draft[m] : -1;
+  const bool real = (uint32_t)x < (uint32_t)a.V;
+  const RowAt row = target_row(a, m);
+  const PartStat* st = a.p_stat + (size_t)m * a.parts;
+  const Dist p = row_dist(st, a.parts, a.tau, pow);
   int tok = -1;
-  bool take = false, mine = tid == 0;  // the thread that writes
-  if (real && p.some) {
-    double wp = 0.0, wq = 0.0;
-    for (int t = 0; t < tiles; ++t) {
-      tile(t);
-      wp += tile_sum(clean_p, p, P, t);
-      if (has_q && q.some) wq += tile_sum(clean_q, q, Q, t);
-    }
-    wp = row_scan(wp);
-    wq = row_scan(wq);
-    if ((lane & 15) == 15) {
-      s.part[0][tid >> 4] = wp;
-      s.part[1][tid >> 4] = wq;
-    }
-    __syncthreads();
-    p.sum = read_lane(lane_scan(lane < nwaves * 4 ? s.part[0][lane] : 0.0), 63);
-    q.sum = read_lane(lane_scan(lane < nwaves * 4 ? s.part[1][lane] : 0.0), 63);
-    const double pr = p.sharp ? (x == p.first ? 1.0 : 0.0) : weight_at(p, pa, x, pow) / p.sum;
-    double qr = 1.0;
-    if (has_q) qr = !q.some ? 0.0 : q.sharp ? (x == q.first ? 1.0 : 0.0) : weight_at(q, qa, x, pow) / q.sum;
-    take = (double)a.u[2 * m] * qr < pr;
-    if (take) tok = x;
-  }
-
-  // a token: from max(p - q, 0) where a draft was refused, else from p
-  if (!take && p.some) {
-    const float u = DRAFT ? a.u[2 * m + 1] : (p.sharp ? 0.0f : a.u[m]);
-    // draws from the weights w4(k, tile, out) of all tiles: false when they sum to 0
-    auto draw = [&](auto w4, double& total) __attribute__((always_inline)) {
-      int at = 0;
-      double before = 0.0, pre;
-      if (ONE) {
-        tile(0);
-        fill_segments(s, pa, 0, [&](int k, double (&w)[4]) __attribute__((always_inline)) { w4(k, 0, w); });
-        total = segment_sum(s, pre);
-      } else {
-        total = 0.0;
-        int last = 0;
-        for (int t = 0; t < tiles; ++t) {
-          tile(t);
-          fill_segments(s, pa, t, [&](int k, double (&w)[4]) __attribute__((always_inline)) { w4(k, t, w); });
-          const double sum = segment_sum(s, pre);
-          if (tid == 0) s.tile[t] = sum;
-          total += sum;
-          if (sum > 0.0) last = t;
-        }
-        __syncthreads();
-        const double target = u < 1.0f ? (double)u * total : INFINITY;
-        for (at = 0; at < last && !(before + s.tile[at] > target); ++at) before += s.tile[at];
-      }
-      if (!(total > 0.0)) return false;
-      const double target = u < 1.0f ? (double)u * total : INFINITY;  // 1 and beyond: no sum exceeds it
-      if (!ONE) {
-        tile(at);
-        fill_segments(s, pa, at, [&](int k, double (&w)[4]) __attribute__((always_inline)) { w4(k, at, w); });
-      }
-      const Spot sp = find_segment(s, before, target);
-      mine = false;
-      if (wave == sp.wave) {  // wave-uniform
-        if (ONE) tile(0);
-        tok = find_id(sp, target, pa, at, [&](int k, double (&w)[4]) __attribute__((always_inline)) { w4(k, at, w); });
-        mine = tok >= 0;
-      }
-      return true;
-    };
-    double total;
-    bool drawn = false;
-    if constexpr (DRAFT) {
-      if (real) {
-        const double ip = 1.0 / p.sum, iq = 1.0 / q.sum;
-        drawn = draw([&](int k, int t, double (&w)[4]) __attribute__((always_inline)) {
-          float v[4];
-          double y[4] = {};
-          const int id = pa.id(t, k);
-          take_group(P, k, v);
-          if (p.sharp) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = id + e == p.first ? 1.0 : 0.0;
-          } else {
-            p.template weights<false>(v, w, pow);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] *= ip;
-          }
-          if (!has_q || (q.some && q.sharp)) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = id + e == (has_q ? q.first : x) ? 1.0 : 0.0;
-          } else if (q.some) {
-            take_group(Q, k, v);
-            q.template weights<false>(v, y, pow);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] *= iq;
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = fmax(w[e] - y[e], 0.0);
-        }, total);
+  if (p.some) {
+    const float u = a.draft ? a.u[2 * m + 1] : p.sharp ? 0.0f : a.u[m];
+    double w[kQuads][4];
+    if (real) {
+      const Spot s = find_part(a.parts, u, [&](int i) { return a.left[(size_t)m * a.parts + i]; });
+      if (s.total > 0.0) {
+        const Pair d(a, m, x, pow);
+        d.left(a, m, s.part, w, pow);
+        tok = find_id(s, w, row);
       }
     }
-    if (!drawn) {
-      auto from_p = [&](auto clean, int k, double (&w)[4]) __attribute__((always_inline)) {
-        float v[4];
-        take_group(P, k, v);
-        p.template weights<decltype(clean)::value>(v, w, pow);
-      };
-      draw([&](int k, int, double (&w)[4]) __attribute__((always_inline)) { clean_p ? from_p(std::true_type{}, k, w) : from_p(std::false_type{}, k, w); },
-           p.sum);
-      if (p.sharp) {
-        tok = p.first;
-        mine = tid == 0;
-      }
+    if (tok < 0 && p.sharp) tok = p.first;
+    if (tok < 0) {
+      const Spot s = find_part(a.parts, u, [&](int i) { return st[i].sum * p.weight(st[i].top, pow); });
+      float l[kQuads][4];
+      row.load(l, s.part);
+      p.weights(l, w, pow);
+      tok = find_id(s, w, row);
     }
   }
-  if (!mine) return;
-  a.tokens[m] = tok;
-  if (a.accepted) a.accepted[m] = take ? 1 : 0;
-  if (a.conf) a.conf[m] = tok >= 0 ? weight_at(p, pa, tok, pow) / p.sum : 0.0;
+  if (lane == 0) {
+    a.tokens[m] = tok;
+    if (a.conf) a.conf[m] = tok >= 0 ? p.weight(row.at(tok), pow) / p.sum : 0.0;
+  }
 }
 
-// k_verify_join: a wave a request: the drafts taken, and in a chain the rows after
-// the first that takes none.
-__global__ __launch_bounds__(64) void k_verify_join(VerifyArgs a) {
-  const int s = blockIdx.x, lane = threadIdx.x;
-  const int r0 = a.cu ? min(max(a.cu[s], 0), a.M) : 0, r1 = a.cu ? min(a.cu[s + 1], a.M) : a.M;
-  int n = 0;
-  bool ended = false;
-  for (int b = r0; b < r1; b += 64) {
-    const int m = b + lane;
-    const bool in = m < r1, took = in && a.accepted[m];
-    const uint64_t no = __builtin_amdgcn_ballot_w64(in && !took);
-    const uint64_t yes = __builtin_amdgcn_ballot_w64(took);
-    if (!a.chain) {
-      n += (int)__popcll(yes);
-      continue;
-    }
-    const int stop = no ? (int)__builtin_ctzll(no) : 64;  // the first row that takes none
-    if (in && (ended || lane > stop)) {
-      a.tokens[m] = -1;
-      a.accepted[m] = 0;
-      if (a.conf) a.conf[m] = 0.0;
-    }
-    if (!ended) n += stop;
-    ended = ended || no;
-  }
-  if (a.chain && !ended) n = max(r1 - r0, 0);
-  if (a.n_accepted && lane == 0) a.n_accepted[s] = n;
+static int parts_of(int V) { return (V + 3 + kPartIds - 1) / kPartIds; }  // with up to 3 ids before the row
+
+size_t verify_ws(int M, int V, bool drafts) {
+  const size_t n = (size_t)M * parts_of(V);
+  return align_up(n * sizeof(PartStat), 256) * (drafts ? 2 : 1) + (drafts ? align_up(n * sizeof(double), 256) : 0);
 }
 
 nmdlm_status launch_verify(const VerifyCall& c, hipStream_t st) {
-  const VerifyArgs a{c.logits, c.draft_logits, c.draft, c.u, c.cu, c.M, c.V, c.n_seq, c.tau, c.draft_tau,
-                     c.tokens, c.accepted, c.n_accepted, c.conf, !c.each};
-  // the fewest threads whose registers hold the row, with up to 3 ids before it
-  int threads = 256;
-  while (threads < kMaxThreads && threads * kQuads * 4 < c.V + 3) threads *= 2;
-  const bool one = threads * kQuads * 4 >= c.V + 3;
-  const auto fn = c.draft ? (one ? k_verify_rows<true, true> : k_verify_rows<true, false>)
-                          : (one ? k_verify_rows<false, true> : k_verify_rows<false, false>);
-  hipLaunchKernelGGL(fn, dim3((unsigned)c.M), dim3(threads), 0, st, a);
-  const nmdlm_status rc = hip_status();
-  if (rc != NMDLM_OK || !c.draft || (c.each && !c.n_accepted)) return rc;
-  hipLaunchKernelGGL(k_verify_join, dim3((unsigned)c.n_seq), dim3(64), 0, st, a);
+  const int parts = parts_of(c.V);
+  const size_t n = (size_t)c.M * parts;
+  Carver cv{static_cast<char*>(c.ws), 0, (size_t)-1, true};
+  PartStat* const p_stat = cv.take<PartStat>(n);
+  PartStat* const q_stat = c.draft ? cv.take<PartStat>(n) : nullptr;
+  double* const left = c.draft ? cv.take<double>(n) : nullptr;
+  const VerifyArgs a{c.logits, c.draft_logits, c.draft, c.u, c.cu, c.M, c.V, c.n_seq, parts, c.tau, c.draft_tau,
+                     c.tokens, c.accepted, c.n_accepted, c.conf, p_stat, q_stat, left, c.draft && !c.each};
+  const unsigned wgs = (parts + kPartWaves - 1) / kPartWaves;
+  hipLaunchKernelGGL(k_logit_parts, dim3(wgs, c.M, c.draft_logits ? 2 : 1), dim3(64 * kPartWaves), 0, st, a);
+  nmdlm_status rc = hip_status();
+  if (rc != NMDLM_OK) return rc;
+  if (c.draft) {
+    hipLaunchKernelGGL(k_verify_left, dim3(wgs, c.M), dim3(64 * kPartWaves), 0, st, a);
+    if ((rc = hip_status()) != NMDLM_OK) return rc;
+  }
+  hipLaunchKernelGGL(k_draw, dim3((unsigned)c.M + (c.n_accepted ? c.n_seq : 0)), dim3(64), 0, st, a);
   return hip_status();
 }
 

@@ -60,25 +60,38 @@ def test_attention_workspace_sizes(lib):
 
 
 def test_sample_refusals(lib):
-    def call(l=FAKE, M=4, V=100, tau=1.0, u=FAKE, tok=FAKE, conf=None):
-        return lib.nmdlm_token_sample(l, M, V, tau, u, tok, conf, None)
+    def call(l=FAKE, M=4, V=100, tau=1.0, u=FAKE, tok=FAKE, conf=None, ws=FAKE, nb=1 << 20):
+        return lib.nmdlm_token_sample(l, M, V, tau, u, tok, conf, ws, nb, None)
     for bad in (dict(l=None), dict(tok=None), dict(u=None), dict(M=0), dict(V=0), dict(tau=-0.5),
                 dict(tau=float("nan")), dict(tau=float("inf")), dict(l=FAKE + 2), dict(u=FAKE + 1),
                 dict(tok=FAKE + 2), dict(conf=FAKE + 4)):
         assert call(**bad) == INVALID, bad
     assert call(V=B.NMDLM_MAX_SAMPLE_V + 1) == UNSUPPORTED
+    assert call(M=B.NMDLM_MAX_SAMPLE_M + 1) == UNSUPPORTED
+    need = lib.nmdlm_token_sample_workspace_size(4, 100)
+    assert need > 0 and need % 256 == 0
+    for bad in (dict(ws=None), dict(ws=FAKE + 8), dict(nb=need - 1)):
+        assert call(**bad) == WORKSPACE, bad
+    for f in (lib.nmdlm_token_sample_workspace_size, lib.nmdlm_draft_verify_workspace_size):
+        for bad in ((0, 5), (5, 0), (-1, 5), (1 << 16, 5), (5, (1 << 24) + 1)):
+            assert f(*bad) == 0
 
 
 def test_verify_refusals(lib):
     def call(l=FAKE, q=FAKE, M=4, V=100, draft=FAKE, u=FAKE, tau=1.0, dtau=1.0, cu=FAKE, n=2, flags=0, tok=FAKE,
-             acc=FAKE, n_acc=None, conf=None):
-        return lib.nmdlm_draft_verify(l, q, M, V, draft, u, tau, dtau, cu, n, flags, tok, acc, n_acc, conf, None)
+             acc=FAKE, n_acc=None, conf=None, ws=FAKE, nb=1 << 20):
+        return lib.nmdlm_draft_verify(l, q, M, V, draft, u, tau, dtau, cu, n, flags, tok, acc, n_acc, conf, ws, nb,
+                                      None)
     for bad in (dict(l=None), dict(draft=None), dict(u=None), dict(tok=None), dict(acc=None), dict(M=0), dict(V=0),
                 dict(n=0), dict(cu=None, n=2), dict(flags=2), dict(tau=-1.0), dict(dtau=-1.0),
                 dict(dtau=float("nan")), dict(l=FAKE + 1), dict(q=FAKE + 2), dict(draft=FAKE + 2), dict(u=FAKE + 2),
                 dict(cu=FAKE + 2), dict(tok=FAKE + 1), dict(n_acc=FAKE + 1), dict(conf=FAKE + 4)):
         assert call(**bad) == INVALID, bad
     assert call(V=B.NMDLM_MAX_SAMPLE_V + 1) == UNSUPPORTED
+    assert call(n=B.NMDLM_MAX_PLAN_ROWS + 1) == UNSUPPORTED
+    need = lib.nmdlm_draft_verify_workspace_size(4, 100)
+    for bad in (dict(ws=None), dict(ws=FAKE + 8), dict(nb=need - 1)):
+        assert call(**bad) == WORKSPACE, bad
 
 
 def test_binding_refuses_host_tensors_and_wrong_masks():
