@@ -13,6 +13,8 @@
 #include <float.h>
 #include <math.h>
 
+#include <algorithm>
+
 #include "masked.h"
 
 namespace nmdlm {
@@ -23,6 +25,18 @@ struct PartStat {
   double sum;    // of exp((l - top) / tau)
 };
 
+// A temperature's constants, from the host: a float64 division costs a wave more than the
+// weights of its ids.
+struct Temper {
+  double inv, scale;  // 1 / tau (finite, so that 0 * inv is 0); 32 / (tau ln 2)
+  double reach;       // 690 tau: no exponent below -700 within this of the largest
+  bool sharp;         // temperature 0: weights at 1
+};
+static Temper temper(double tau) {
+  const double inv = tau == 0.0 ? 1.0 : std::min(1.0 / tau, 1e300);
+  return Temper{inv, inv * 46.16624130844683, 690.0 / inv, tau == 0.0};
+}
+
 struct VerifyArgs {
   const float* logits;
   const float* draft_logits;
@@ -30,7 +44,7 @@ struct VerifyArgs {
   const float* u;
   const int32_t* cu;
   int M, V, n_seq, parts;
-  double tau, draft_tau;
+  Temper tau, draft_tau;
   int32_t* tokens;
   uint8_t* accepted;
   int32_t* n_accepted;
@@ -75,7 +89,7 @@ struct RowAt {
   __device__ __forceinline__ int id(int part, int k) const {
     return part * kPartIds + 4 * (64 * k + (int)(threadIdx.x & 63)) - shift;
   }
-  // NaN and ids outside the row become -inf
+  // ids outside the row become -inf
   __device__ __forceinline__ void load(float (&x)[kQuads][4], int part) const {
     if (vec && part * kPartIds >= shift && (part + 1) * kPartIds - shift <= V) {  // uniform
 #pragma unroll
@@ -96,10 +110,6 @@ struct RowAt {
           x[k][e] = v >= 0 && v < V ? y : -INFINITY;
         }
     }
-#pragma unroll
-    for (int k = 0; k < kQuads; ++k)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[k][e] = fmaxf(x[k][e], -INFINITY);
   }
   __device__ __forceinline__ float at(int v) const { return fmaxf(l[v], -INFINITY); }
 };
@@ -123,16 +133,12 @@ __device__ __forceinline__ bool row_counts(const VerifyArgs& a, int m) {
 // it is the instructions that count, 17 a weight.
 struct Dist {
   float top, cut;     // the largest; below cut an exponent may be below -700
-  double inv, scale;  // 1 / tau; 32 / (tau ln 2)
+  double inv, scale, reach;
   double sum;
   bool some, sharp, lift;  // any weight; temperature 0; the largest is +inf
   int first;               // id of the largest
-  __device__ __forceinline__ explicit Dist(double tau) {
-    sharp = tau == 0.0;
-    inv = sharp ? 1.0 : fmin(1.0 / tau, 1e300);  // finite, so that 0 * inv is 0
-    scale = inv * 46.16624130844683;
-    sum = 0.0;
-    first = 0;
+  __device__ __forceinline__ explicit Dist(const Temper& t)
+      : inv(t.inv), scale(t.scale), reach(t.reach), sum(0.0), sharp(t.sharp), first(0) {
     set_top(-INFINITY);
   }
   // with a largest of +inf these logits count as 0, the others as -inf
@@ -140,7 +146,7 @@ struct Dist {
     some = t > -INFINITY;
     lift = t == INFINITY;
     top = lift ? 0.0f : t;
-    cut = fmaxf((float)((double)top - 690.0 / inv), -FLT_MAX);
+    cut = fmaxf((float)((double)top - reach), -FLT_MAX);
   }
   __device__ __forceinline__ float seen(float x) const {
     return !lift ? x : x == INFINITY ? 0.0f : -INFINITY;
@@ -164,9 +170,22 @@ struct Dist {
   __device__ __forceinline__ double weight(float x, const double* pow) const {
     return weight_of<false>(seen(x), pow);
   }
-  // the weights of a lane's ids
-  __device__ __forceinline__ void weights(float (&x)[kQuads][4], double (&w)[kQuads][4], const double* pow) const {
-    float least = INFINITY;
+  // use(k, the weights of group k) for a lane's ids, four chains at a time: more would
+  // take the registers of other waves
+  template <bool CLEAN, typename U>
+  __device__ __forceinline__ void each_group(const float (&x)[kQuads][4], const double* pow, U use) const {
+#pragma unroll
+    for (int k = 0; k < kQuads; ++k) {
+      double w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = weight_of<CLEAN>(x[k][e], pow);
+      use(k, w);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  template <typename U>
+  __device__ __forceinline__ void groups(float (&x)[kQuads][4], const double* pow, U use) const {
+    float least = INFINITY;  // NaN where a logit is
     if (lift) {  // uniform
 #pragma unroll
       for (int k = 0; k < kQuads; ++k)
@@ -176,18 +195,20 @@ struct Dist {
 #pragma unroll
     for (int k = 0; k < kQuads; ++k)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) least = fminf(least, x[k][e]);
-    if (__builtin_amdgcn_ballot_w64(least >= cut) == ~0ull) {
+      for (int e = 0; e < 4; ++e) least = __builtin_elementwise_minimum(least, x[k][e]);
+    if (__builtin_amdgcn_ballot_w64(least >= cut) == ~0ull) each_group<true>(x, pow, use);
+    else each_group<false>(x, pow, use);
+  }
+  __device__ __forceinline__ void weights(float (&x)[kQuads][4], double (&w)[kQuads][4], const double* pow) const {
+    groups(x, pow, [&](int k, const double (&g)[4]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int k = 0; k < kQuads; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[k][e] = weight_of<true>(x[k][e], pow);
-    } else {
-#pragma unroll
-      for (int k = 0; k < kQuads; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[k][e] = weight_of<false>(x[k][e], pow);
-    }
+      for (int e = 0; e < 4; ++e) w[k][e] = g[e];
+    });
+  }
+  __device__ __forceinline__ double weight_sum(float (&x)[kQuads][4], const double* pow) const {
+    double sum = 0.0;
+    groups(x, pow, [&](int, const double (&g)[4]) __attribute__((always_inline)) { sum += (g[0] + g[1]) + (g[2] + g[3]); });
+    return sum;
   }
 };
 
@@ -233,52 +254,86 @@ __device__ __forceinline__ int wave_min(int x) {
 __device__ __forceinline__ double sum4(const double (&w)[4]) { return (w[0] + w[1]) + (w[2] + w[3]); }
 
 // ---------------------------------------------------------------------------
-// k_logit_parts: grid (parts / 4, rows, 1 or 2: the target's and the draft's), a wave a
-// part.
+// k_logit_parts: the parts of all rows, the target's and then the draft's, in turn to the
+// waves; a wave's next part is on its way while it weighs one.
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(64 * kPartWaves) void k_logit_parts(VerifyArgs a) {
+__global__ __launch_bounds__(64 * kPartWaves, 5) void k_logit_parts(VerifyArgs a) {
   __shared__ double pow[32];
-  const int m = blockIdx.y, lane = threadIdx.x & 63;
-  const int part = blockIdx.x * kPartWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const bool of_draft = blockIdx.z != 0;
-  if (!row_counts(a, m)) return;  // uniform
-  if (of_draft && (uint32_t)a.draft[m] >= (uint32_t)a.V) return;
+  const int lane = threadIdx.x & 63, rows = a.draft_logits ? 2 * a.M : a.M;
+  const int step = gridDim.x * kPartWaves;
+  const int step_m = step / a.parts, step_p = step - step_m * a.parts;
+  const int unit = blockIdx.x * kPartWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  int m = unit / a.parts, part = unit - m * a.parts;  // rows past M: the draft's
+  // whether the row's parts are needed
+  auto wanted = [&](int r) {
+    if (r >= rows) return false;
+    const bool of_draft = r >= a.M;
+    const int row = of_draft ? r - a.M : r;
+    return row_counts(a, row) && !(of_draft && (uint32_t)a.draft[row] >= (uint32_t)a.V);
+  };
+  auto row_at = [&](int r) { return r >= a.M ? draft_row(a, r - a.M) : target_row(a, r); };
+  auto advance = [&](int& r, int& p) {
+    r += step_m;
+    p += step_p;
+    if (p >= a.parts) {
+      p -= a.parts;
+      ++r;
+    }
+  };
+  float next[kQuads][4], x[kQuads][4];
+  bool here = wanted(m);
+  if (here) row_at(m).load(next, part);
   fill_pow(pow);
-  const RowAt row = of_draft ? draft_row(a, m) : target_row(a, m);
-  float x[kQuads][4];
-  if (part < a.parts) row.load(x, part);  // wave-uniform
   __syncthreads();
-  if (part >= a.parts) return;
-  float t = -INFINITY;
-#pragma unroll
-  for (int k = 0; k < kQuads; ++k)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) t = fmaxf(t, x[k][e]);
-  t = wave_top(t);
-  Dist d(of_draft ? a.draft_tau : a.tau);
-  d.set_top(t);
-  int first = a.V;
-  if (d.sharp) {  // uniform
+  while (m < rows) {  // wave-uniform
 #pragma unroll
     for (int k = 0; k < kQuads; ++k)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (x[k][e] == t && d.some) first = min(first, row.id(part, k) + e);
-    first = wave_min(first);
-  }
-  double sum = 0.0;
-  if (d.some) {  // wave-uniform
-    double w[kQuads][4];
-    d.weights(x, w, pow);
+      for (int e = 0; e < 4; ++e) x[k][e] = next[k][e];
+    const int at_m = m, at_part = part;
+    const bool at_here = here;
+    advance(m, part);
+    here = wanted(m);
+    if (here) row_at(m).load(next, part);
+    if (!at_here) continue;
+    float t = -INFINITY;  // NaN where a logit is
 #pragma unroll
-    for (int k = 0; k < kQuads; ++k) sum += sum4(w[k]);
-    sum = lane_scan(sum);
+    for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t = __builtin_elementwise_maximum(t, x[k][e]);
+    if (__builtin_amdgcn_ballot_w64(t != t)) {  // wave-uniform, rare
+      t = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t = fmaxf(t, x[k][e]);
+    }
+    t = wave_top(t);
+    Dist d(at_m >= a.M ? a.draft_tau : a.tau);
+    d.set_top(t);
+    int first = a.V;
+    if (d.sharp) {  // uniform
+      const RowAt row = row_at(at_m);
+#pragma unroll
+      for (int k = 0; k < kQuads; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (x[k][e] == t && d.some) first = min(first, row.id(at_part, k) + e);
+      first = wave_min(first);
+    }
+    double sum = 0.0;
+    if (d.some) {  // wave-uniform
+      sum = d.weight_sum(x, pow);
+      sum = lane_scan(sum);
+    }
+    if (lane == 63)
+      (at_m >= a.M ? a.q_stat : a.p_stat)[(size_t)(at_m >= a.M ? at_m - a.M : at_m) * a.parts + at_part] =
+          PartStat{t, first, sum};
   }
-  if (lane == 63) (of_draft ? a.q_stat : a.p_stat)[(size_t)m * a.parts + part] = PartStat{t, first, sum};
 }
 
 // The row's distribution from its parts; every lane gets it.
-__device__ __forceinline__ Dist row_dist(const PartStat* st, int parts, double tau, const double* pow) {
+__device__ __forceinline__ Dist row_dist(const PartStat* st, int parts, const Temper& tau, const double* pow) {
   const int lane = threadIdx.x & 63;
   Dist d(tau);
   float top = -INFINITY;
@@ -297,6 +352,15 @@ __device__ __forceinline__ Dist row_dist(const PartStat* st, int parts, double t
   return d;
 }
 
+// The logits of a part of a row, the target's and the draft's.
+struct Logits {
+  float p[kQuads][4], q[kQuads][4];
+  __device__ __forceinline__ void load(const VerifyArgs& a, int m, int part) {
+    target_row(a, m).load(p, part);
+    if (a.draft_logits) draft_row(a, m).load(q, part);
+  }
+};
+
 // The target's and the draft's distribution of a row with a draft x.
 struct Pair {
   Dist p, q;
@@ -308,12 +372,9 @@ struct Pair {
     if (!certain) q = row_dist(a.q_stat + (size_t)m * a.parts, a.parts, a.draft_tau, pow);
   }
   // max(p - q, 0) of a part's ids
-  __device__ __forceinline__ void left(const VerifyArgs& a, int m, int part, double (&w)[kQuads][4],
+  __device__ __forceinline__ void left(const RowAt& row, int part, Logits& l, double (&w)[kQuads][4],
                                        const double* pow) const {
-    const RowAt row = target_row(a, m);
-    float lp[kQuads][4], lq[kQuads][4];
-    row.load(lp, part);
-    if (!certain) draft_row(a, m).load(lq, part);
+    auto &lp = l.p, &lq = l.q;
     double y[kQuads][4];
     if (p.sharp) {
 #pragma unroll
@@ -329,7 +390,7 @@ struct Pair {
         for (int e = 0; e < 4; ++e) w[k][e] *= ip;
     }
     if (certain || q.sharp || !q.some) {
-      const int at = certain ? x : q.some ? q.first : -1 << 30;
+      const int at = certain ? x : q.some ? q.first : INT32_MIN;
 #pragma unroll
       for (int k = 0; k < kQuads; ++k)
 #pragma unroll
@@ -350,46 +411,54 @@ struct Pair {
 };
 
 // ---------------------------------------------------------------------------
-// k_verify_left: grid (parts / 4, rows), a wave a part.  Each decides on its row's draft
-// for itself; part 0 writes what was decided.
+// k_verify_left: grid (waves of a row / 4, rows).  Each wave decides on its row's draft for
+// itself; the first writes what was decided.  (With the logits of the wave's first part on
+// their way meanwhile, 576 rows took 62 us against 58: most rows do not need them.)
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(64 * kPartWaves) void k_verify_left(VerifyArgs a) {
   __shared__ double pow[32];
-  const int m = blockIdx.y, lane = threadIdx.x & 63;
-  const int part = blockIdx.x * kPartWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int m = blockIdx.y, lane = threadIdx.x & 63, step = gridDim.x * kPartWaves;
+  int part = blockIdx.x * kPartWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   if (!row_counts(a, m)) return;  // uniform
   const int x = a.draft[m];
   if ((uint32_t)x >= (uint32_t)a.V) {
     if (part == 0 && lane == 0) a.accepted[m] = 0;
     return;
   }
+  const RowAt row = target_row(a, m);
+  const float u = a.u[2 * m], px = row.at(x), qx = a.draft_logits ? draft_row(a, m).at(x) : 0.0f;
   fill_pow(pow);
   __syncthreads();
   if (part >= a.parts) return;
   const Pair d(a, m, x, pow);
   const Dist &p = d.p, &q = d.q;
   bool take = false;
+  double prob = 0.0;
   if (p.some) {
-    const double pr = p.sharp ? (x == p.first ? 1.0 : 0.0) : p.weight(target_row(a, m).at(x), pow) / p.sum;
+    prob = p.weight(px, pow) / p.sum;
+    const double pr = p.sharp ? (x == p.first ? 1.0 : 0.0) : prob;
     double qr = 1.0;
-    if (!d.certain)
-      qr = !q.some ? 0.0 : q.sharp ? (x == q.first ? 1.0 : 0.0) : q.weight(draft_row(a, m).at(x), pow) / q.sum;
-    take = (double)a.u[2 * m] * qr < pr;
+    if (!d.certain) qr = !q.some ? 0.0 : q.sharp ? (x == q.first ? 1.0 : 0.0) : q.weight(qx, pow) / q.sum;
+    take = (double)u * qr < pr;
   }
   if (part == 0 && lane == 0) {
     a.accepted[m] = take ? 1 : 0;
     if (take) {
       a.tokens[m] = x;
-      if (a.conf) a.conf[m] = p.weight(target_row(a, m).at(x), pow) / p.sum;
+      if (a.conf) a.conf[m] = prob;
     }
   }
   if (take || !p.some) return;
-  double w[kQuads][4], sum = 0.0;
-  d.left(a, m, part, w, pow);
+  for (; part < a.parts; part += step) {
+    Logits l;
+    l.load(a, m, part);
+    double w[kQuads][4], sum = 0.0;
+    d.left(row, part, l, w, pow);
 #pragma unroll
-  for (int k = 0; k < kQuads; ++k) sum += sum4(w[k]);
-  sum = lane_scan(sum);
-  if (lane == 63) a.left[(size_t)m * a.parts + part] = sum;
+    for (int k = 0; k < kQuads; ++k) sum += sum4(w[k]);
+    sum = lane_scan(sum);
+    if (lane == 63) a.left[(size_t)m * a.parts + part] = sum;
+  }
 }
 
 // First part whose running sum exceeds u times the sum of all (the last of positive sum
@@ -426,7 +495,6 @@ __device__ __forceinline__ Spot find_part(int parts, float u, F of) {
 }
 // The id in the spot's part, from the weights of its ids; every lane gets it.
 __device__ __forceinline__ int find_id(const Spot& s, const double (&w)[kQuads][4], const RowAt& row) {
-  const int lane = threadIdx.x & 63;
   int id = -1;
   double run = s.before;
 #pragma unroll
@@ -480,14 +548,17 @@ __global__ __launch_bounds__(64) void k_draw(VerifyArgs a) {
   if (!row_counts(a, m)) return;
   if (a.chain) {
     int r0 = 0;
-    if (a.cu) {  // the last request that begins at or before the row
-      int lo = 0, hi = a.n_seq;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.cu[mid] <= m) lo = mid;
-        else hi = mid;
+    if (a.cu) {  // where the last request begins that begins at or before the row: 64 probes at once
+      for (int lo = 0, n = a.n_seq; n > 0;) {  // among cu[lo], ..., cu[lo + n - 1]; cu[0] is one
+        const int gap = (n + 63) / 64, i = lo + lane * gap;
+        const int c = a.cu[min(i, lo + n - 1)];
+        const uint64_t at = __builtin_amdgcn_ballot_w64(i < lo + n && c <= m);
+        const int L = at ? 63 - (int)__builtin_clzll(at) : 0;
+        r0 = max(__builtin_amdgcn_readlane(c, L), 0);
+        n = min(gap - 1, lo + n - 1 - (lo + L * gap));
+        lo += L * gap + 1;
+        if (n > 0 && a.cu[lo] > m) break;  // none of the rest
       }
-      r0 = max(a.cu[lo], 0);
     }
     bool ended = false;
     for (int b = r0; b < m && !ended; b += 64)
@@ -516,8 +587,10 @@ __global__ __launch_bounds__(64) void k_draw(VerifyArgs a) {
     if (real) {
       const Spot s = find_part(a.parts, u, [&](int i) { return a.left[(size_t)m * a.parts + i]; });
       if (s.total > 0.0) {
+        Logits l;
+        l.load(a, m, s.part);
         const Pair d(a, m, x, pow);
-        d.left(a, m, s.part, w, pow);
+        d.left(row, s.part, l, w, pow);
         tok = find_id(s, w, row);
       }
     }
@@ -536,6 +609,8 @@ __global__ __launch_bounds__(64) void k_draw(VerifyArgs a) {
   }
 }
 
+constexpr int kPartWgs = 1280;     // five waves a SIMD
+constexpr int kLeftWaves = 4096;
 static int parts_of(int V) { return (V + 3 + kPartIds - 1) / kPartIds; }  // with up to 3 ids before the row
 
 size_t verify_ws(int M, int V, bool drafts) {
@@ -550,14 +625,18 @@ nmdlm_status launch_verify(const VerifyCall& c, hipStream_t st) {
   PartStat* const p_stat = cv.take<PartStat>(n);
   PartStat* const q_stat = c.draft ? cv.take<PartStat>(n) : nullptr;
   double* const left = c.draft ? cv.take<double>(n) : nullptr;
-  const VerifyArgs a{c.logits, c.draft_logits, c.draft, c.u, c.cu, c.M, c.V, c.n_seq, parts, c.tau, c.draft_tau,
+  const VerifyArgs a{c.logits, c.draft_logits, c.draft, c.u, c.cu, c.M, c.V, c.n_seq, parts, temper(c.tau), temper(c.draft_tau),
                      c.tokens, c.accepted, c.n_accepted, c.conf, p_stat, q_stat, left, c.draft && !c.each};
-  const unsigned wgs = (parts + kPartWaves - 1) / kPartWaves;
-  hipLaunchKernelGGL(k_logit_parts, dim3(wgs, c.M, c.draft_logits ? 2 : 1), dim3(64 * kPartWaves), 0, st, a);
+  // waves to fill the chip once, a few parts each where there are more
+  const long long units = (long long)n * (c.draft_logits ? 2 : 1);
+  const unsigned wgs = (unsigned)std::min<long long>((units + kPartWaves - 1) / kPartWaves, kPartWgs);
+  hipLaunchKernelGGL(k_logit_parts, dim3(wgs), dim3(64 * kPartWaves), 0, st, a);
   nmdlm_status rc = hip_status();
   if (rc != NMDLM_OK) return rc;
   if (c.draft) {
-    hipLaunchKernelGGL(k_verify_left, dim3(wgs, c.M), dim3(64 * kPartWaves), 0, st, a);
+    const int each = (int)std::min<long long>(std::max<long long>(n / kLeftWaves, 1), parts);
+    const unsigned row_wgs = (parts + each * kPartWaves - 1) / (each * kPartWaves);
+    hipLaunchKernelGGL(k_verify_left, dim3(row_wgs, c.M), dim3(64 * kPartWaves), 0, st, a);
     if ((rc = hip_status()) != NMDLM_OK) return rc;
   }
   hipLaunchKernelGGL(k_draw, dim3((unsigned)c.M + (c.n_accepted ? c.n_seq : 0)), dim3(64), 0, st, a);
