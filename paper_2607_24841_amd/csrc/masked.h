@@ -21,9 +21,10 @@ struct MaskedAttnCall {
   void* ws;
 };
 // Rows of a workgroup (1: the row kernel; 16 or 32: tiles), waves a timestep, most
-// splits.
+// splits; heads: workgroups of several heads, whose sums a second kernel joins.
 struct MaskedRoute {
   int tile, parts, splits;
+  bool heads;
 };
 MaskedRoute masked_route(int T, int M, int n_keys, int H);
 size_t masked_attn_ws(int T, int M, int n_keys, int H, int dh);

@@ -6,6 +6,7 @@
 
 #include "attn_device.h"
 #include "masked.h"
+#include "pages.h"
 
 namespace nmdlm {
 
@@ -25,10 +26,11 @@ struct MaskedArgs {
   int32_t* part;  // sums of the splits [row][head][split][T][64 DHW + kMaskedDen]
   int n_keys, max_rows, T, H, parts, splits, max_dist;
   int tile;       // rows that a workgroup takes: 1, 16 or 32
+  bool vec;       // the caches are 16-byte aligned
   int32_t theta;
 };
 constexpr int kMaskedDen = 4;    // the weights' sum behind the channels' sums, and padding
-constexpr int kSplitChunks = 8;  // a split has at least this many chunks
+constexpr int kSplitChunks = 4;  // a split has at least this many chunks
 
 // The keys of two ranges [lo, hi) within [0, n_keys), the empty ones at 0.
 struct KeyRanges {
@@ -65,11 +67,7 @@ __device__ __forceinline__ ChunkList chunk_list(const KeyRanges& k) {
 struct TileKeys {
   KeyRanges hull, all;
 };
-__device__ __forceinline__ int wave_min(int x) {
-  for (int o = 32; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o));
-  return __builtin_amdgcn_readfirstlane(x);
-}
-__device__ __forceinline__ int wave_max(int x) { return ~wave_min(~x); }
+__device__ __forceinline__ int wave_min(int x) { return ~wave_max(~x); }
 __device__ __forceinline__ TileKeys tile_keys(const MaskedArgs& a, int row0, int lane) {
   const int row = row0 + lane % a.tile;
   KeyRanges k = key_ranges(a.ranges[min(row, a.max_rows - 1)], a.n_keys);
@@ -95,8 +93,34 @@ __device__ __forceinline__ int32_t* split_sums(const MaskedArgs& a, int row, int
   return a.part + (((size_t)row * a.H + h) * a.splits + z) * a.T * (64 * DHW + kMaskedDen);
 }
 
+// What a wave of a workgroup takes.  HEADS: up to kHeadWaves heads of one timestep, split
+// and tile, a wave each: their key rows lie in the same 128-byte lines, which the first
+// wave brings into the CU's cache for all (with a head a workgroup the reads of L2, eight
+// times the keys' bytes, set the pace).  Else a head and tile, wave = (timestep, part).
+// Logical ids go head fastest, and the last tiles first, which see most keys where
+// rows see what is before them.
+constexpr int kHeadWaves = 8;
+struct Place {
+  int h, t, z, tile, part, np;
+  bool there;  // the wave has a head
+};
+template <bool HEADS>
+__device__ __forceinline__ Place place(const MaskedArgs& a, int wave, int nwaves) {
+  const int lid = xcd_order(blockIdx.x, gridDim.x), n_tiles = (a.max_rows + a.tile - 1) / a.tile;
+  if constexpr (HEADS) {
+    const int hg = (a.H + nwaves - 1) / nwaves;
+    const int h = (lid % hg) * nwaves + wave, r = lid / hg, tz = r % (a.T * a.splits);
+    return Place{min(h, a.H - 1), tz % a.T, tz / a.T, n_tiles - 1 - r / (a.T * a.splits), 0, 1, h < a.H};
+  } else {
+    const int t = wave / a.parts;
+    return Place{lid % a.H, t, 0, n_tiles - 1 - lid / a.H, wave - t * a.parts, a.parts, true};
+  }
+}
+
 // ---------------------------------------------------------------------------
-// k_masked_rows: one row, head and split; wave = (timestep, part).  Bit by bit:
+// k_masked_rows: single rows.  HEADS: a workgroup takes one timestep and one of the
+// row's splits, wave = head, and leaves the sums to k_masked_join; else one head, wave =
+// (timestep, part), and the neuron.  Bit by bit:
 // lane = key for the scores (popcount of the key's row and the query, the same
 // for all lanes), the weight's eight bits become eight 64-key masks by ballots,
 // and with lane = channel
@@ -104,38 +128,75 @@ __device__ __forceinline__ int32_t* split_sums(const MaskedArgs& a, int row, int
 // A key that the row does not see weighs 0.
 // ---------------------------------------------------------------------------
 constexpr int kRowWaves = 12;  // of a workgroup at most
+constexpr int kRowAhead = 2;   // chunks of a wave on their way
 
 template <int DHW>
+struct RowChunk {
+  uint64_t k[DHW], v[DHW];  // key row `lane`; channels DHW * lane (and + 1)
+  int pos;                  // the key's position (with a bias)
+};
+
+template <int DHW, bool HEADS>
 __global__ __launch_bounds__(64 * kRowWaves) void k_masked_rows(MaskedArgs a) {
   constexpr int DH = 64 * DHW;
+  typedef const ulonglong2 __attribute__((may_alias)) pair;
   __shared__ uint8_t sLut[256];
-  __shared__ int8_t sBias[2 * NMDLM_MAX_DIST + 1];
-  __shared__ int sNum[NMDLM_MAX_T][DH];
+  __shared__ int8_t sBiasAll[HEADS ? kHeadWaves : 1][2 * NMDLM_MAX_DIST + 4];
+  __shared__ int sNum[HEADS ? 1 : NMDLM_MAX_T][DH];
   __shared__ int sDen[NMDLM_MAX_T];
   const int nth = blockDim.x, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nwaves = nth >> 6;
-  // neighbouring heads share key lines: consecutive logical ids, head fastest
-  const int lid = xcd_order(blockIdx.x, gridDim.x);
-  const int h = lid % a.H, z = (lid / a.H) % a.splits, row = lid / (a.H * a.splits);
+  const Place pl = place<HEADS>(a, wave, nwaves);
+  const int h = pl.h, t = pl.t, part = pl.part, np = pl.np, row = pl.tile;
   const KeyRanges kr = key_ranges(a.ranges[row], a.n_keys);
   const ChunkList cl = chunk_list(kr);
-  const int splits = split_count(a, cl.n);
-  if (z >= splits) return;  // uniform
-  const int i0 = split_at(cl.n, z, splits), i1 = split_at(cl.n, z + 1, splits);
-  const int np = a.parts, t = wave / np, part = wave - t * np;
+  const int splits = HEADS ? split_count(a, cl.n) : 1;
+  if (pl.z >= splits) return;  // uniform
+  const int i0 = split_at(cl.n, pl.z, splits);
+  const int i1 = pl.there ? split_at(cl.n, pl.z + 1, splits) : i0;
   const int d = a.H * DH, dw = d / 64;
   const uint64_t* kb = a.kc + (size_t)t * a.cap * dw + h * DHW;
   const uint64_t* vb = a.vt + (size_t)t * (a.cap / 64) * d + h * DH;
   const uint64_t* qp = a.q + ((size_t)t * a.max_rows + row) * dw + h * DHW;
+  auto load = [&](int i) __attribute__((always_inline)) {
+    RowChunk<DHW> r;
+    const int jc = cl.at(min(i, i1 - 1));
+    const uint64_t *kr0 = kb + (size_t)jc * 64 * dw, *vr0 = vb + (size_t)jc * d;
+    if (DHW == 2 && a.vec) {  // uniform
+      const ulonglong2 k = *reinterpret_cast<pair*>(kr0 + (uint32_t)(lane * dw));
+      const ulonglong2 v = *reinterpret_cast<pair*>(vr0 + (uint32_t)(lane * DHW));
+      r.k[0] = k.x;
+      r.k[DHW - 1] = k.y;
+      r.v[0] = v.x;
+      r.v[DHW - 1] = v.y;
+    } else {
+#pragma unroll
+      for (int w = 0; w < DHW; ++w) {
+        r.k[w] = kr0[(uint32_t)(lane * dw + w)];
+        r.v[w] = vr0[(uint32_t)(lane * DHW + w)];
+      }
+    }
+    r.pos = a.bias ? a.k_pos[min(64 * jc + lane, a.n_keys - 1)] : 0;
+    return r;
+  };
+  RowChunk<DHW> ch[kRowAhead];
+  if (i0 < i1) {  // uniform
+#pragma unroll
+    for (int j = 0; j < kRowAhead; ++j) ch[j] = load(i0 + part + j * np);
+  }
   uint64_t q[DHW];
 #pragma unroll
   for (int w = 0; w < DHW; ++w) q[w] = qp[w];
   const int D = a.max_dist, q_pos = a.bias ? a.q_pos[row] : 0;
+  int8_t* const sBias = sBiasAll[HEADS ? wave : 0];
   for (int i = tid; i < 256; i += nth) sLut[i] = a.lut[i];
   if (a.bias)
-    for (int i = tid; i < 2 * D + 1; i += nth) sBias[i] = a.bias[(size_t)h * (2 * D + 1) + i];
-  for (int i = tid; i < a.T * DH; i += nth) (&sNum[0][0])[i] = 0;
-  if (tid < a.T) sDen[tid] = 0;
+    for (int i = HEADS ? lane : tid; i < 2 * D + 1; i += HEADS ? 64 : nth)
+      sBias[i] = a.bias[(size_t)h * (2 * D + 1) + i];
+  if constexpr (!HEADS) {
+    for (int i = tid; i < a.T * DH; i += nth) (&sNum[0][0])[i] = 0;
+    if (tid < a.T) sDen[tid] = 0;
+  }
   __syncthreads();
 
   int acc[8][DHW], den = 0;
@@ -143,54 +204,61 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_masked_rows(MaskedArgs a) {
   for (int b = 0; b < 8; ++b)
 #pragma unroll
     for (int w = 0; w < DHW; ++w) acc[b][w] = 0;
-  for (int i = i0 + part; i < i1; i += np) {  // wave-uniform
-    const int jc = cl.at(i), j = 64 * jc + lane;
-    int s = 0;
-    uint64_t v[DHW];
+  for (int i = i0 + part; i < i1; i += kRowAhead * np) {  // wave-uniform
 #pragma unroll
-    for (int w = 0; w < DHW; ++w) {
-      s += (int)__popcll(kb[(size_t)j * dw + w] & q[w]);
-      v[w] = vb[(size_t)jc * d + w * 64 + lane];
-    }
-    const bool seen = (j >= kr.a0 && j < kr.a1) || (j >= kr.b0 && j < kr.b1);
-    if (a.bias) {
-      const int off = __builtin_elementwise_sub_sat(q_pos, a.k_pos[min(j, a.n_keys - 1)]);
-      s = min(max(s + sBias[min(max(off, -D), D) + D], 0), 255);
-    }
-    const int p = seen ? sLut[s] : 0;
-    den += p;
+    for (int n = 0; n < kRowAhead; ++n) {
+      const int e = i + n * np;
+      if (e < i1) {  // wave-uniform
+        const int j = 64 * cl.at(e) + lane;
+        int s = 0;
 #pragma unroll
-    for (int b = 0; b < 8; ++b) {
-      const uint64_t mask = __builtin_amdgcn_ballot_w64((p >> b) & 1);
+        for (int w = 0; w < DHW; ++w) s += (int)__popcll(ch[n].k[w] & q[w]);
+        const bool seen = (j >= kr.a0 && j < kr.a1) || (j >= kr.b0 && j < kr.b1);
+        if (a.bias) {
+          const int off = __builtin_elementwise_sub_sat(q_pos, ch[n].pos);
+          s = min(max(s + sBias[min(max(off, -D), D) + D], 0), 255);
+        }
+        const int p = seen ? sLut[s] : 0;
+        den += p;
 #pragma unroll
-      for (int w = 0; w < DHW; ++w) acc[b][w] += (int)__popcll(v[w] & mask);
+        for (int b = 0; b < 8; ++b) {
+          const uint64_t mask = __builtin_amdgcn_ballot_w64((p >> b) & 1);
+#pragma unroll
+          for (int w = 0; w < DHW; ++w) acc[b][w] += (int)__popcll(ch[n].v[w] & mask);
+        }
+        ch[n] = load(e + kRowAhead * np);
+      }
     }
   }
-  for (int o = 32; o > 0; o >>= 1) den += __shfl_xor(den, o);
-  if (lane == 0) atomicAdd(&sDen[t], den);
+  den = wave_sum(den);
+  int num[DHW];
 #pragma unroll
   for (int w = 0; w < DHW; ++w) {
-    int x = 0;
+    num[w] = 0;
 #pragma unroll
-    for (int b = 7; b >= 0; --b) x = 2 * x + acc[b][w];
-    atomicAdd(&sNum[t][64 * w + lane], x);
+    for (int b = 7; b >= 0; --b) num[w] = 2 * num[w] + acc[b][w];
   }
-  __syncthreads();
-  if (splits > 1) {  // uniform
-    int32_t* o = split_sums<DHW>(a, row, h, z);
-    for (int i = tid; i < a.T * DH; i += nth) o[(i / DH) * (DH + kMaskedDen) + i % DH] = (&sNum[0][0])[i];
-    if (tid < a.T) o[tid * (DH + kMaskedDen) + DH] = sDen[tid];
+  if constexpr (HEADS) {
+    if (!pl.there) return;  // wave-uniform
+    int32_t* o = split_sums<DHW>(a, row, h, pl.z) + (size_t)t * (DH + kMaskedDen);
+#pragma unroll
+    for (int w = 0; w < DHW; ++w) o[DHW * lane + w] = num[w];
+    if (lane == 0) o[DH] = den;
     return;
   }
+  if (lane == 0) atomicAdd(&sDen[t], den);
+#pragma unroll
+  for (int w = 0; w < DHW; ++w) atomicAdd(&sNum[HEADS ? 0 : t][DHW * lane + w], num[w]);
+  __syncthreads();
   for (int w = wave; w < DHW; w += nwaves)
-    fire_row<DHW>(a, row, h, w, lane, a.n_keys < 65536, [&](int tt) { return sNum[tt][w * 64 + lane]; },
+    fire_row<DHW>(a, row, h, w, lane, a.n_keys < 65536, [&](int tt) { return sNum[HEADS ? 0 : tt][w * 64 + lane]; },
                   [&](int tt) { return sDen[tt]; });
 }
 
 // ---------------------------------------------------------------------------
-// k_masked_tiles: a tile of 16*QG rows, a head and one of the tile's splits; wave =
-// (timestep, part), the sums and the pipeline of attn_device.h over the chunks
-// that any row of the tile sees.  A chunk that not all of them see whole is
+// k_masked_tiles: a tile of 16*QG rows, the sums and the pipeline of attn_device.h over the
+// chunks that any row of the tile sees.  HEADS: wave = head of one timestep and split,
+// the sums go to k_masked_join; else wave = (timestep, part) of one head, and the neuron.  A chunk that not all of them see whole is
 // masked: a lane (one row, 16 keys) makes the bits of its keys from the row's
 // ranges, and the weights of the others become 0 (byte -128).  The values of the
 // keys past n_keys in the last chunk then count with weight 0 too.
@@ -198,9 +266,19 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_masked_rows(MaskedArgs a) {
 // Bias: the scores' sums begin with 8 * bias, so it costs no instruction behind the
 // products; the table is extended by 128 entries below and above, which clamps.  A
 // chunk whose keys are all at least max_dist before (or behind) all rows of the tile
-// has one bias for all pairs.
+// has one bias for all pairs.  Where a chunk's positions are consecutive a lane's 16
+// keys take 16 consecutive entries of the bias, reversed and extended by 16 on each
+// side: one clamped index for all of them.
 // ---------------------------------------------------------------------------
 constexpr int kWideEntries = 384;  // scores -128 .. 255
+constexpr int kBiasPad = 16;
+// How a staged chunk's keys lie to the rows: all max_dist or more before or behind, at
+// positions in a row from `base` on, or anyhow.
+enum Side : int { SIDE_ANY, SIDE_ROW, SIDE_BEFORE, SIDE_BEHIND };
+struct ChunkSide {
+  Side side;
+  int base;
+};
 struct WideLut {
   int e[2][kWideEntries][2];
 };
@@ -238,7 +316,7 @@ __device__ __forceinline__ uint32_t bits16(int lo, int hi) {
   return ((1u << min(max(hi, 0), 16)) - 1u) & ~((1u << min(max(lo, 0), 16)) - 1u);
 }
 
-template <int DHW, int QG, bool BIAS>
+template <int DHW, int QG, bool BIAS, bool HEADS>
 __global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_masked_tiles(MaskedArgs a) {
   constexpr int NT = DHW * 4, DH = DHW * 64;
   constexpr int kHalf = (BIAS ? kWideEntries : kLutEntries) * 8;  // bytes of half a table
@@ -246,21 +324,16 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_masked_ti
   __shared__ int sDen[NMDLM_MAX_T][16];  // [part][T], at most eight waves
   __shared__ uint32_t sWord[NMDLM_MAX_T][16][2 * DHW];
   __shared__ int sPos[BIAS ? NMDLM_MAX_T * kAttnStages : 1][64];  // positions of the staged keys
-  // the waves' stages, then their sums [part][T][NT][64]; behind them 8 * bias
+  // the waves' stages, then (without HEADS) their sums [part][T][NT][64]; behind them 8 * bias
   extern __shared__ v4i sNum[];
   AttnStage<DHW>* sStage = reinterpret_cast<AttnStage<DHW>*>(sNum);
 
   const int nth = blockDim.x, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nwaves = nth >> 6;
   const int g = lane >> 4, c = lane & 15;
-  // neighbouring heads share key lines: consecutive logical ids, head fastest; the
-  // last tiles first, which see most keys where rows see what is before them
-  const int lid = xcd_order(blockIdx.x, gridDim.x);
-  const int h = lid % a.H, z = (lid / a.H) % a.splits;
-  const int n_tiles = (a.max_rows + 16 * QG - 1) / (16 * QG);
-  const int row0 = (n_tiles - 1 - lid / (a.H * a.splits)) * 16 * QG;
+  const Place pl = place<HEADS>(a, wave, nwaves);
+  const int h = pl.h, t = pl.t, part = pl.part, np = pl.np, row0 = pl.tile * 16 * QG;
   const int nr = min(a.max_rows - row0, 16 * QG);
-  const int np = a.parts, t = wave / np, part = wave - t * np;
   const int d = a.H * DH, dw = d / 64, D = a.max_dist;
   const uint64_t* kb = a.kc + (size_t)t * a.cap * dw + h * DHW;
   const uint64_t* vb = a.vt + (size_t)t * (a.cap / 64) * d + h * DH;
@@ -277,11 +350,15 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_masked_ti
   }
   const TileKeys tk = tile_keys(a, row0, lane);
   const ChunkList cl = chunk_list(tk.hull);
-  const int splits = split_count(a, cl.n);
-  if (z >= splits) return;  // uniform
-  const int i0 = split_at(cl.n, z, splits), i1 = split_at(cl.n, z + 1, splits);
-  int* const sBias = reinterpret_cast<int*>(sNum + nwaves * NT * 64);
+  const int splits = HEADS ? split_count(a, cl.n) : 1;
+  if (pl.z >= splits) return;  // uniform
+  const int i0 = split_at(cl.n, pl.z, splits);
+  const int i1 = pl.there ? split_at(cl.n, pl.z + 1, splits) : i0;
+  int* const sBias = HEADS ? reinterpret_cast<int*>(sStage + kAttnStages * nwaves) + wave * (2 * D + 2 * kBiasPad)
+                           : reinterpret_cast<int*>(sNum + nwaves * NT * 64);
   int q_lo = 0, q_hi = 0;
+  constexpr int kSmallPos = 1 << 29;  // differences of such positions fit
+  bool small_pos = true;
   if constexpr (BIAS) {
     q_lo = q_hi = qp[0];
 #pragma unroll
@@ -291,7 +368,9 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_masked_ti
     }
     q_lo = wave_min(q_lo);
     q_hi = wave_max(q_hi);
-    for (int i = tid; i < 2 * D + 1; i += nth) sBias[i] = 8 * a.bias[(size_t)h * (2 * D + 1) + i];
+    small_pos = q_lo >= -kSmallPos && q_hi <= kSmallPos;
+    for (int i = HEADS ? lane : tid; i < 2 * D + 2 * kBiasPad; i += HEADS ? 64 : nth)  // entry i: key behind the row by i - D - kBiasPad
+      sBias[i] = 8 * a.bias[(size_t)h * (2 * D + 1) + min(max(D + kBiasPad - i, -D), D) + D];
     for (int i = tid; i < kWideEntries; i += nth) {
       const uint32_t v = (uint32_t)a.lut[min(max(i - 128, 0), 255)] ^ 0x80u;
 #pragma unroll
@@ -316,47 +395,58 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_masked_ti
       AttnWave<DHW, QG>::load(ch, kb, vb, dw, d, jc, lane);
       if constexpr (BIAS) kp = a.k_pos[min(64 * jc + lane, a.n_keys - 1)];
     };
-    // returns the side of the chunk: 1 all keys max_dist or more before the rows, -1
-    // behind, 0 between
-    auto put = [&](const AttnChunk<DHW>& ch, AttnStage<DHW>& s, int slot) {
-      int side = 0;
+    auto put = [&](const AttnChunk<DHW>& ch, AttnStage<DHW>& s, int slot, int jc) {
+      ChunkSide cs{SIDE_ANY, 0};
       if constexpr (BIAS) {
+        cs.base = __builtin_amdgcn_readfirstlane(kp);
         const bool before = __builtin_elementwise_sub_sat(q_lo, kp) >= D;
         const bool behind = __builtin_elementwise_sub_sat(q_hi, kp) <= -D;
-        side = __builtin_amdgcn_ballot_w64(before) == ~0ull ? 1
-               : __builtin_amdgcn_ballot_w64(behind) == ~0ull ? -1 : 0;
-        sPos[kAttnStages * wave + slot][lane] = kp;
+        const bool in_row = kp - lane == cs.base || 64 * jc + lane >= a.n_keys;
+        if (__builtin_amdgcn_ballot_w64(before) == ~0ull) cs.side = SIDE_BEFORE;
+        else if (__builtin_amdgcn_ballot_w64(behind) == ~0ull) cs.side = SIDE_BEHIND;
+        else if (small_pos && cs.base == max(min(cs.base, kSmallPos), -kSmallPos) &&
+                 __builtin_amdgcn_ballot_w64(in_row) == ~0ull)
+          cs.side = SIDE_ROW;
+        else
+          sPos[kAttnStages * wave + slot][lane] = kp;
       }
       w.put(ch, s, lane);
-      return side;
+      return cs;
     };
     v4i s[QG][4], p[QG];
-    auto biased = [&](int slot, int side) {  // what the scores begin with
-      if constexpr (BIAS) {
-        if (side != 0) {  // wave-uniform
-          const int b = sBias[side > 0 ? 2 * D : 0];
+    auto biased = [&](int slot, ChunkSide cs) {  // what the scores begin with
+      if (cs.side == SIDE_BEFORE || cs.side == SIDE_BEHIND) {  // wave-uniform
+        const int b = sBias[cs.side == SIDE_BEFORE ? kBiasPad : 2 * D + kBiasPad];
+#pragma unroll
+        for (int u = 0; u < QG; ++u)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) s[u][k] = v4i{b, b, b, b};
+      } else if (cs.side == SIDE_ROW) {
+#pragma unroll
+        for (int u = 0; u < QG; ++u) {
+          const int* b = sBias + min(max(cs.base + 16 * g - qp[u], -D - kBiasPad), D) + D + kBiasPad;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[u][k][e] = b[4 * k + e];
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const v4i pos = *reinterpret_cast<const v4i*>(&sPos[kAttnStages * wave + slot][16 * g + 4 * k]);
 #pragma unroll
           for (int u = 0; u < QG; ++u)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s[u][k] = v4i{b, b, b, b};
-        } else {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const v4i pos = *reinterpret_cast<const v4i*>(&sPos[kAttnStages * wave + slot][16 * g + 4 * k]);
-#pragma unroll
-            for (int u = 0; u < QG; ++u)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int off = __builtin_elementwise_sub_sat(qp[u], pos[e]);
-                s[u][k][e] = sBias[min(max(off, -D), D) + D];
-              }
-          }
+            for (int e = 0; e < 4; ++e) {
+              const int off = __builtin_elementwise_sub_sat(pos[e], qp[u]);
+              s[u][k][e] = sBias[min(max(off, -D), D) + D + kBiasPad];
+            }
         }
       }
     };
-    auto score = [&](const uint32_t (&k)[4], int slot, int side) {
+    auto score = [&](const uint32_t (&k)[4], int slot, ChunkSide cs) {
       if constexpr (BIAS) {
-        biased(slot, side);
+        biased(slot, cs);
         add_scores<DHW, QG>(w.q, k, s);
       } else {
         w.scores(k, s);
@@ -388,10 +478,10 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_masked_ti
     AttnChunk<DHW> first, next;
     int i = i0 + part, s0 = 0, s1 = 1, s2 = 2;  // the stages of chunks i - np, i, i + np
     load(first, chunk_at(i));
-    int d0 = put(first, st[s0], s0), d1, d2;  // their sides
+    ChunkSide d0 = put(first, st[s0], s0, chunk_at(i)), d1, d2;  // how they lie
     load(next, chunk_at(i + np));
     w.key_pieces(st[s0], k, g, c);
-    d1 = put(next, st[s1], s1);
+    d1 = put(next, st[s1], s1, chunk_at(i + np));
     load(next, chunk_at(i + 2 * np));
     score(k, s0, d0);
     lookup();
@@ -403,7 +493,7 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_masked_ti
       score(k, s1, d1);
       __builtin_amdgcn_sched_barrier(0);
       lookup();
-      d2 = put(next, st[s2], s2);
+      d2 = put(next, st[s2], s2, chunk_at(i + np));
       load(next, chunk_at(i + 2 * np));
       w.key_pieces(st[s2], k, g, c);
       keys += 64;
@@ -422,6 +512,18 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_masked_ti
     w.weigh(v, p);
   }
   w.finish(reinterpret_cast<char*>(st), lane, g, c);
+  if constexpr (HEADS) {
+    if (!pl.there) return;  // wave-uniform
+#pragma unroll
+    for (int u = 0; u < QG; ++u)
+      if (16 * u + c < nr) {
+        int32_t* o = split_sums<DHW>(a, row0 + 16 * u + c, h, pl.z) + (size_t)t * (DH + kMaskedDen);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) *reinterpret_cast<v4i*>(o + 16 * n + 4 * g) = w.acc[u][n];
+        if (g == 0) o[DH] = w.den[u] + 128 * keys;
+      }
+    return;
+  }
   __syncthreads();  // the stages are read
 
 #pragma unroll
@@ -432,52 +534,45 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_masked_ti
     for (int n = 0; n < NT; ++n) sNum[(pt * NT + n) * 64 + lane] = w.acc[u][n];
     if (g == 0) sDen[pt][c] = w.den[u] + 128 * keys;
     __syncthreads();
-    if (splits > 1) {  // uniform
-      for (int i = tid; i < a.T * NT * 64; i += nth) {
-        const int tt = i / (NT * 64), n = (i >> 6) % NT, r = i & 15, lg = (i >> 4) & 3;
-        if (r < rows) {
-          v4i x = sNum[i];
-          for (int p = 1; p < np; ++p) x += sNum[p * a.T * NT * 64 + i];
-          *reinterpret_cast<v4i*>(split_sums<DHW>(a, row0 + 16 * u + r, h, z) +
-                                  (size_t)tt * (DH + kMaskedDen) + 16 * n + 4 * lg) = x;
-        }
-      }
-      for (int i = tid; i < a.T * 16; i += nth)
-        if (i % 16 < rows) {
-          int den = 0;
-          for (int p = 0; p < np; ++p) den += sDen[p * a.T + i / 16][i % 16];
-          split_sums<DHW>(a, row0 + 16 * u + i % 16, h, z)[(size_t)(i / 16) * (DH + kMaskedDen) + DH] = den;
-        }
-      continue;
-    }
     if (rows <= 0) continue;  // uniform
     fire_rows<DHW>(a, sNum, sDen, sWord, row0 + 16 * u, min(rows, 16), h, a.n_keys < 65536, tid, nth);
   }
 }
 
 // k_masked_join: the sums of a row's splits (integers: any order gives the same)
-// and the neuron.  A workgroup per row and head, a wave per timestep and 64
-// channels.
+// and the neuron.  A workgroup per row and head, kJoinWaves / (T DHW) waves for each
+// timestep and 64 channels, which take the splits in turn, sixteen loads at once.
+constexpr int kJoinWaves = 16;
 template <int DHW>
-__global__ __launch_bounds__(64 * NMDLM_MAX_T * DHW) void k_masked_join(MaskedArgs a) {
+__global__ __launch_bounds__(64 * kJoinWaves) void k_masked_join(MaskedArgs a) {
   constexpr int LD = 64 * DHW + kMaskedDen;
   __shared__ int sNum[NMDLM_MAX_T][64 * DHW];
   __shared__ int sDen[NMDLM_MAX_T];
   const int h = blockIdx.x % a.H, row = blockIdx.x / a.H;
-  const int lane = threadIdx.x & 63;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tw = a.T * DHW, nz = (int)blockDim.x / 64 / tw;  // waves of a timestep's 64 channels
+  const int t = wave % tw / DHW, w = wave % DHW, z0 = wave / tw;
+  for (int i = tid; i < a.T * 64 * DHW; i += blockDim.x) (&sNum[0][0])[i] = 0;
   const int n = split_count(a, chunk_list(tile_keys(a, row - row % a.tile, lane).hull).n);
-  if (n == 1) return;  // uniform; a single split fired by itself
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int t = wave / DHW, w = wave - t * DHW;
   const int32_t* base = split_sums<DHW>(a, row, h, 0) + (size_t)t * LD;
   const size_t ld = (size_t)a.T * LD;
-  int x = 0, den = 0;
-  for (int z = 0; z < n; ++z) {
-    x += base[z * ld + w * 64 + lane];
-    den += base[z * ld + 64 * DHW];
+  int den = 0;
+  if (w == 0 && z0 == 0)  // wave-uniform
+    for (int z = lane; z < n; z += 64) den += base[z * ld + 64 * DHW];
+  int x = 0;
+  for (int z = z0; z < n; z += 16 * nz) {
+    int v[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] = base[min(z + k * nz, n - 1) * ld + w * 64 + lane];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) x += z + k * nz < n ? v[k] : 0;
   }
-  sNum[t][w * 64 + lane] = x;
-  if (w == 0 && lane == 0) sDen[t] = den;
+  __syncthreads();
+  atomicAdd(&sNum[t][w * 64 + lane], x);
+  if (w == 0 && z0 == 0) {
+    den = wave_sum(den);
+    if (lane == 0) sDen[t] = den;
+  }
   __syncthreads();
   if (wave < DHW)
     fire_row<DHW>(a, row, h, wave, lane, a.n_keys < 65536,
@@ -485,34 +580,56 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T * DHW) void k_masked_join(MaskedAr
 }
 
 MaskedRoute masked_route(int T, int M, int n_keys, int H) {
-  MaskedRoute r{1, T <= 2 ? 4 : (T <= 4 ? 2 : 1), 1};
+  MaskedRoute r{1, T <= 2 ? 4 : (T <= 4 ? 2 : 1), 1, false};
   if (M > 2) r.tile = M >= 32 && (long long)(M / 32) * H * T >= 1024 ? 32 : 16;
   if (r.tile == 1) r.parts = std::max(std::min(kRowWaves / T, 4), 1);
   if (r.tile == 32) r.parts = 1;
-  const long long units = (long long)((M + r.tile - 1) / r.tile) * H;
-  r.splits = (int)std::max(1LL, std::min<long long>({(r.tile == 1 ? 512 : 256) / units, 64,
+  const long long wgs = (long long)((M + r.tile - 1) / r.tile) * H;
+  if (wgs >= 128 || n_keys < 2 * 64 * kSplitChunks) return r;
+  r.heads = true;
+  r.parts = 1;
+  if (r.tile > 1) r.tile = ((M + 15) / 16) * 155 <= ((M + 31) / 32) * 200 ? 16 : 32;
+  const long long units = (long long)((M + r.tile - 1) / r.tile) * ((H + kHeadWaves - 1) / kHeadWaves) * T;
+  r.splits = (int)std::max(1LL, std::min<long long>({(r.tile == 32 ? 256 : 512) / units, 64,
                                                      n_keys / (64 * kSplitChunks)}));
   return r;
 }
 
 size_t masked_attn_ws(int T, int M, int n_keys, int H, int dh) {
   const MaskedRoute r = masked_route(T, M, n_keys, H);
-  if (r.splits == 1) return 0;
+  if (!r.heads) return 0;
   return align_up((size_t)M * H * r.splits * T * (dh + kMaskedDen) * sizeof(int32_t), 256);
 }
 
 constexpr size_t kMaskedPlainLds = 32768;  // dynamic LDS that needs no attribute beside the static
 
-template <int DHW, int QG, bool BIAS>
-static nmdlm_status launch_tiles(const MaskedArgs& a, unsigned grid, hipStream_t st) {
-  size_t dyn = (size_t)a.T * a.parts * std::max(DHW * 4 * 64 * sizeof(v4i), kAttnStages * sizeof(AttnStage<DHW>));
-  if (BIAS) dyn += (2 * a.max_dist + 1) * sizeof(int);
+template <int DHW, int QG, bool BIAS, bool HEADS>
+static nmdlm_status launch_tiles(const MaskedArgs& a, unsigned grid, int waves, hipStream_t st) {
+  size_t dyn = (size_t)waves * (HEADS ? kAttnStages * sizeof(AttnStage<DHW>) : DHW * 4 * 64 * sizeof(v4i));
+  static_assert(DHW * 4 * 64 * sizeof(v4i) >= kAttnStages * sizeof(AttnStage<DHW>), "sums over the stages");
+  if (BIAS) dyn += (size_t)(HEADS ? waves : 1) * (2 * a.max_dist + 2 * kBiasPad) * sizeof(int);
   if (dyn > kMaskedPlainLds &&
-      hipFuncSetAttribute(reinterpret_cast<const void*>(&k_masked_tiles<DHW, QG, BIAS>),
+      hipFuncSetAttribute(reinterpret_cast<const void*>(&k_masked_tiles<DHW, QG, BIAS, HEADS>),
                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)dyn) != hipSuccess)
     return NMDLM_ERR_HIP;
-  hipLaunchKernelGGL((k_masked_tiles<DHW, QG, BIAS>), dim3(grid), dim3(64 * a.T * a.parts), (uint32_t)dyn, st, a);
+  hipLaunchKernelGGL((k_masked_tiles<DHW, QG, BIAS, HEADS>), dim3(grid), dim3(64 * waves), (uint32_t)dyn, st, a);
   return hip_status();
+}
+
+template <int DHW, bool HEADS>
+static nmdlm_status launch_masked(const MaskedArgs& a, hipStream_t st) {
+  const int waves = HEADS ? std::min(a.H, kHeadWaves) : a.T * a.parts;
+  const unsigned tiles = (a.max_rows + a.tile - 1) / a.tile;
+  const unsigned grid = HEADS ? tiles * ((a.H + waves - 1) / waves) * a.T * a.splits : tiles * a.H;
+  if (a.tile == 1) {
+    hipLaunchKernelGGL((k_masked_rows<DHW, HEADS>), dim3(grid), dim3(64 * waves), 0, st, a);
+    return hip_status();
+  }
+  if (a.tile == 16)
+    return a.bias ? launch_tiles<DHW, 1, true, HEADS>(a, grid, waves, st)
+                  : launch_tiles<DHW, 1, false, HEADS>(a, grid, waves, st);
+  return a.bias ? launch_tiles<DHW, 2, true, HEADS>(a, grid, waves, st)
+                : launch_tiles<DHW, 2, false, HEADS>(a, grid, waves, st);
 }
 
 template <int DHW>
@@ -521,19 +638,14 @@ static nmdlm_status launch_masked_dh(const MaskedAttnCall& c, hipStream_t st) {
   const MaskedArgs a{c.q, c.k_cache, c.vt_cache, c.cap, reinterpret_cast<const int4*>(c.mask.ranges),
                      c.mask.q_pos, c.mask.k_pos, c.bias, c.lut, c.a_out, c.s_out, c.u_out,
                      static_cast<int32_t*>(c.ws), c.n_keys, c.M, c.T, c.H, r.parts, r.splits,
-                     c.bias ? c.mask.max_dist : 0, r.tile, c.theta};
-  const unsigned grid = (unsigned)((c.M + r.tile - 1) / r.tile) * c.H * r.splits;
-  nmdlm_status rc;
-  if (r.tile == 1) {
-    hipLaunchKernelGGL(k_masked_rows<DHW>, dim3(grid), dim3(64 * c.T * r.parts), 0, st, a);
-    rc = hip_status();
-  } else if (r.tile == 16) {
-    rc = c.bias ? launch_tiles<DHW, 1, true>(a, grid, st) : launch_tiles<DHW, 1, false>(a, grid, st);
-  } else {
-    rc = c.bias ? launch_tiles<DHW, 2, true>(a, grid, st) : launch_tiles<DHW, 2, false>(a, grid, st);
-  }
-  if (rc != NMDLM_OK || r.splits == 1) return rc;
-  hipLaunchKernelGGL(k_masked_join<DHW>, dim3((unsigned)c.M * c.H), dim3(64 * c.T * DHW), 0, st, a);
+                     c.bias ? c.mask.max_dist : 0, r.tile,
+                     ((reinterpret_cast<uintptr_t>(c.k_cache) | reinterpret_cast<uintptr_t>(c.vt_cache)) & 15) == 0,
+                     c.theta};
+  if (!r.heads) return launch_masked<DHW, false>(a, st);
+  const nmdlm_status rc = launch_masked<DHW, true>(a, st);
+  if (rc != NMDLM_OK) return rc;
+  const int tw = c.T * DHW, nz = std::max(1, std::min(kJoinWaves / tw, (r.splits + 15) / 16));
+  hipLaunchKernelGGL(k_masked_join<DHW>, dim3((unsigned)c.M * c.H), dim3(64 * tw * nz), 0, st, a);
   return hip_status();
 }
 

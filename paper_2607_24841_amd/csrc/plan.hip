@@ -88,12 +88,13 @@ void nmdlm_internal_paged_route(int n_seq, int max_rows, int max_pages, int T, i
 }
 
 // The route of a masked attention call: rows of a workgroup (1: the row kernel),
-// waves per timestep, most splits.
+// waves per timestep, most splits, 1 when a workgroup takes several heads.
 void nmdlm_internal_masked_route(int T, int M, int n_keys, int H, int32_t* out) {
   const MaskedRoute r = masked_route(T, M, n_keys, H);
   out[0] = r.tile;
   out[1] = r.parts;
   out[2] = r.splits;
+  out[3] = r.heads ? 1 : 0;
 }
 
 // The runs of row block y of M tokens into out[4 i ..]: sequence, first position,

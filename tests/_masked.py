@@ -63,14 +63,14 @@ def make_case(seed, ranges, q_pos, n_keys, T=4, H=2, dh=64, max_dist=None, rate=
 
 def route(T, M, n_keys, H):
     """The kernel a call takes (a host-side query): rows of a workgroup (1: the row
-    kernel), waves per timestep, most splits."""
+    kernel), waves per timestep, most splits, whether workgroups take several heads."""
     import ctypes as C
 
     from paper_2607_24841_amd import binding as B
 
-    out = (C.c_int32 * 3)()
+    out = (C.c_int32 * 4)()
     B.load().nmdlm_internal_masked_route(T, M, n_keys, H, out)
-    return SimpleNamespace(tile=out[0], parts=out[1], splits=out[2])
+    return SimpleNamespace(tile=out[0], parts=out[1], splits=out[2], heads=bool(out[3]))
 
 
 def attention(c):

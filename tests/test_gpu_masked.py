@@ -66,14 +66,28 @@ def test_tiles_of_32_rows(dh, max_dist):
     check(K.make_case(dh, r, pos, 400, T=8, H=16, dh=dh, max_dist=max_dist))
 
 
-@pytest.mark.parametrize("T, M, n_keys, H, tile, split", [(4, 1, 300, 2, 1, False), (4, 2, 3000, 2, 1, True),
-                                                          (4, 3, 300, 2, 16, False), (2, 40, 5000, 1, 16, True)])
-def test_routes_of_small_calls(T, M, n_keys, H, tile, split):
-    """The kernels that the sizes of these tests reach."""
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("max_dist", [None, 33])
+@pytest.mark.parametrize("T, M, n_keys, H, tile, heads", [(4, 1, 300, 2, 1, False), (4, 2, 3000, 2, 1, True),
+                                                          (4, 3, 300, 2, 16, False), (2, 12, 5000, 1, 16, True),
+                                                          (3, 30, 1500, 11, 32, True), (4, 40, 700, 9, 32, True),
+                                                          (2, 1, 9000, 13, 1, True), (8, 70, 1200, 3, 32, True)])
+def test_routes_of_small_calls(T, M, n_keys, H, tile, heads, max_dist, dh):
+    """The kernels that the sizes of these tests reach, heads that do not fill a workgroup."""
     r = K.route(T, M, n_keys, H)
-    assert (r.tile, r.splits > 1) == (tile, split)
+    assert (r.tile, r.heads) == (tile, heads)
     pos = n_keys - M + np.arange(M)
-    check(K.make_case(M, np.stack([0 * pos, pos + 1, 0 * pos, 0 * pos], 1), pos, n_keys, T=T, H=H, max_dist=33))
+    ranges = np.stack([0 * pos, pos + 1, 0 * pos, 0 * pos], 1)
+    ranges[M // 2] = 0   # sees nothing
+    ranges[-1] = 70, 70 + n_keys // 3, n_keys - 5, n_keys
+    check(K.make_case(M, ranges, pos, n_keys, T=T, H=H, dh=dh, max_dist=max_dist))
+
+
+def test_one_split_of_several():
+    """A route of several splits whose rows see too little for more than one, or nothing."""
+    assert K.route(4, 20, 4000, 2).splits > 4
+    for r in ((0, 0, 0, 0), (100, 130, 3900, 3990), (0, 4000, 0, 0)):
+        check(K.make_case(1, np.tile([r], (20, 1)), np.full(20, 4000), 4000, max_dist=8))
 
 
 def test_documents_and_rows_of_none():
