@@ -101,19 +101,19 @@ __device__ __forceinline__ int32_t* split_sums(const MaskedArgs& a, int row, int
 // rows see what is before them.
 constexpr int kHeadWaves = 8;
 struct Place {
-  int h, t, z, tile, part, np;
-  bool there;  // the wave has a head
+  int h, h0, t, z, tile, part, np;  // h0: the workgroup's first head
+  bool there;                       // the wave has a head
 };
 template <bool HEADS>
 __device__ __forceinline__ Place place(const MaskedArgs& a, int wave, int nwaves) {
   const int lid = xcd_order(blockIdx.x, gridDim.x), n_tiles = (a.max_rows + a.tile - 1) / a.tile;
   if constexpr (HEADS) {
     const int hg = (a.H + nwaves - 1) / nwaves;
-    const int h = (lid % hg) * nwaves + wave, r = lid / hg, tz = r % (a.T * a.splits);
-    return Place{min(h, a.H - 1), tz % a.T, tz / a.T, n_tiles - 1 - r / (a.T * a.splits), 0, 1, h < a.H};
+    const int h0 = (lid % hg) * nwaves, h = h0 + wave, r = lid / hg, tz = r % (a.T * a.splits);
+    return Place{min(h, a.H - 1), h0, tz % a.T, tz / a.T, n_tiles - 1 - r / (a.T * a.splits), 0, 1, h < a.H};
   } else {
     const int t = wave / a.parts;
-    return Place{lid % a.H, t, 0, n_tiles - 1 - lid / a.H, wave - t * a.parts, a.parts, true};
+    return Place{lid % a.H, lid % a.H, t, 0, n_tiles - 1 - lid / a.H, wave - t * a.parts, a.parts, true};
   }
 }
 
@@ -126,24 +126,43 @@ __device__ __forceinline__ Place place(const MaskedArgs& a, int wave, int nwaves
 // and with lane = channel
 //     sum_j p_j V[j,c] = sum_b 2^b popcount(mask_b AND word of channel c).
 // A key that the row does not see weighs 0.
+//
+// HEADS: the waves bring a chunk's key rows into LDS together, 8 rows of all their heads
+// each, one barrier a chunk, two buffers.  (Each wave reading its own pieces counted
+// on the CU's cache to keep the lines for the others: 80 us a call of 130 thousand keys, 16
+// heads of 128, T = 4, where 92 with four chunks of loads on their way in place of two: they
+// no longer fitted.)
 // ---------------------------------------------------------------------------
 constexpr int kRowWaves = 12;  // of a workgroup at most
-constexpr int kRowAhead = 2;   // chunks of a wave on their way
 
 template <int DHW>
-struct RowChunk {
-  uint64_t k[DHW], v[DHW];  // key row `lane`; channels DHW * lane (and + 1)
-  int pos;                  // the key's position (with a bias)
+struct RowValues {
+  uint64_t v[DHW];  // channels DHW * lane (and + 1)
+  int pos;          // the position of key `lane` (with a bias)
 };
+// DHW words from 8-byte aligned memory, at once where vec says that it is 16-byte aligned
+template <int DHW>
+__device__ __forceinline__ void load_words(uint64_t (&r)[DHW], const uint64_t* p, bool vec) {
+  typedef const ulonglong2 __attribute__((may_alias)) pair;
+  if (DHW == 2 && vec) {  // uniform
+    const ulonglong2 x = *reinterpret_cast<pair*>(p);
+    r[0] = x.x;
+    r[DHW - 1] = x.y;
+  } else {
+#pragma unroll
+    for (int w = 0; w < DHW; ++w) r[w] = p[w];
+  }
+}
 
 template <int DHW, bool HEADS>
 __global__ __launch_bounds__(64 * kRowWaves) void k_masked_rows(MaskedArgs a) {
   constexpr int DH = 64 * DHW;
-  typedef const ulonglong2 __attribute__((may_alias)) pair;
+  constexpr int kKeyLd = DHW * (kHeadWaves + 1);  // words of a key in LDS, a head of padding
   __shared__ uint8_t sLut[256];
   __shared__ int8_t sBiasAll[HEADS ? kHeadWaves : 1][2 * NMDLM_MAX_DIST + 4];
   __shared__ int sNum[HEADS ? 1 : NMDLM_MAX_T][DH];
   __shared__ int sDen[NMDLM_MAX_T];
+  __shared__ __attribute__((aligned(16))) uint64_t sKeys[HEADS ? 2 : 1][HEADS ? 64 * kKeyLd : 1];
   const int nth = blockDim.x, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nwaves = nth >> 6;
   const Place pl = place<HEADS>(a, wave, nwaves);
@@ -152,37 +171,55 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_masked_rows(MaskedArgs a) {
   const ChunkList cl = chunk_list(kr);
   const int splits = HEADS ? split_count(a, cl.n) : 1;
   if (pl.z >= splits) return;  // uniform
-  const int i0 = split_at(cl.n, pl.z, splits);
-  const int i1 = pl.there ? split_at(cl.n, pl.z + 1, splits) : i0;
+  const int i0 = split_at(cl.n, pl.z, splits), i1 = split_at(cl.n, pl.z + 1, splits);
   const int d = a.H * DH, dw = d / 64;
-  const uint64_t* kb = a.kc + (size_t)t * a.cap * dw + h * DHW;
+  const uint64_t* kt = a.kc + (size_t)t * a.cap * dw;
   const uint64_t* vb = a.vt + (size_t)t * (a.cap / 64) * d + h * DH;
   const uint64_t* qp = a.q + ((size_t)t * a.max_rows + row) * dw + h * DHW;
-  auto load = [&](int i) __attribute__((always_inline)) {
-    RowChunk<DHW> r;
+  // HEADS: key row `wave * 8 + lane / 8` (of eight waves) of head `lane % 8` of the group, for
+  // all of the workgroup's waves; else the wave's own, row `lane`
+  const int my_head = HEADS ? min(pl.h0 + lane % kHeadWaves, a.H - 1) : h;
+  auto load_keys = [&](uint64_t (&k)[DHW], int i, int row8) __attribute__((always_inline)) {
     const int jc = cl.at(min(i, i1 - 1));
-    const uint64_t *kr0 = kb + (size_t)jc * 64 * dw, *vr0 = vb + (size_t)jc * d;
-    if (DHW == 2 && a.vec) {  // uniform
-      const ulonglong2 k = *reinterpret_cast<pair*>(kr0 + (uint32_t)(lane * dw));
-      const ulonglong2 v = *reinterpret_cast<pair*>(vr0 + (uint32_t)(lane * DHW));
-      r.k[0] = k.x;
-      r.k[DHW - 1] = k.y;
-      r.v[0] = v.x;
-      r.v[DHW - 1] = v.y;
-    } else {
-#pragma unroll
-      for (int w = 0; w < DHW; ++w) {
-        r.k[w] = kr0[(uint32_t)(lane * dw + w)];
-        r.v[w] = vr0[(uint32_t)(lane * DHW + w)];
-      }
-    }
+    load_words<DHW>(k, kt + (size_t)jc * 64 * dw + (uint32_t)(row8 * dw + my_head * DHW), a.vec);
+  };
+  auto load = [&](int i) __attribute__((always_inline)) {
+    RowValues<DHW> r;
+    const int jc = cl.at(min(i, i1 - 1));
+    load_words<DHW>(r.v, vb + (size_t)jc * d + (uint32_t)(lane * DHW), a.vec);
     r.pos = a.bias ? a.k_pos[min(64 * jc + lane, a.n_keys - 1)] : 0;
     return r;
   };
-  RowChunk<DHW> ch[kRowAhead];
-  if (i0 < i1) {  // uniform
+  // rows of a chunk that this wave brings: all 64 over the waves there are
+  constexpr int kPieces = HEADS ? 8 : 1;  // at most (one wave: eight times 8 rows)
+  uint64_t keys[2][HEADS ? 1 : DHW];      // without HEADS: two chunks on their way
+  uint64_t piece[kPieces][DHW];
+  RowValues<DHW> val[2];
+  auto load_pieces = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < kRowAhead; ++j) ch[j] = load(i0 + part + j * np);
+    for (int n = 0; n < kPieces; ++n) {
+      const int r = (n * nwaves + wave) * 8 + lane / kHeadWaves;
+      if (n * nwaves * 8 < 64) load_keys(piece[n], i, min(r, 63));  // uniform
+    }
+  };
+  auto put_pieces = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int n = 0; n < kPieces; ++n) {
+      const int r = (n * nwaves + wave) * 8 + lane / kHeadWaves;
+      if (n * nwaves * 8 < 64 && r < 64) {
+#pragma unroll
+        for (int w = 0; w < DHW; ++w) sKeys[HEADS ? buf : 0][HEADS ? r * kKeyLd + (lane % kHeadWaves) * DHW + w : 0] = piece[n][w];
+      }
+    }
+  };
+  if (i0 < i1) {  // uniform
+    if constexpr (HEADS) load_pieces(i0);
+    else {
+      load_keys(keys[0], i0 + part, lane);
+      load_keys(keys[1], i0 + part + np, lane);
+    }
+    val[0] = load(i0 + part);
+    val[1] = load(i0 + part + np);
   }
   uint64_t q[DHW];
 #pragma unroll
@@ -196,6 +233,9 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_masked_rows(MaskedArgs a) {
   if constexpr (!HEADS) {
     for (int i = tid; i < a.T * DH; i += nth) (&sNum[0][0])[i] = 0;
     if (tid < a.T) sDen[tid] = 0;
+  } else if (i0 < i1) {
+    put_pieces(0);
+    load_pieces(i0 + 1);
   }
   __syncthreads();
 
@@ -204,29 +244,47 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_masked_rows(MaskedArgs a) {
   for (int b = 0; b < 8; ++b)
 #pragma unroll
     for (int w = 0; w < DHW; ++w) acc[b][w] = 0;
-  for (int i = i0 + part; i < i1; i += kRowAhead * np) {  // wave-uniform
+  auto weigh = [&](const uint64_t (&k)[DHW], const RowValues<DHW>& r, int jc) __attribute__((always_inline)) {
+    const int j = 64 * jc + lane;
+    int s = 0;
 #pragma unroll
-    for (int n = 0; n < kRowAhead; ++n) {
+    for (int w = 0; w < DHW; ++w) s += (int)__popcll(k[w] & q[w]);
+    const bool seen = (j >= kr.a0 && j < kr.a1) || (j >= kr.b0 && j < kr.b1);
+    if (a.bias) {
+      const int off = __builtin_elementwise_sub_sat(q_pos, r.pos);
+      s = min(max(s + sBias[min(max(off, -D), D) + D], 0), 255);
+    }
+    const int p = seen ? sLut[s] : 0;
+    den += p;
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+      const uint64_t mask = __builtin_amdgcn_ballot_w64((p >> b) & 1);
+#pragma unroll
+      for (int w = 0; w < DHW; ++w) acc[b][w] += (int)__popcll(r.v[w] & mask);
+    }
+  };
+  for (int i = i0 + part; i < i1; i += 2 * np) {  // wave-uniform; HEADS: uniform
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
       const int e = i + n * np;
-      if (e < i1) {  // wave-uniform
-        const int j = 64 * cl.at(e) + lane;
-        int s = 0;
+      if (e < i1) {
+        if constexpr (HEADS) {
+          put_pieces((e - i0 + 1) & 1);  // the next chunk's, whose readers of two chunks ago are through
+          load_pieces(e + 2);
+          uint64_t k[DHW];
 #pragma unroll
-        for (int w = 0; w < DHW; ++w) s += (int)__popcll(ch[n].k[w] & q[w]);
-        const bool seen = (j >= kr.a0 && j < kr.a1) || (j >= kr.b0 && j < kr.b1);
-        if (a.bias) {
-          const int off = __builtin_elementwise_sub_sat(q_pos, ch[n].pos);
-          s = min(max(s + sBias[min(max(off, -D), D) + D], 0), 255);
+          for (int w = 0; w < DHW; ++w) k[w] = sKeys[(e - i0) & 1][lane * kKeyLd + wave * DHW + w];
+          weigh(k, val[n], cl.at(e));
+          val[n] = load(e + 2);
+          __syncthreads();
+        } else {
+          uint64_t k[DHW];
+#pragma unroll
+          for (int w = 0; w < DHW; ++w) k[w] = keys[n][HEADS ? 0 : w];
+          weigh(k, val[n], cl.at(e));
+          if constexpr (!HEADS) load_keys(keys[n], e + 2 * np, lane);
+          val[n] = load(e + 2 * np);
         }
-        const int p = seen ? sLut[s] : 0;
-        den += p;
-#pragma unroll
-        for (int b = 0; b < 8; ++b) {
-          const uint64_t mask = __builtin_amdgcn_ballot_w64((p >> b) & 1);
-#pragma unroll
-          for (int w = 0; w < DHW; ++w) acc[b][w] += (int)__popcll(ch[n].v[w] & mask);
-        }
-        ch[n] = load(e + kRowAhead * np);
       }
     }
   }
