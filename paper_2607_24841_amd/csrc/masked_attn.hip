@@ -27,10 +27,11 @@ struct MaskedArgs {
   int n_keys, max_rows, T, H, parts, splits, max_dist;
   int tile;       // rows that a workgroup takes: 1, 16 or 32
   bool vec;       // the caches are 16-byte aligned
+  bool spread;    // see Place
   int32_t theta;
 };
 constexpr int kMaskedDen = 4;    // the weights' sum behind the channels' sums, and padding
-constexpr int kSplitChunks = 4;  // a split has at least this many chunks
+constexpr int kSplitChunks = 2;  // a split has at least this many chunks
 
 // The keys of two ranges [lo, hi) within [0, n_keys), the empty ones at 0.
 struct KeyRanges {
@@ -98,7 +99,9 @@ __device__ __forceinline__ int32_t* split_sums(const MaskedArgs& a, int row, int
 // wave brings into the CU's cache for all (with a head a workgroup the reads of L2, eight
 // times the keys' bytes, set the pace).  Else a head and tile, wave = (timestep, part).
 // Logical ids go head fastest, and the last tiles first, which see most keys where
-// rows see what is before them.
+// rows see what is before them.  In grids that fill the chip (spread) groups of up to eight
+// heads of a tile go to the dies in turn: a range of tiles a die, as xcd_order has it,
+// gave the first die the longest ones (2048 causal rows 84 us, as long as if all saw all).
 constexpr int kHeadWaves = 8;
 struct Place {
   int h, h0, t, z, tile, part, np;  // h0: the workgroup's first head
@@ -113,6 +116,12 @@ __device__ __forceinline__ Place place(const MaskedArgs& a, int wave, int nwaves
     return Place{min(h, a.H - 1), h0, tz % a.T, tz / a.T, n_tiles - 1 - r / (a.T * a.splits), 0, 1, h < a.H};
   } else {
     const int t = wave / a.parts;
+    if (a.spread) {  // uniform
+      const int groups = (a.H + kHeadWaves - 1) / kHeadWaves, gs = (a.H + groups - 1) / groups;
+      const int slot = (int)blockIdx.x / kXcds, u = slot / gs * kXcds + (int)blockIdx.x % kXcds;
+      const int h = u % groups * gs + slot % gs, tile = n_tiles - 1 - u / groups;
+      return Place{h, h, t, 0, tile, wave - t * a.parts, a.parts, tile >= 0 && h < a.H};
+    }
     return Place{lid % a.H, lid % a.H, t, 0, n_tiles - 1 - lid / a.H, wave - t * a.parts, a.parts, true};
   }
 }
@@ -390,6 +399,7 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_masked_ti
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nwaves = nth >> 6;
   const int g = lane >> 4, c = lane & 15;
   const Place pl = place<HEADS>(a, wave, nwaves);
+  if (!HEADS && !pl.there) return;  // uniform
   const int h = pl.h, t = pl.t, part = pl.part, np = pl.np, row0 = pl.tile * 16 * QG;
   const int nr = min(a.max_rows - row0, 16 * QG);
   const int d = a.H * DH, dw = d / 64, D = a.max_dist;
@@ -637,13 +647,28 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_masked_join(MaskedArgs a) {
                   [&](int tt) { return sNum[tt][wave * 64 + lane]; }, [&](int tt) { return sDen[tt]; });
 }
 
+// Which kernel and grid; the ranges are on the device, the rule sees the sizes.  Measured in
+// graphs with spikes out, T = 4, H = 16, dh = 128 unless said, us by heads / in one kernel:
+//  * By heads (a second launch joins the sums) where a wave's walk of all keys would be
+//    long and few workgroups would make it, the more rows the longer, since each row's sums
+//    go through memory: 1 row x 1000 keys 11.3 / 8.1, x 2000 11.2 / 11.7, x 8000 15 / 49; 4 rows
+//    x 450 12.0 / 10.2, x 1000 12.1 / 13.4; 18 x 1000 16.6 / 13.4, x 2000 19 / 20, x 4000 21 / 32;
+//    34 x 2000 23 / 20, x 4000 24 / 32; 66 x 2000 28 / 21, x 8000 37 / 56; 130 x 4000 43 / 35, x
+//    16000 72 / 104; 250 (16 tiles, a workgroup a CU without) x 16000 104 / 109.  T = 8, H = 8, dh =
+//    64: 18 x 1000 13 / 15; T = 1, H = 4: 1 x 1500 8.7 / 5.2, x 6000 9.2 / 11.4, 18 x 1500 11 / 8.3.
+//  * 32 rows a wave where the tiles give 1024 such waves (2 x 1024 rows in blocks 52 against
+//    72 with 16), by heads where fewer keys are expanded so: a chunk costs 155 for 16 rows
+//    and 200 for 32 (18 rows x 65 thousand keys 62 against 85).
+//  * Splits to fill the chip: 18 x 65 thousand keys, 16, 32 and 64 splits 64, 62 and 79; one
+//    row x 130 thousand, 64 splits 68, 96 77, 128 73.
 MaskedRoute masked_route(int T, int M, int n_keys, int H) {
   MaskedRoute r{1, T <= 2 ? 4 : (T <= 4 ? 2 : 1), 1, false};
   if (M > 2) r.tile = M >= 32 && (long long)(M / 32) * H * T >= 1024 ? 32 : 16;
   if (r.tile == 1) r.parts = std::max(std::min(kRowWaves / T, 4), 1);
   if (r.tile == 32) r.parts = 1;
   const long long wgs = (long long)((M + r.tile - 1) / r.tile) * H;
-  if (wgs >= 128 || n_keys < 2 * 64 * kSplitChunks) return r;
+  const int walk = (n_keys + 63) / 64 / r.parts;
+  if (wgs >= 256 || walk <= (r.tile == 1 ? 11 : 8 + M / 3)) return r;
   r.heads = true;
   r.parts = 1;
   if (r.tile > 1) r.tile = ((M + 15) / 16) * 155 <= ((M + 31) / 32) * 200 ? 16 : 32;
@@ -659,6 +684,7 @@ size_t masked_attn_ws(int T, int M, int n_keys, int H, int dh) {
   return align_up((size_t)M * H * r.splits * T * (dh + kMaskedDen) * sizeof(int32_t), 256);
 }
 
+constexpr unsigned kSpreadGroups = 64;
 constexpr size_t kMaskedPlainLds = 32768;  // dynamic LDS that needs no attribute beside the static
 
 template <int DHW, int QG, bool BIAS, bool HEADS>
@@ -675,10 +701,14 @@ static nmdlm_status launch_tiles(const MaskedArgs& a, unsigned grid, int waves, 
 }
 
 template <int DHW, bool HEADS>
-static nmdlm_status launch_masked(const MaskedArgs& a, hipStream_t st) {
+static nmdlm_status launch_masked(MaskedArgs a, hipStream_t st) {
   const int waves = HEADS ? std::min(a.H, kHeadWaves) : a.T * a.parts;
   const unsigned tiles = (a.max_rows + a.tile - 1) / a.tile;
-  const unsigned grid = HEADS ? tiles * ((a.H + waves - 1) / waves) * a.T * a.splits : tiles * a.H;
+  const unsigned groups = (a.H + kHeadWaves - 1) / kHeadWaves, gs = (a.H + groups - 1) / groups;
+  a.spread = !HEADS && a.tile > 1 && tiles * groups >= kSpreadGroups;
+  const unsigned grid = HEADS      ? tiles * ((a.H + waves - 1) / waves) * a.T * a.splits
+                        : a.spread ? (tiles * groups + kXcds - 1) / kXcds * kXcds * gs
+                                   : tiles * a.H;
   if (a.tile == 1) {
     hipLaunchKernelGGL((k_masked_rows<DHW, HEADS>), dim3(grid), dim3(64 * waves), 0, st, a);
     return hip_status();
@@ -698,7 +728,7 @@ static nmdlm_status launch_masked_dh(const MaskedAttnCall& c, hipStream_t st) {
                      static_cast<int32_t*>(c.ws), c.n_keys, c.M, c.T, c.H, r.parts, r.splits,
                      c.bias ? c.mask.max_dist : 0, r.tile,
                      ((reinterpret_cast<uintptr_t>(c.k_cache) | reinterpret_cast<uintptr_t>(c.vt_cache)) & 15) == 0,
-                     c.theta};
+                     false, c.theta};
   if (!r.heads) return launch_masked<DHW, false>(a, st);
   const nmdlm_status rc = launch_masked<DHW, true>(a, st);
   if (rc != NMDLM_OK) return rc;

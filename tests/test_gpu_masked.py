@@ -66,12 +66,19 @@ def test_tiles_of_32_rows(dh, max_dist):
     check(K.make_case(dh, r, pos, 400, T=8, H=16, dh=dh, max_dist=max_dist))
 
 
+@pytest.mark.parametrize("H", [1, 5, 9, 16])
+def test_many_tiles(H):
+    """Tiles enough to go to the dies in turn, with heads in groups of unequal size."""
+    r, pos = K.docs_mask([40] * (40 if H > 8 else 32), 7)
+    check(K.make_case(H, r, pos, len(r), T=1, H=H, max_dist=5, k_pos=pos))
+
+
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("max_dist", [None, 33])
 @pytest.mark.parametrize("T, M, n_keys, H, tile, heads", [(4, 1, 300, 2, 1, False), (4, 2, 3000, 2, 1, True),
                                                           (4, 3, 300, 2, 16, False), (2, 12, 5000, 1, 16, True),
-                                                          (3, 30, 1500, 11, 32, True), (4, 40, 700, 9, 32, True),
-                                                          (2, 1, 9000, 13, 1, True), (8, 70, 1200, 3, 32, True)])
+                                                          (3, 30, 3000, 11, 32, True), (4, 40, 3500, 9, 32, True),
+                                                          (2, 1, 9000, 13, 1, True), (8, 70, 2600, 3, 32, True)])
 def test_routes_of_small_calls(T, M, n_keys, H, tile, heads, max_dist, dh):
     """The kernels that the sizes of these tests reach, heads that do not fill a workgroup."""
     r = K.route(T, M, n_keys, H)
