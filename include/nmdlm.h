@@ -742,6 +742,30 @@ nmdlm_status nmdlm_bbm_attn_masked(const uint64_t* q, const uint64_t* k_cache,
 size_t nmdlm_bbm_attn_masked_workspace_size(int T, int M, int n_keys, int H, int dh);
 
 /* ------------------------------------------------------------------------
+ * nmdlm_block_step_masked — nmdlm_block_step (the same layers, head and
+ * unmasking) of one sequence's rows that see the keys of a mask: keys and values
+ * of the M rows go to cache rows [C, C+M), and row m sees the cache rows of
+ * ranges[m] among the C+M.  In one step it scores drafted tokens, several
+ * documents or a whole sequence block by block.
+ *
+ *   mask   HOST struct; q_pos are the rows' positions (with x_in they are read for a
+ *          bias only).  One outside the position table has no position spike and
+ *          sets NMDLM_STATUS_BAD_REQUEST; k_pos [C+M], the new rows' own among them
+ *   bias   HOST array [n_layers] of device tables (as nmdlm_bbm_attn_masked; NULL:
+ *          none in this layer), or NULL
+ *   io     as nmdlm_block_step; pos0 and NMDLM_ATTN_FUSED are not read, n_seq is 0 or 1
+ *          (else NMDLM_ERR_UNSUPPORTED)
+ *   ws     nmdlm_block_step_masked_workspace_size() for C+M keys (which does not
+ *          fall as the keys grow), cleared as for nmdlm_block_step
+ * Errors: as nmdlm_block_step and nmdlm_bbm_attn_masked.
+ * ------------------------------------------------------------------------ */
+nmdlm_status nmdlm_block_step_masked(const nmdlm_model* model, const nmdlm_mask* mask,
+                                     const int8_t* const* bias, nmdlm_step_io* io, void* ws,
+                                     size_t ws_bytes, void* stream);
+size_t nmdlm_block_step_masked_workspace_size(const nmdlm_model* model, int M, int n_keys,
+                                              unsigned flags);
+
+/* ------------------------------------------------------------------------
  * nmdlm_token_sample — a token of each row of logits.  With the row's largest
  * logit l_max, temperature tau and w_v = exp((l_v - l_max) / tau) (float64; 0 for
  * exponents below -700 and for NaN, 1 where l_v = l_max), the token is the first

@@ -779,3 +779,87 @@ def draft_verify(logits, draft_logits, draft, u, tau: float, draft_tau: float, c
             if tok[m] >= 0:
                 conf[m] = w1[tok[m]] / w1.sum()
     return tok, acc, conf, n_acc
+
+
+def masked_stack(X, layers, k_caches, v_caches, c0: int, ranges, bias=None, q_pos=None, k_pos=None,
+                 max_dist: int = 0):
+    """layer_forward over a stack, row m of X seeing the cache rows of ranges[m]
+    among [0, c0+M); bias: a table (or None) a layer."""
+    X = np.asarray(X, dtype=bool)
+    T, M, d = X.shape
+    J = c0 + M
+    for l, L in enumerate(layers):
+        th = L.theta
+        qkv = qbsm(X, L.W_qkv)
+        q, k, v = (if_neuron(qkv[:, :, i * d:(i + 1) * d], th[n])[0] for i, n in enumerate("qkv"))
+        k_caches[l][:, c0:J], v_caches[l][:, c0:J] = k, v
+        a = masked_attention(q, k_caches[l][:, :J], v_caches[l][:, :J], L.H, L.lut_att,
+                             np.clip(np.asarray(ranges, dtype=np.int64), 0, J),
+                             None if bias is None else bias[l], q_pos, k_pos, max_dist)
+        A = if_neuron(a, th["a"])[0]
+        X1 = if_neuron(qbsm(A, L.W_o), th["o"], resid=X)[0]
+        Hs = if_neuron(qnl_lut(qbsm(X1, L.W_up), L.s_up, L.lut_act, QNL_S8), th["up"])[0]
+        X = if_neuron(qbsm(Hs, L.W_dn), th["dn"], resid=X1)[0]
+    return X
+
+
+def masked_logits(model, emb01, tokens, masked, pos, c0: int, kc, vc, ranges, n_layers=None):
+    """Head logits of a masked step of the first n_layers."""
+    cur = np.where(np.asarray(masked, dtype=bool), model.mask_id, tokens)
+    X = block_input(cur, pos, emb01, model.pos_ch)
+    Y = masked_stack(X, model.layers[:n_layers], kc, vc, c0, ranges)
+    return head_logits(Y, model.W_head, model.scale)
+
+
+def left_to_right(model, prompt, n_tokens: int):
+    """The most likely token behind the tokens before, one at a time: a masked row
+    that sees them, and nothing else, at each position."""
+    emb01 = unpack_model_emb(model)
+    seq = [int(x) for x in prompt]
+    cap, P = len(seq) + n_tokens + 2, len(seq) - 1
+    kc, vc = new_caches(model.n_layers, model.T, cap, model.d)
+    if P > 0:
+        prefill(block_input(seq[:P], np.arange(P), emb01, model.pos_ch), model.layers, kc, vc)
+    for C in range(P, P + n_tokens):
+        l = masked_logits(model, emb01, [seq[C], 0], [0, 1], [C, C + 1], C, kc, vc,
+                          [[0, C + 1, 0, 0], [0, C + 2, 0, 0]])
+        seq.append(int(np.argmax(l[1])))
+    return seq[len(prompt):]
+
+
+def drafted(model, draft, n_layers, prompt, n_rounds: int, B: int, tau: float, draft_tau: float, numbers):
+    """Rounds of drafted generation: tokens of each.  draft None: the first n_layers
+    of the model draft, over its caches; else a model with caches of its own.
+    numbers(shape): the uniform numbers of a round, [B] and then [B + 1][2]."""
+    own = draft is not None
+    dmod = draft if own else model
+    emb, demb = unpack_model_emb(model), unpack_model_emb(dmod)
+    seq = [int(x) for x in prompt]
+    P, cap = len(seq) - 1, len(seq) + (n_rounds + 3) * (2 * B + 2)
+    kc, vc = new_caches(model.n_layers, model.T, cap, model.d)
+    dkc, dvc = new_caches(dmod.n_layers, dmod.T, cap, dmod.d) if own else (kc, vc)
+    for m, e, k, v in [(model, emb, kc, vc)] + ([(dmod, demb, dkc, dvc)] if own else []):
+        if P > 0:
+            prefill(block_input(seq[:P], np.arange(P), e, m.pos_ch), m.layers, k, v)
+    C = D = P
+    rounds = []
+    for _ in range(n_rounds):
+        new = seq[D:]
+        k = len(new)
+        r = [[0, D + i + 1 if i < k else D + k + B, 0, 0] for i in range(k + B)]
+        dl = masked_logits(dmod, demb, new + [0] * B, [0] * k + [1] * B, np.arange(D, D + k + B), D, dkc, dvc, r,
+                           n_layers)[k:]
+        x = token_sample(dl, draft_tau, numbers(B))[0]
+        toks = [seq[-1]] + [int(t) for t in x] + [0] * (B + 1)
+        pos = [C + i for i in range(B + 1)] + [C + i + 1 for i in range(B + 1)]
+        r = ([[0, C + i + 1, 0, 0] for i in range(B + 1)]
+             + [[0, C + i + 1, C + B + 1 + i, C + B + 2 + i] for i in range(B + 1)])
+        l = masked_logits(model, emb, toks, [0] * (B + 1) + [1] * (B + 1), pos, C, kc, vc, r)[B + 1:]
+        tok, _, _, n = draft_verify(l, np.concatenate([dl, dl[:1]]), list(x) + [-1], numbers(B + 1, 2), tau, draft_tau,
+                                    [0, B + 1])
+        got = [int(t) for t in tok[:n[0] + 1]]
+        D = D + k if own else C + len(got)
+        C += len(got)
+        seq += got
+        rounds.append(got)
+    return rounds

@@ -69,6 +69,7 @@ EXPORTS = (
     "nmdlm_block_step_paged_workspace_size", "nmdlm_bbm_attn_masked",
     "nmdlm_bbm_attn_masked_workspace_size", "nmdlm_token_sample",
     "nmdlm_token_sample_workspace_size", "nmdlm_draft_verify", "nmdlm_draft_verify_workspace_size",
+    "nmdlm_block_step_masked", "nmdlm_block_step_masked_workspace_size",
 )
 
 
@@ -203,6 +204,10 @@ def load(path: str = LIB_PATH):
     lib.nmdlm_token_sample.argtypes = [vp, C.c_int, C.c_int, C.c_double, vp, vp, vp, vp, sz, vp]
     lib.nmdlm_draft_verify.argtypes = [vp, vp, C.c_int, C.c_int, vp, vp, C.c_double, C.c_double, vp,
                                        C.c_int, u, vp, vp, vp, vp, vp, sz, vp]
+    lib.nmdlm_block_step_masked.argtypes = [C.POINTER(Model), C.POINTER(MaskC), C.POINTER(vp),
+                                            C.POINTER(StepIO), vp, sz, vp]
+    lib.nmdlm_block_step_masked_workspace_size.argtypes = [C.POINTER(Model), C.c_int, C.c_int, u]
+    lib.nmdlm_block_step_masked_workspace_size.restype = sz
     for fn in (lib.nmdlm_token_sample_workspace_size, lib.nmdlm_draft_verify_workspace_size):
         fn.argtypes, fn.restype = [C.c_int] * 2, sz
     lib.nmdlm_workspace_clear.argtypes = [vp, sz, vp]
@@ -780,6 +785,28 @@ def nmdlm_block_step_paged(model: PagedModel, io: StepIO, ws: torch.Tensor, n_se
     fn, ref, counts = load().nmdlm_block_step_paged, C.byref(model.c), model.key_counts
     pages._call(lambda pg, st: fn(ref, pg, counts, n_sel, C.byref(io), pages._arg(what, "ws", ws, 1, 1),
                                   ws.numel(), st), what, stream=stream)
+
+
+def nmdlm_block_step_masked(model: "DeviceModel", io: StepIO, mask: Mask, ws: torch.Tensor, bias=None,
+                            stream=None) -> None:
+    """bias: a table (or None) for each layer, or None."""
+    what, ix, n = "nmdlm_block_step_masked", mask._index, len(model.layers)
+    mask.check(what, io.M, io.C + io.M, bias is not None)
+    tables = None
+    if bias is not None:
+        if len(bias) != n:
+            raise NmdlmError(NMDLM_ERR_INVALID_ARG, f"{what}: {len(bias)} tables for {n} layers")
+        size = model.H * (2 * mask.max_dist + 1)
+        tables = (C.c_void_p * max(1, n))(*[_arg(what, "bias", t, size, 1, ix) for t in bias])
+    for l in model.layers:
+        if l.w_qkv.get_device() != ix:
+            raise NmdlmError(NMDLM_ERR_INVALID_ARG, f"{what}: the layers are not on the mask's device")
+    at, fn = _arg(what, "ws", ws, 1, 1, ix), load().nmdlm_block_step_masked
+    _on(ix, what, lambda st: fn(C.byref(model.c), mask._ref, tables, C.byref(io), at, ws.numel(), st), stream)
+
+
+def nmdlm_block_step_masked_workspace_size(model: "DeviceModel", M: int, n_keys: int, flags: int = 0) -> int:
+    return load().nmdlm_block_step_masked_workspace_size(C.byref(model.c), M, n_keys, flags)
 
 
 def nmdlm_block_step_paged_workspace_size(model: PagedModel, flags: int = 0) -> int:

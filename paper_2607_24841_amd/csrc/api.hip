@@ -12,7 +12,8 @@ namespace nmdlm {
 size_t block_step_ws_size(const nmdlm_model* md, int M, unsigned flags);
 size_t block_step_paged_ws_size(const nmdlm_model* md, const nmdlm_pages& pg, unsigned flags);
 nmdlm_status block_step_impl(const nmdlm_model* md, nmdlm_step_io* io, void* ws, size_t ws_bytes,
-                             hipStream_t st, const PagedStep* paged);
+                             hipStream_t st, const PagedStep* paged, const MaskedStep* masked);
+size_t block_step_masked_ws_size(const nmdlm_model* md, int M, int n_keys, unsigned flags);
 }  // namespace nmdlm
 
 using namespace nmdlm;
@@ -605,7 +606,7 @@ nmdlm_status nmdlm_block_step(const nmdlm_model* md, nmdlm_step_io* io, void* ws
   if (!ws || !aligned(ws, 256) || ws_bytes < block_step_ws_size(md, (int)Mt, io->flags))
     return NMDLM_ERR_WORKSPACE;
   if ((rc = events_ok(io, stream)) != NMDLM_OK) return rc;
-  return block_step_impl(md, io, ws, ws_bytes, static_cast<hipStream_t>(stream), nullptr);
+  return block_step_impl(md, io, ws, ws_bytes, static_cast<hipStream_t>(stream), nullptr, nullptr);
 }
 
 size_t nmdlm_block_step_paged_workspace_size(const nmdlm_model* md, const nmdlm_pages* pages, unsigned flags) {
@@ -639,7 +640,44 @@ nmdlm_status nmdlm_block_step_paged(const nmdlm_model* md, const nmdlm_pages* pa
     return NMDLM_ERR_WORKSPACE;
   if ((rc = events_ok(io, stream)) != NMDLM_OK) return rc;
   const PagedStep paged{pages, key_counts, n_sel};
-  return block_step_impl(md, io, ws, ws_bytes, static_cast<hipStream_t>(stream), &paged);
+  return block_step_impl(md, io, ws, ws_bytes, static_cast<hipStream_t>(stream), &paged, nullptr);
+}
+
+size_t nmdlm_block_step_masked_workspace_size(const nmdlm_model* md, int M, int n_keys, unsigned flags) {
+  if (!md || model_ok(md) != NMDLM_OK) return 0;
+  if (masked_sizes_ok(md->T, M, n_keys, md->H, md->d / md->H) != NMDLM_OK || n_keys < M) return 0;
+  return block_step_masked_ws_size(md, M, n_keys, flags);
+}
+
+nmdlm_status nmdlm_block_step_masked(const nmdlm_model* md, const nmdlm_mask* mask, const int8_t* const* bias,
+                                     nmdlm_step_io* io, void* ws, size_t ws_bytes, void* stream) {
+  if (!md || !io) return NMDLM_ERR_INVALID_ARG;
+  nmdlm_status rc = model_ok(md);
+  if (rc != NMDLM_OK) return rc;
+  if (io->M < 1 || io->C < 0 || io->n_seq < 0) return NMDLM_ERR_INVALID_ARG;
+  if (io->n_seq > 1) return NMDLM_ERR_UNSUPPORTED;
+  if ((int64_t)io->C + io->M > NMDLM_MAX_KEYS) return NMDLM_ERR_UNSUPPORTED;
+  if ((rc = masked_sizes_ok(md->T, io->M, io->C + io->M, md->H, md->d / md->H)) != NMDLM_OK) return rc;
+  bool any_bias = false;
+  for (int l = 0; bias && l < md->n_layers; ++l) any_bias = any_bias || bias[l];
+  if ((rc = mask_ok(mask, any_bias)) != NMDLM_OK) return rc;
+  if (!io->x_in && (!mask->q_pos || !aligned(mask->q_pos, 4))) return NMDLM_ERR_INVALID_ARG;
+  if (md->cache_cap % 64 != 0 || md->cache_cap < (int64_t)io->C + io->M) return NMDLM_ERR_INVALID_ARG;
+  if (md->cache_cap / 64 > INT_MAX) return NMDLM_ERR_UNSUPPORTED;
+  if ((rc = layers_ok(md, io->flags)) != NMDLM_OK) return rc;
+  for (int l = 0; l < md->n_layers; ++l)
+    if (!aligned(md->layers[l].k_cache, 8) || !aligned(md->layers[l].vt_cache, 8)) return NMDLM_ERR_INVALID_ARG;
+  if (!io->x_in) {
+    if (!md->emb || !md->pos_ch || md->max_pos < 0) return NMDLM_ERR_INVALID_ARG;
+    if (!io->tokens && !io->masked) return NMDLM_ERR_INVALID_ARG;
+  }
+  if ((rc = head_ok(md, io)) != NMDLM_OK) return rc;
+  if (!(io->flags & NMDLM_NO_HEAD) && io->M > NMDLM_MAX_HEAD_M) return NMDLM_ERR_UNSUPPORTED;
+  if (!ws || !aligned(ws, 256) || ws_bytes < block_step_masked_ws_size(md, io->M, io->C + io->M, io->flags))
+    return NMDLM_ERR_WORKSPACE;
+  if ((rc = events_ok(io, stream)) != NMDLM_OK) return rc;
+  const MaskedStep masked{mask, bias};
+  return block_step_impl(md, io, ws, ws_bytes, static_cast<hipStream_t>(stream), nullptr, &masked);
 }
 
 nmdlm_status nmdlm_workspace_clear(void* ws, size_t ws_bytes, void* stream) {

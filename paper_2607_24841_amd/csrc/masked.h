@@ -30,6 +30,12 @@ MaskedRoute masked_route(int T, int M, int n_keys, int H);
 size_t masked_attn_ws(int T, int M, int n_keys, int H, int dh);
 nmdlm_status launch_masked_attn(const MaskedAttnCall& c, hipStream_t st);
 
+// A block step whose rows see the keys of a mask.
+struct MaskedStep {
+  const nmdlm_mask* mask;
+  const int8_t* const* bias;  // host array [n_layers], or null
+};
+
 struct VerifyCall {
   const float* logits;
   const float* draft_logits;  // or null

@@ -7,6 +7,7 @@
 #include <algorithm>
 
 #include "common.h"
+#include "masked.h"
 #include "pages.h"
 
 namespace nmdlm {
@@ -40,9 +41,9 @@ __global__ __launch_bounds__(256) void k_assemble(const uint64_t* __restrict__ e
   X[i] = word;
 }
 
-// The same for the packed rows of a page plan: row m at position pos[m] of its
-// request.  Rows without a page are empty; a position past the table has no
-// position spike and sets NMDLM_STATUS_BAD_REQUEST.
+// The same for rows at positions pos[m], of a page plan or of a mask.  Rows without a page
+// (slot, if given, below 0) are empty; a position outside the table has no position
+// spike and sets NMDLM_STATUS_BAD_REQUEST.
 __global__ __launch_bounds__(256) void k_assemble_rows(const uint64_t* __restrict__ emb,
                                                        const int32_t* __restrict__ pos_ch, int max_pos,
                                                        const int32_t* __restrict__ tokens,
@@ -56,7 +57,7 @@ __global__ __launch_bounds__(256) void k_assemble_rows(const uint64_t* __restric
   const int w = (int)(i % dw);
   const int m = (int)((i / dw) % M);
   const int t = (int)(i / ((long long)dw * M));
-  if (slot[m] < 0) {
+  if (slot && slot[m] < 0) {
     X[i] = 0ull;
     return;
   }
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(256) void k_assemble_rows(const uint64_t* __restric
     tok = min(max(tok, 0), V);
   }
   uint64_t word = emb[((size_t)tok * T + t) * dw + w];
-  if (pos[m] < max_pos) {
+  if ((unsigned)pos[m] < (unsigned)max_pos) {
     const int pc = pos_ch[(size_t)pos[m] * T + t];
     if ((pc >> 6) == w) word |= 1ull << (pc & 63);
   } else {
@@ -380,6 +381,20 @@ static void carve_paged(Carver& cv, const nmdlm_model* md, const nmdlm_pages& pg
   b->ws_attn = cv.take<char>(paged_attn_ws(pg, md->T, md->H, md->d / md->H));
 }
 
+// What a step with a mask has besides: the attention's workspace.
+static void carve_masked(Carver& cv, const nmdlm_model* md, int M, int n_keys, char** ws_attn) {
+  *ws_attn = cv.take<char>(masked_attn_ws(md->T, M, n_keys, md->H, md->d / md->H));
+}
+
+size_t block_step_masked_ws_size(const nmdlm_model* md, int M, int n_keys, unsigned flags) {
+  Carver cv{nullptr, 0, (size_t)-1, true};
+  StepBuffers b;
+  char* ws_attn;
+  carve_step(cv, md, M, flags, true, true, true, true, false, &b);
+  carve_masked(cv, md, M, n_keys, &ws_attn);
+  return align_up(cv.off, 256);
+}
+
 size_t block_step_paged_ws_size(const nmdlm_model* md, const nmdlm_pages& pg, unsigned flags) {
   Carver cv{nullptr, 0, (size_t)-1, true};
   StepBuffers b;
@@ -461,11 +476,11 @@ static void attach_events(QbsmCall& c, const nmdlm_step_io* io, int i) {
 }
 
 nmdlm_status block_step_impl(const nmdlm_model* md, nmdlm_step_io* io, void* ws, size_t ws_bytes,
-                             hipStream_t st, const PagedStep* paged) {
+                             hipStream_t st, const PagedStep* paged, const MaskedStep* masked) {
   // Ms tokens in each of n_seq sequences, or the packed rows of a page plan; every
   // product takes all M rows
   const int T = md->T, Ms = paged ? paged->pages->max_rows : io->M;
-  const int n_seq = paged ? 1 : std::max(io->n_seq, 1), M = n_seq * Ms, C = io->C;
+  const int n_seq = paged || masked ? 1 : std::max(io->n_seq, 1), M = n_seq * Ms, C = io->C;
   const int d = md->d, F = md->F, H = md->H;
   const int dh = d / H, dw = d / 64, Fw = (F + 63) / 64;
   const int64_t cap = md->cache_cap, capw = cap / 64;
@@ -475,8 +490,10 @@ nmdlm_status block_step_impl(const nmdlm_model* md, nmdlm_step_io* io, void* ws,
   Carver cv{static_cast<char*>(ws), 0, ws_bytes, true};
   StepBuffers b;
   carve_step(cv, md, M, io->flags, io->x_in == nullptr, io->logits == nullptr,
-             io->pred == nullptr, io->conf == nullptr, paged == nullptr, &b);
+             io->pred == nullptr, io->conf == nullptr, !paged && !masked, &b);
   PagedBuffers pb{};
+  char* ws_masked = nullptr;
+  if (masked) carve_masked(cv, md, M, C + M, &ws_masked);
   if (paged) carve_paged(cv, md, *paged->pages, paged->n_sel >= 0, &pb);
   if (!cv.ok) return NMDLM_ERR_WORKSPACE;
 
@@ -487,11 +504,11 @@ nmdlm_status block_step_impl(const nmdlm_model* md, nmdlm_step_io* io, void* ws,
     if ((rc = launch_fill_zero(b.A, align_up((size_t)T * M * dw * 8, 16), st)) != NMDLM_OK) return rc;
     if ((rc = launch_fill_zero(b.uA, align_up((size_t)M * dw * 8, 16), st)) != NMDLM_OK) return rc;
   }
-  if (!X && paged) {
+  if (!X && (paged || masked)) {
     const long long total = (long long)T * M * dw;
     hipLaunchKernelGGL(k_assemble_rows, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, md->emb,
-                       md->pos_ch, md->max_pos, io->tokens, io->masked, paged->pages->slot, paged->pages->pos,
-                       md->V, T, M, dw, b.X, io->status);
+                       md->pos_ch, md->max_pos, io->tokens, io->masked, paged ? paged->pages->slot : nullptr,
+                       paged ? paged->pages->pos : masked->mask->q_pos, md->V, T, M, dw, b.X, io->status);
     if ((rc = hip_status()) != NMDLM_OK) return rc;
     X = b.X;
   } else if (!X) {
@@ -552,6 +569,10 @@ nmdlm_status block_step_impl(const nmdlm_model* md, nmdlm_step_io* io, void* ws,
       const PagedAttnCall pa{b.Q, ly.k_cache, ly.vt_cache, T, H, dh, ly.lut_att,
                              paged->n_sel >= 0 ? pb.sel : nullptr, nullptr, ly.theta_a, b.A, b.uA, pb.ws_attn};
       if ((rc = launch_paged_attn(pg, pa, st)) != NMDLM_OK) return rc;
+    } else if (masked) {
+      const MaskedAttnCall ma{b.Q, ly.k_cache, ly.vt_cache, cap, T, M, C + M, H, dh, ly.lut_att, *masked->mask,
+                              masked->bias ? masked->bias[l] : nullptr, nullptr, ly.theta_a, b.A, b.uA, ws_masked};
+      if ((rc = launch_masked_attn(ma, st)) != NMDLM_OK) return rc;
     } else {
       AttnCall at{b.Q, ly.k_cache, ly.vt_cache, cap, T, Ms, C, H, dh, n_seq, seq_words, ly.lut_att,
                   ly.theta_a, nullptr, b.a, b.A, b.uA,

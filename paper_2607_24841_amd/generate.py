@@ -4,7 +4,9 @@ finished block's keys/values stay in the caches as context.  The host only
 loops and marshals; every step runs in libnmdlm's kernels and the token
 state stays on the device until the end.  Several sequences (prompts of
 one length) advance together, one batched step per denoising step; requests
-of different lengths share pools of pages (PagedGenerator)."""
+of different lengths share pools of pages (PagedGenerator).  DraftedGenerator
+goes left to right: a cheaper model drafts a block in one step, one masked step of
+the model checks all of it."""
 from __future__ import annotations
 
 import numpy as np
@@ -199,3 +201,136 @@ class PagedGenerator:
         self._plan(self.pages, new)
         for s in requests:
             self.ctx[s], self.live[s] = 0, False
+
+
+class DraftedGenerator:
+    """Left-to-right generation of one sequence with drafted blocks.
+
+    A token is distributed as the model `dm` has it at a masked row that sees the
+    tokens before (at temperature 0 it is the most likely one).  Each round `draft`,
+    a cheaper model, fills a block of `block` masked tokens in one step, and one
+    masked step of `dm` computes the distributions behind the pending token and
+    behind each draft at once; nmdlm_draft_verify keeps the drafts that stand and
+    draws the token that follows them, so a round yields 1 to block + 1 tokens.
+
+    draft: the first layers of dm (dm.view(0, n, head=True)), which share dm's keys and
+    values, or another model over the same vocabulary with caches of its own.
+    Prompts are read as prefixes whose tokens see each other."""
+
+    def __init__(self, dm: B.DeviceModel, draft, block: int, temperature: float = 1.0,
+                 draft_temperature: float | None = None, seed: int = 0):
+        if not 1 <= block <= B.NMDLM_MAX_HEAD_M // 2 - 1:
+            raise ValueError(f"a block of {block} drafts: 1 to {B.NMDLM_MAX_HEAD_M // 2 - 1}")
+        if draft.V != dm.V:
+            raise ValueError(f"vocabularies of {dm.V} and {draft.V} tokens")
+        n = len(draft.layers)
+        self.shared = n > 0 and all(a is b for a, b in zip(draft.layers, dm.layers)) and n <= len(dm.layers)
+        if not self.shared and any(a is b for a in draft.layers for b in dm.layers):
+            raise ValueError("a draft of the model's own layers takes the first ones")
+        self.dm, self.draft, self.block = dm, draft, block
+        self.temperature = float(temperature)
+        self.draft_temperature = self.temperature if draft_temperature is None else float(draft_temperature)
+        self.rng = torch.Generator(device="cuda").manual_seed(seed)
+        # rows: the pending token and the drafts, then a masked row behind each of them
+        late, i = np.arange(block + 1), np.arange(2 * block + 2)
+        rows = np.zeros((2 * block + 2, 4), np.int32)
+        rows[:, 1] = i % (block + 1) + 1
+        rows[block + 1:, 2], rows[block + 1:, 3] = block + 1 + late, block + 2 + late
+        moves = (rows > 0).astype(np.int32)   # ends that go with the context
+        i32 = dict(dtype=torch.int32, device="cuda")
+        dev = lambda a: torch.as_tensor(a, **i32)  # noqa: E731
+        self._rows, self._moves = dev(rows), dev(moves)
+        self._pos = dev(np.concatenate([late, late + 1]))
+        self.mask = B.Mask(torch.zeros_like(self._rows), q_pos=torch.zeros_like(self._pos))
+        self.tokens = torch.zeros(2 * block + 2, **i32)
+        self.masked = dev((i > block)).to(torch.uint8)
+        self.logits = torch.empty(2 * block + 2, dm.V, device="cuda")
+        # the draft's rows: tokens that it has not seen, then the block
+        most = block + 1 + block
+        self.d_mask = B.Mask(torch.zeros(most, 4, **i32), q_pos=torch.zeros(most, **i32))
+        self.d_tokens = torch.zeros(most, **i32)
+        self.d_masked = torch.zeros(most, dtype=torch.uint8, device="cuda")
+        self.d_logits = torch.empty(most + 1, dm.V, device="cuda")
+        self.drafts = torch.full((block + 1,), -1, **i32)   # the last row has none
+        self.out = torch.zeros(block + 1, **i32)
+        self.accepted = torch.zeros(block + 1, dtype=torch.uint8, device="cuda")
+        self.n_accepted = torch.zeros(1, **i32)
+        size = B.nmdlm_block_step_masked_workspace_size
+        self.ws = B.workspace(max(
+            [size(dm, 2 * block + 2, dm.cache_cap)]
+            + [size(draft, m, draft.cache_cap) for m in range(block + 1, most + 1) if m <= draft.cache_cap]))
+        self.seq: list[int] = []   # all tokens; the last is pending: in no cache
+        self.ctx = self.d_ctx = 0  # tokens in the caches of dm and of the draft
+
+    def numbers(self, *shape: int) -> torch.Tensor:
+        """The uniform numbers of a round: [block] for the drafts, then [block + 1][2]."""
+        return torch.rand(*shape, generator=self.rng, device="cuda")
+
+    def start(self, prompt) -> None:
+        """Prefills the prompt, all but its last token."""
+        ids = np.asarray(prompt).reshape(-1)
+        if len(ids) < 1 or ids.min() < 0 or ids.max() >= self.dm.V:
+            raise ValueError(f"a prompt of {len(ids)} tokens: at least one, of ids below {self.dm.V}")
+        self._check_room(len(ids) - 1, len(ids) - 1)
+        P = len(ids) - 1
+        if P > 0:
+            t = torch.as_tensor(ids[:P].astype(np.int32)).cuda()
+            io = B.step_io(P, 0, flags=B.NMDLM_NO_HEAD, tokens=t)
+            for m in [self.dm] + ([] if self.shared else [self.draft]):
+                B.nmdlm_block_step(m, io, B.workspace(B.nmdlm_block_step_workspace_size(m, P, B.NMDLM_NO_HEAD)))
+        self.seq = [int(x) for x in ids]
+        self.ctx = self.d_ctx = P
+
+    def _check_room(self, ctx: int, d_ctx: int) -> None:
+        """A round's rows have places in the caches and in the position tables."""
+        rows, last = 2 * self.block + 2, ctx + self.block + 1
+        if ctx + rows > self.dm.cache_cap or last >= self.dm.c.max_pos:
+            raise ValueError(f"{ctx} tokens and {rows} rows: at most {self.dm.cache_cap} in the caches, "
+                             f"{self.dm.c.max_pos} positions")
+        if ctx + 1 + self.block > self.draft.cache_cap or last > self.draft.c.max_pos:
+            raise ValueError(f"{ctx} tokens and a block: at most {self.draft.cache_cap} in the draft's caches")
+
+    def round(self) -> list[int]:
+        """The tokens of one round: the drafts that stand and the one that follows them."""
+        if not self.seq:
+            raise ValueError("no prompt")
+        self._check_room(self.ctx, self.d_ctx)
+        n, C, D = self.block, self.ctx, self.d_ctx
+        # the draft: tokens that its caches lack, then the block
+        new = self.seq[D:]
+        k, rows = len(new), len(new) + n
+        r = np.zeros((rows, 4), np.int32)
+        r[:, 1] = np.minimum(D + np.arange(rows) + 1, D + rows)
+        r[k:, 1] = D + rows
+        self.d_mask.ranges[:rows].copy_(torch.from_numpy(r))
+        torch.arange(D, D + rows, out=self.d_mask.q_pos[:rows])
+        self.d_tokens[:k].copy_(torch.tensor(new, dtype=torch.int32))
+        self.d_masked[:k].zero_()
+        self.d_masked[k:rows].fill_(1)
+        io = B.step_io(rows, D, tokens=self.d_tokens, masked=self.d_masked, logits=self.d_logits)
+        B.nmdlm_block_step_masked(self.draft, io, self.d_mask, self.ws)
+        B.nmdlm_token_sample(self.d_logits[k:], n, self.dm.V, self.draft_temperature, self.numbers(n), self.drafts)
+        # the model: the pending token, the drafts, and the rows behind them
+        torch.add(self._rows, self._moves, alpha=C, out=self.mask.ranges)
+        torch.add(self._pos, C, out=self.mask.q_pos)
+        self.tokens[:1].fill_(self.seq[-1])
+        self.tokens[1:n + 1].copy_(self.drafts[:n])
+        io = B.step_io(2 * n + 2, C, tokens=self.tokens, masked=self.masked, logits=self.logits)
+        B.nmdlm_block_step_masked(self.dm, io, self.mask, self.ws)
+        B.nmdlm_draft_verify(self.logits[n + 1:], self.d_logits[k:], n + 1, self.dm.V, self.drafts,
+                             self.numbers(n + 1, 2), self.temperature, self.draft_temperature, self.out,
+                             self.accepted, n_accepted=self.n_accepted)
+        got = self.out[:int(self.n_accepted) + 1].tolist()
+        # dm has the pending token and the drafts that stand; the draft what it was given
+        self.ctx = C + len(got)
+        self.d_ctx = self.ctx if self.shared else D + k
+        self.seq += got
+        return got
+
+    def run(self, prompt, n_tokens: int) -> list[int]:
+        """n_tokens ids that follow the prompt (the last round may find more)."""
+        self.start(prompt)
+        out: list[int] = []
+        while len(out) < n_tokens:
+            out += self.round()
+        return out[:n_tokens]

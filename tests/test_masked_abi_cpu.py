@@ -146,3 +146,30 @@ def test_oracle_of_the_draw():
     take = np.minimum(1.0, p / q)
     left = np.maximum(p - q, 0)
     assert np.allclose(q * take + (q * (1 - take)).sum() * left / left.sum(), p)
+
+
+def test_masked_step_refusals(lib):
+    layers = (B.Layer * 1)(B.Layer(FAKE, FAKE, FAKE, FAKE, 200, 200, 200, 200, 200, 200, 200, 4, FAKE, FAKE, FAKE, FAKE))
+
+    def call(flags=B.NMDLM_NO_HEAD, M=16, C_=512, ranges=FAKE, q_pos=FAKE, k_pos=FAKE, dist=4, bias=None, nb=1 << 30,
+             ws=FAKE, no_mask=False, emb=FAKE, **io):
+        m = B.Model(1, 1024, 16, 4096, 32000, 4, 576, 64, layers, emb, FAKE, None, None)
+        step = B.step_io(M, C_, flags=flags, tokens=FAKE, **io)
+        mask = B.MaskC(ranges, q_pos, k_pos, dist)
+        table = (C.c_void_p * 1)(bias) if bias else None
+        return lib.nmdlm_block_step_masked(C.byref(m), None if no_mask else C.byref(mask), table, C.byref(step), ws, nb, None)
+    for bad in (dict(no_mask=True), dict(ranges=None), dict(ranges=FAKE + 4), dict(q_pos=None), dict(emb=None),
+                dict(bias=FAKE, k_pos=None), dict(bias=FAKE, dist=-1), dict(bias=FAKE, dist=2000), dict(M=0),
+                dict(C_=-1), dict(C_=561), dict(flags=0), dict(n_seq=-1)):
+        assert call(**bad) == INVALID, bad
+    assert call(n_seq=2) == UNSUPPORTED
+    assert call(M=1 << 18) == UNSUPPORTED
+    m = B.Model(1, 1024, 16, 4096, 32000, 4, 576, 64, layers, FAKE, FAKE, None, None)
+    f = lambda M, n: lib.nmdlm_block_step_masked_workspace_size(C.byref(m), M, n, B.NMDLM_NO_HEAD)  # noqa: E731
+    need = f(16, 528)
+    assert need > 0
+    for bad in (dict(ws=None), dict(ws=FAKE + 8), dict(nb=need - 1)):
+        assert call(**bad) == WORKSPACE, bad
+    assert f(0, 5) == f(5, 4) == f(5, 0) == 0
+    sizes = [f(16, n) for n in range(16, 40000, 97)]
+    assert sizes == sorted(sizes)     # does not fall as the keys grow
