@@ -281,8 +281,8 @@ __global__ __launch_bounds__(64 * kPartWaves, 5) void k_logit_parts(VerifyArgs a
     }
   };
   float next[kQuads][4], x[kQuads][4];
+  if (m < rows) row_at(m).load(next, part);  // wanted or not: asking takes as long
   bool here = wanted(m);
-  if (here) row_at(m).load(next, part);
   fill_pow(pow);
   __syncthreads();
   while (m < rows) {  // wave-uniform
@@ -332,17 +332,24 @@ __global__ __launch_bounds__(64 * kPartWaves, 5) void k_logit_parts(VerifyArgs a
   }
 }
 
-// The row's distribution from its parts; every lane gets it.
-__device__ __forceinline__ Dist row_dist(const PartStat* st, int parts, const Temper& tau, const double* pow) {
+// A lane's part of the first 64 of a row: loaded early, before what it is for is known.
+__device__ __forceinline__ PartStat lane_stat(const PartStat* st, int parts) {
+  return st[min((int)(threadIdx.x & 63), parts - 1)];
+}
+// The row's distribution from its parts (mine: this lane's of the first 64); every lane
+// gets it.
+__device__ __forceinline__ Dist row_dist(const PartStat* st, PartStat mine, int parts, const Temper& tau,
+                                         const double* pow) {
   const int lane = threadIdx.x & 63;
   Dist d(tau);
-  float top = -INFINITY;
-  for (int i = lane; i < parts; i += 64) top = fmaxf(top, st[i].top);
+  if (lane >= parts) mine = PartStat{-INFINITY, INT32_MAX, 0.0};
+  float top = mine.top;
+  for (int i = lane + 64; i < parts; i += 64) top = fmaxf(top, st[i].top);
   top = wave_top(top);
   d.set_top(top);
-  double sum = 0.0;
-  int first = INT32_MAX;
-  for (int i = lane; i < parts; i += 64) {
+  double sum = mine.sum * d.weight(mine.top, pow);
+  int first = mine.top == top ? mine.first : INT32_MAX;
+  for (int i = lane + 64; i < parts; i += 64) {
     const PartStat s = st[i];
     sum += s.sum * d.weight(s.top, pow);
     if (s.top == top) first = min(first, s.first);
@@ -366,10 +373,9 @@ struct Pair {
   Dist p, q;
   int x;
   bool certain;  // q is 1 at x
-  __device__ __forceinline__ Pair(const VerifyArgs& a, int m, int x_, const double* pow)
-      : p(row_dist(a.p_stat + (size_t)m * a.parts, a.parts, a.tau, pow)), q(a.draft_tau), x(x_),
-        certain(!a.draft_logits) {
-    if (!certain) q = row_dist(a.q_stat + (size_t)m * a.parts, a.parts, a.draft_tau, pow);
+  __device__ __forceinline__ Pair(const VerifyArgs& a, int m, int x_, const Dist& p_, PartStat mine_q, const double* pow)
+      : p(p_), q(a.draft_tau), x(x_), certain(!a.draft_logits) {
+    if (!certain) q = row_dist(a.q_stat + (size_t)m * a.parts, mine_q, a.parts, a.draft_tau, pow);
   }
   // max(p - q, 0) of a part's ids
   __device__ __forceinline__ void left(const RowAt& row, int part, Logits& l, double (&w)[kQuads][4],
@@ -419,18 +425,24 @@ __global__ __launch_bounds__(64 * kPartWaves) void k_verify_left(VerifyArgs a) {
   __shared__ double pow[32];
   const int m = blockIdx.y, lane = threadIdx.x & 63, step = gridDim.x * kPartWaves;
   int part = blockIdx.x * kPartWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  // the loads leave before what they are for is known: each wait is a trip to memory, since
+  // another die wrote the sums
+  const PartStat* const p_stat = a.p_stat + (size_t)m * a.parts;
+  const PartStat mine_p = lane_stat(p_stat, a.parts);
+  const PartStat mine_q = a.draft_logits ? lane_stat(a.q_stat + (size_t)m * a.parts, a.parts) : mine_p;
+  const int x = a.draft[m], at = min(max(x, 0), a.V - 1);
+  const float u = a.u[2 * m];
+  const RowAt row = target_row(a, m);
+  const float px = row.at(at), qx = a.draft_logits ? draft_row(a, m).at(at) : 0.0f;
+  fill_pow(pow);
   if (!row_counts(a, m)) return;  // uniform
-  const int x = a.draft[m];
   if ((uint32_t)x >= (uint32_t)a.V) {
     if (part == 0 && lane == 0) a.accepted[m] = 0;
     return;
   }
-  const RowAt row = target_row(a, m);
-  const float u = a.u[2 * m], px = row.at(x), qx = a.draft_logits ? draft_row(a, m).at(x) : 0.0f;
-  fill_pow(pow);
   __syncthreads();
   if (part >= a.parts) return;
-  const Pair d(a, m, x, pow);
+  const Pair d(a, m, x, row_dist(p_stat, mine_p, a.parts, a.tau, pow), mine_q, pow);
   const Dist &p = d.p, &q = d.q;
   bool take = false;
   double prob = 0.0;
@@ -493,9 +505,15 @@ __device__ __forceinline__ Spot find_part(int parts, float u, F of) {
   }
   return s;
 }
-// The id in the spot's part, from the weights of its ids; every lane gets it.
-__device__ __forceinline__ int find_id(const Spot& s, const double (&w)[kQuads][4], const RowAt& row) {
-  int id = -1;
+// The id in the spot's part, from the weights of its ids, and the target's logit there;
+// every lane gets them.
+struct Token {
+  int id;
+  float logit;  // as Dist::seen has it
+};
+__device__ __forceinline__ Token find_id(const Spot& s, const double (&w)[kQuads][4], const float (&l)[kQuads][4],
+                                         const RowAt& row) {
+  Token t{-1, -INFINITY};
   double run = s.before;
 #pragma unroll
   for (int k = 0; k < kQuads; ++k) {
@@ -505,19 +523,20 @@ __device__ __forceinline__ int find_id(const Spot& s, const double (&w)[kQuads][
     if (some) {  // uniform
       const int L = over ? (int)__builtin_ctzll(over) : 63 - (int)__builtin_clzll(some);
       double r = run + (in - x);
-      int mine = -1;
+      Token mine{-1, -INFINITY};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const bool past = mine >= 0 && r > s.target;
-        if (!past && w[k][e] > 0.0) mine = row.id(s.part, k) + e;
+        const bool past = mine.id >= 0 && r > s.target;
+        if (!past && w[k][e] > 0.0) mine = Token{row.id(s.part, k) + e, l[k][e]};
         r += past ? 0.0 : w[k][e];
       }
-      id = __builtin_amdgcn_readlane(mine, L);
-      if (over) return id;
+      t.id = __builtin_amdgcn_readlane(mine.id, L);
+      t.logit = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine.logit), L));
+      if (over) return t;
     }
     run += read_lane(in, 63);
   }
-  return id;
+  return t;
 }
 
 // ---------------------------------------------------------------------------
@@ -545,6 +564,16 @@ __global__ __launch_bounds__(64) void k_draw(VerifyArgs a) {
     return;
   }
   const int m = blockIdx.x;
+  // the loads leave before what they are for is known
+  const PartStat* const st = a.p_stat + (size_t)m * a.parts;
+  const double* const left = a.draft ? a.left + (size_t)m * a.parts : nullptr;
+  const PartStat mine_p = lane_stat(st, a.parts);
+  const PartStat mine_q = a.draft_logits ? lane_stat(a.q_stat + (size_t)m * a.parts, a.parts) : mine_p;
+  const double mine_left = left ? left[min(lane, a.parts - 1)] : 0.0;
+  const int x = a.draft ? a.draft[m] : -1;
+  const float u = a.draft ? a.u[2 * m + 1] : a.tau.sharp ? 0.0f : a.u[m];
+  const bool taken = a.accepted && a.accepted[m];
+  fill_pow(pow);
   if (!row_counts(a, m)) return;
   if (a.chain) {
     int r0 = 0;
@@ -572,40 +601,40 @@ __global__ __launch_bounds__(64) void k_draw(VerifyArgs a) {
       return;
     }
   }
-  if (a.accepted && a.accepted[m]) return;
-  fill_pow(pow);
+  if (taken) return;
   __syncthreads();
-  const int x = a.draft ? a.draft[m] : -1;
   const bool real = (uint32_t)x < (uint32_t)a.V;
   const RowAt row = target_row(a, m);
-  const PartStat* st = a.p_stat + (size_t)m * a.parts;
-  const Dist p = row_dist(st, a.parts, a.tau, pow);
-  int tok = -1;
+  const Dist p = row_dist(st, mine_p, a.parts, a.tau, pow);
+  Token tok{-1, 0.0f};
   if (p.some) {
-    const float u = a.draft ? a.u[2 * m + 1] : p.sharp ? 0.0f : a.u[m];
     double w[kQuads][4];
     if (real) {
-      const Spot s = find_part(a.parts, u, [&](int i) { return a.left[(size_t)m * a.parts + i]; });
+      const Spot s = find_part(a.parts, u, [&](int i) { return i < 64 ? mine_left : left[i]; });
       if (s.total > 0.0) {
         Logits l;
         l.load(a, m, s.part);
-        const Pair d(a, m, x, pow);
+        const Pair d(a, m, x, p, mine_q, pow);
         d.left(row, s.part, l, w, pow);
-        tok = find_id(s, w, row);
+        tok = find_id(s, w, l.p, row);
+        if (p.sharp) tok.logit = p.seen(tok.logit);  // else weighing has made it so
       }
     }
-    if (tok < 0 && p.sharp) tok = p.first;
-    if (tok < 0) {
-      const Spot s = find_part(a.parts, u, [&](int i) { return st[i].sum * p.weight(st[i].top, pow); });
+    if (tok.id < 0 && p.sharp) tok = Token{p.first, p.seen(row.at(p.first))};
+    if (tok.id < 0) {
+      const Spot s = find_part(a.parts, u, [&](int i) {
+        const PartStat t = i < 64 ? mine_p : st[i];
+        return t.sum * p.weight(t.top, pow);
+      });
       float l[kQuads][4];
       row.load(l, s.part);
       p.weights(l, w, pow);
-      tok = find_id(s, w, row);
+      tok = find_id(s, w, l, row);
     }
   }
   if (lane == 0) {
-    a.tokens[m] = tok;
-    if (a.conf) a.conf[m] = tok >= 0 ? p.weight(row.at(tok), pow) / p.sum : 0.0;
+    a.tokens[m] = tok.id;
+    if (a.conf) a.conf[m] = tok.id >= 0 ? p.weight_of<false>(tok.logit, pow) / p.sum : 0.0;
   }
 }
 
