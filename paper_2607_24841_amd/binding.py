@@ -10,6 +10,7 @@ runtimes end up mapped.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -579,36 +580,44 @@ def nmdlm_bbm_attn_masked_workspace_size(T, M, n_keys, H, dh) -> int:
     return load().nmdlm_bbm_attn_masked_workspace_size(T, M, n_keys, H, dh)
 
 
-def _floats(what: str, *named) -> None:
-    for name, t, dtype in named:
-        if t is not None and t.dtype != dtype:
-            raise NmdlmError(NMDLM_ERR_INVALID_ARG, f"{what}: {name} is {t.dtype}, not {dtype}")
+def _typed(what: str, name: str, t, n: int, dtype, index: int) -> int | None:
+    """_arg for a tensor of one type."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() < n or t.get_device() != index or not t.is_contiguous():
+        raise NmdlmError(NMDLM_ERR_INVALID_ARG,
+                         f"{what}: {name} needs {n} contiguous elements of {dtype} on GPU {index}")
+    return t.data_ptr()
 
 
 def _scratch(what: str, ws, nbytes: int, index: int, stream):
     """The given workspace, or one of torch's allocator for this call."""
     if ws is None and index >= 0:
-        ws = torch.empty(max(256, nbytes), dtype=torch.uint8, device=torch.device("cuda", index))
+        ws = torch.empty(max(256, nbytes), dtype=torch.uint8, device=index)
         if stream is not None:
             ws.record_stream(stream)
+        return ws, ws.data_ptr(), nbytes
     return ws, _arg(what, "ws", ws, 1, 1, index), 0 if ws is None else ws.numel()
 
 
+@functools.lru_cache(maxsize=256)
 def nmdlm_token_sample_workspace_size(M, V) -> int:
     return load().nmdlm_token_sample_workspace_size(M, V)
 
 
 def nmdlm_token_sample(logits, M, V, temperature, u, tokens, conf=None, ws=None, stream=None) -> None:
     """ws None: a workspace of torch's allocator for the call."""
-    what, ix, lib = "nmdlm_token_sample", logits.get_device(), load()
-    _floats(what, ("logits", logits, torch.float32), ("u", u, torch.float32), ("conf", conf, torch.float64))
-    args = (_arg(what, "logits", logits, M * V, 4, ix), M, V, float(temperature),
-            _arg(what, "u", u, M, 4, ix), _arg(what, "tokens", tokens, M, 4, ix),
-            _arg(what, "conf", conf, M, 8, ix))
-    ws, at, nbytes = _scratch(what, ws, lib.nmdlm_token_sample_workspace_size(M, V), ix, stream)
-    _on(ix, what, lambda st: lib.nmdlm_token_sample(*args, at, nbytes, st), stream)
+    what, ix = "nmdlm_token_sample", logits.get_device()
+    f32 = torch.float32
+    args = (_typed(what, "logits", logits, M * V, f32, ix), M, V, float(temperature),
+            _typed(what, "u", u, M, f32, ix), _typed(what, "tokens", tokens, M, torch.int32, ix),
+            _typed(what, "conf", conf, M, torch.float64, ix))
+    ws, at, nbytes = _scratch(what, ws, nmdlm_token_sample_workspace_size(M, V), ix, stream)
+    fn = load().nmdlm_token_sample
+    _on(ix, what, lambda st: fn(*args, at, nbytes, st), stream)
 
 
+@functools.lru_cache(maxsize=256)
 def nmdlm_draft_verify_workspace_size(M, V) -> int:
     return load().nmdlm_draft_verify_workspace_size(M, V)
 
@@ -618,17 +627,18 @@ def nmdlm_draft_verify(logits, draft_logits, M, V, draft, u, temperature, draft_
                        ws=None, stream=None) -> None:
     """chain False: every row counts (NMDLM_VERIFY_EACH).  ws None: a workspace of
     torch's allocator for the call."""
-    what, ix, lib = "nmdlm_draft_verify", logits.get_device(), load()
-    _floats(what, ("logits", logits, torch.float32), ("draft_logits", draft_logits, torch.float32),
-            ("u", u, torch.float32), ("conf", conf, torch.float64))
-    args = (_arg(what, "logits", logits, M * V, 4, ix), _arg(what, "draft_logits", draft_logits, M * V, 4, ix),
-            M, V, _arg(what, "draft", draft, M, 4, ix), _arg(what, "u", u, 2 * M, 4, ix), float(temperature),
-            float(draft_temperature), _arg(what, "cu_rows", cu_rows, n_seq + 1, 4, ix), n_seq,
-            0 if chain else NMDLM_VERIFY_EACH, _arg(what, "tokens", tokens, M, 4, ix),
-            _arg(what, "accepted", accepted, M, 1, ix), _arg(what, "n_accepted", n_accepted, n_seq, 4, ix),
-            _arg(what, "conf", conf, M, 8, ix))
-    ws, at, nbytes = _scratch(what, ws, lib.nmdlm_draft_verify_workspace_size(M, V), ix, stream)
-    _on(ix, what, lambda st: lib.nmdlm_draft_verify(*args, at, nbytes, st), stream)
+    what, ix = "nmdlm_draft_verify", logits.get_device()
+    f32, i32 = torch.float32, torch.int32
+    args = (_typed(what, "logits", logits, M * V, f32, ix),
+            _typed(what, "draft_logits", draft_logits, M * V, f32, ix), M, V,
+            _typed(what, "draft", draft, M, i32, ix), _typed(what, "u", u, 2 * M, f32, ix), float(temperature),
+            float(draft_temperature), _typed(what, "cu_rows", cu_rows, n_seq + 1, i32, ix), n_seq,
+            0 if chain else NMDLM_VERIFY_EACH, _typed(what, "tokens", tokens, M, i32, ix),
+            _typed(what, "accepted", accepted, M, torch.uint8, ix),
+            _typed(what, "n_accepted", n_accepted, n_seq, i32, ix), _typed(what, "conf", conf, M, torch.float64, ix))
+    ws, at, nbytes = _scratch(what, ws, nmdlm_draft_verify_workspace_size(M, V), ix, stream)
+    fn = load().nmdlm_draft_verify
+    _on(ix, what, lambda st: fn(*args, at, nbytes, st), stream)
 
 
 def nmdlm_block_step(model: "DeviceModel", io: StepIO, ws: torch.Tensor, stream=None) -> None:
