@@ -101,7 +101,8 @@ __device__ __forceinline__ int32_t* split_sums(const MaskedArgs& a, int row, int
 // Logical ids go head fastest, and the last tiles first, which see most keys where
 // rows see what is before them.  In grids that fill the chip (spread) groups of up to eight
 // heads of a tile go to the dies in turn: a range of tiles a die, as xcd_order has it,
-// gave the first die the longest ones (2048 causal rows 84 us, as long as if all saw all).
+// gave the first die the longest ones (2048 causal rows with a bias 94 us against 66, 2 x
+// 1024 rows in blocks 51 against 45).
 constexpr int kHeadWaves = 8;
 struct Place {
   int h, h0, t, z, tile, part, np;  // h0: the workgroup's first head
@@ -140,7 +141,10 @@ __device__ __forceinline__ Place place(const MaskedArgs& a, int wave, int nwaves
 // each, one barrier a chunk, two buffers.  (Each wave reading its own pieces counted
 // on the CU's cache to keep the lines for the others: 80 us a call of 130 thousand keys, 16
 // heads of 128, T = 4, where 92 with four chunks of loads on their way in place of two: they
-// no longer fitted.)
+// no longer fitted.)  That call takes 57 to 66 us of the kernel and 8 of the join: 268 MB at
+// 4.1 to 4.7 TB/s, where a plain read has 6.3; what is missing is at the chunk's barrier,
+// where all waves wait for the slowest load.  One row of a thousand keys, 5.5 us, is a chain
+// of trips to memory: arguments, ranges, query, keys, values.
 // ---------------------------------------------------------------------------
 constexpr int kRowWaves = 12;  // of a workgroup at most
 
@@ -325,10 +329,11 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_masked_rows(MaskedArgs a) {
 // ---------------------------------------------------------------------------
 // k_masked_tiles: a tile of 16*QG rows, the sums and the pipeline of attn_device.h over the
 // chunks that any row of the tile sees.  HEADS: wave = head of one timestep and split,
-// the sums go to k_masked_join; else wave = (timestep, part) of one head, and the neuron.  A chunk that not all of them see whole is
-// masked: a lane (one row, 16 keys) makes the bits of its keys from the row's
-// ranges, and the weights of the others become 0 (byte -128).  The values of the
-// keys past n_keys in the last chunk then count with weight 0 too.
+// the sums go to k_masked_join; else wave = (timestep, part) of one head, and the neuron.
+// A chunk that not all of them see whole is masked: a lane (one row, 16 keys) makes
+// the bits of its keys from the row's ranges, and the weights of the others become 0
+// (byte -128).  The values of the keys past n_keys in the last chunk then count with
+// weight 0 too.
 //
 // Bias: the scores' sums begin with 8 * bias, so it costs no instruction behind the
 // products; the table is extended by 128 entries below and above, which clamps.  A
@@ -336,6 +341,13 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_masked_rows(MaskedArgs a) {
 // has one bias for all pairs.  Where a chunk's positions are consecutive a lane's 16
 // keys take 16 consecutive entries of the bias, reversed and extended by 16 on each
 // side: one clamped index for all of them.
+//
+// Bound by the instructions issued at two waves a SIMD: 266 vector instructions a chunk of
+// 32 rows (key and value bits made bytes, table bytes packed, addresses), 1170 before and
+// behind a tile's chunks.  2 x 1024 rows in blocks 45 us (0.8 POP/s of what the rows see),
+// 2048 causal rows with a bias 66 us, 18 rows x 65 thousand keys 51 and 10 of the join; 48
+// rows x 500 keys, 14 us, fill a fifth of the CUs.  (Sixteen waves a workgroup there:
+// 17.2.)
 // ---------------------------------------------------------------------------
 constexpr int kWideEntries = 384;  // scores -128 .. 255
 constexpr int kBiasPad = 16;
@@ -656,11 +668,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_masked_join(MaskedArgs a) {
 //    34 x 2000 23 / 20, x 4000 24 / 32; 66 x 2000 28 / 21, x 8000 37 / 56; 130 x 4000 43 / 35, x
 //    16000 72 / 104; 250 (16 tiles, a workgroup a CU without) x 16000 104 / 109.  T = 8, H = 8, dh =
 //    64: 18 x 1000 13 / 15; T = 1, H = 4: 1 x 1500 8.7 / 5.2, x 6000 9.2 / 11.4, 18 x 1500 11 / 8.3.
-//  * 32 rows a wave where the tiles give 1024 such waves (2 x 1024 rows in blocks 52 against
-//    72 with 16), by heads where fewer keys are expanded so: a chunk costs 155 for 16 rows
-//    and 200 for 32 (18 rows x 65 thousand keys 62 against 85).
-//  * Splits to fill the chip: 18 x 65 thousand keys, 16, 32 and 64 splits 64, 62 and 79; one
-//    row x 130 thousand, 64 splits 68, 96 77, 128 73.
+//  * 32 rows a wave where the tiles give 1024 such waves (2 x 1024 rows in blocks 45 against
+//    58 with 16, 2048 causal rows with a bias 66 against 84), by heads where fewer keys are
+//    expanded so: a chunk costs 155 for 16 rows and 200 for 32 (18 rows x 65 thousand keys
+//    62 against 88).
+//  * Splits to fill the chip: 18 x 65 thousand keys, 16, 32 and 64 splits 91, 62 and 75; one
+//    row x 130 thousand, 32, 64 and 128 splits 85, 67 and 75.
 MaskedRoute masked_route(int T, int M, int n_keys, int H) {
   MaskedRoute r{1, T <= 2 ? 4 : (T <= 4 ? 2 : 1), 1, false};
   if (M > 2) r.tile = M >= 32 && (long long)(M / 32) * H * T >= 1024 ? 32 : 16;
