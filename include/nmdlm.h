@@ -782,8 +782,8 @@ size_t nmdlm_block_step_masked_workspace_size(const nmdlm_model* model, int M, i
  *   conf    device double [M] or NULL
  *   ws      workspace of nmdlm_token_sample_workspace_size() bytes (any content)
  * Limits: M <= NMDLM_MAX_SAMPLE_M, V <= NMDLM_MAX_SAMPLE_V, else
- * NMDLM_ERR_UNSUPPORTED.  Errors: NMDLM_ERR_INVALID_ARG for a missing or misaligned pointer, a size below
- * 1, a temperature that is negative, infinite or NaN.
+ * NMDLM_ERR_UNSUPPORTED.  Errors: NMDLM_ERR_INVALID_ARG for a missing or misaligned
+ * pointer, a size below 1, a temperature that is negative, infinite or NaN.
  * ------------------------------------------------------------------------ */
 #define NMDLM_MAX_SAMPLE_V 16777216
 #define NMDLM_MAX_SAMPLE_M 65535
@@ -824,8 +824,8 @@ size_t nmdlm_token_sample_workspace_size(int M, int V);
  *                 token, as in nmdlm_token_sample
  *   flags         0 or NMDLM_VERIFY_EACH
  *   ws            workspace of nmdlm_draft_verify_workspace_size() bytes (any content)
- * Limits and errors: as nmdlm_token_sample; n_seq <= NMDLM_MAX_PLAN_ROWS; NMDLM_ERR_INVALID_ARG for other flags and for
- * n_seq other than 1 without cu_rows.
+ * Limits and errors: as nmdlm_token_sample; n_seq <= NMDLM_MAX_PLAN_ROWS;
+ * NMDLM_ERR_INVALID_ARG for other flags and for n_seq other than 1 without cu_rows.
  * ------------------------------------------------------------------------ */
 #define NMDLM_VERIFY_EACH 0x1u
 nmdlm_status nmdlm_draft_verify(const float* logits, const float* draft_logits, int M, int V,

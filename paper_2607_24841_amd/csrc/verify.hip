@@ -272,8 +272,8 @@ __device__ __forceinline__ double sum4(const double (&w)[4]) { return (w[0] + w[
 // took 42 us where half of the others were through in 21: 1000 rows x 32000.)
 //
 // Bound by the float64 instructions, 17 a weight and 430 a part in all, beside the read:
-// 1000 rows x 32000 29 to 35 us, 3.7 to 4.4 TB/s (the read without the weights 27 us).  Five
-// waves a SIMD hold what they need in registers; with eight some was spilled (52 us).
+// 1000 rows x 32000 36 us, 3.5 TB/s (the read without the weights 27 us).  Five waves a SIMD
+// hold what they need in registers; with eight some was spilled (52 us).
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(64 * kPartWaves, 5) void k_logit_parts(VerifyArgs a) {
   __shared__ double pow[32];
