@@ -593,9 +593,11 @@ def _typed(what: str, name: str, t, n: int, dtype, index: int) -> int | None:
 def _scratch(what: str, ws, nbytes: int, index: int, stream):
     """The given workspace, or one of torch's allocator for this call."""
     if ws is None and index >= 0:
-        ws = torch.empty(max(256, nbytes), dtype=torch.uint8, device=index)
-        if stream is not None:
-            ws.record_stream(stream)
+        if stream is None:
+            ws = torch.empty(max(256, nbytes), dtype=torch.uint8, device=index)
+        else:  # of the stream's own memory: the current one's may still be read by work before the call
+            with torch.cuda.stream(stream):
+                ws = torch.empty(max(256, nbytes), dtype=torch.uint8, device=index)
         return ws, ws.data_ptr(), nbytes
     return ws, _arg(what, "ws", ws, 1, 1, index), 0 if ws is None else ws.numel()
 

@@ -124,6 +124,40 @@ def test_documents_of_one_step_are_those_of_steps_by_themselves():
         at += len(x)
 
 
+def test_step_captured_and_replayed():
+    """Every replay takes the ranges, positions and tokens that are there then."""
+    torch, B = need_gpu()
+    m = model(64)
+    r, pos = K.draft_mask(0, 6)
+    M = len(r)
+    dm = B.DeviceModel.from_mdlm(m, M)
+    rng = np.random.default_rng(5)
+    emb = O.unpack_model_emb(m)
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a.astype(np.int32))).cuda()  # noqa: E731
+    mask, ids = B.Mask(dev(r), dev(pos)), dev(rng.integers(0, m.V, M))
+    y = torch.zeros(m.T, M, m.d // 64, dtype=torch.int64, device="cuda")
+    ws = B.workspace(B.nmdlm_block_step_masked_workspace_size(dm, M, M, B.NMDLM_NO_HEAD))
+    io = B.step_io(M, 0, flags=B.NMDLM_NO_HEAD, tokens=ids, y_out=y)
+    B.nmdlm_block_step_masked(dm, io, mask, ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.nmdlm_block_step_masked(dm, io, mask, ws)
+    for k in range(4):
+        r2 = r.copy()
+        if k:
+            r2[:, 1] = np.maximum(r[:, 1] - k, 0)
+        toks = rng.integers(0, m.V, M)
+        mask.ranges.copy_(dev(r2).view(mask.ranges.shape))
+        ids.copy_(dev(toks))
+        kc, vc = O.new_caches(m.n_layers, m.T, dm.cache_cap, m.d)
+        want = O.masked_stack(O.block_input(toks, pos, emb, m.pos_ch), m.layers, kc, vc, 0, r2, None, pos, pos, 0)
+        for how in (graph.replay, lambda: B.nmdlm_block_step_masked(dm, io, mask, ws)):
+            y.zero_()
+            how()
+            torch.cuda.synchronize()
+            assert_same(synth.unpack_bits(B.from_dev_bits(y), m.d), want, f"replay {k}")
+
+
 def test_positions_outside_the_table():
     torch, B = need_gpu()
     m = model(62, max_pos=64)

@@ -277,6 +277,91 @@ def test_verify_captured_and_replayed():
             same4([out[k].cpu().numpy() for k in ("tok", "acc", "cf", "n")], want)
 
 
+def test_workspace_on_another_stream():
+    """Memory that the current stream's waiting work still reads is not taken for a call
+    on another stream."""
+    torch, B = need_gpu()
+    l, ql, draft, u, cu = make(15, [4] * 40, 9000, spare=(0, 0))
+    M, V = l.shape
+    g = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+    t = [g(l), g(ql), g(draft.astype(np.int32)), g(u), g(cu.astype(np.int32)), g(u[:, 0])]
+    tok, acc = torch.zeros(M, dtype=torch.int32, device="cuda"), torch.zeros(M, dtype=torch.uint8, device="cuda")
+    cf, drawn = torch.zeros(M, dtype=torch.float64, device="cuda"), torch.zeros(M, dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    calls = [(B.nmdlm_draft_verify_workspace_size(M, V),
+              lambda: B.nmdlm_draft_verify(t[0], t[1], M, V, t[2], t[3], 0.8, 0.8, tok, acc, cu_rows=t[4],
+                                           n_seq=len(cu) - 1, conf=cf, stream=side)),
+             (B.nmdlm_token_sample_workspace_size(M, V),
+              lambda: B.nmdlm_token_sample(t[0], M, V, 0.8, t[5], drawn, stream=side))]
+    for size, call in calls:
+        for _ in range(3):
+            x = torch.full((size,), 7, dtype=torch.uint8, device="cuda")
+            y = torch.zeros_like(x)
+            torch.cuda.synchronize()
+            torch.cuda._sleep(2_000_000)
+            y.copy_(x)
+            del x
+            call()
+            torch.cuda.synchronize()
+            assert bool((y == 7).all())
+    same4((tok.cpu().numpy(), acc.cpu().numpy(), cf.cpu().numpy(), None),
+          O.draft_verify(l, ql, draft, u, 0.8, 0.8, cu, True))
+    assert_same(drawn.cpu().numpy(), O.token_sample(l, 0.8, u[:, 0])[0], "drawn")
+
+
+def test_two_calls_at_once():
+    """On two streams, and two captured graphs."""
+    torch, B = need_gpu()
+    g = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+    jobs = []
+    for i in (0, 1):
+        l, ql, draft, u, cu = make(16 + i, [6, 2, 30], 7000, spare=(0, 0))
+        M = len(l)
+        t = [g(l), g(ql), g(draft.astype(np.int32)), g(u), g(cu.astype(np.int32))]
+        tok, acc = torch.zeros(M, dtype=torch.int32, device="cuda"), torch.zeros(M, dtype=torch.uint8, device="cuda")
+        jobs.append((M, t, tok, acc, torch.cuda.Stream(), O.draft_verify(l, ql, draft, u, 0.7, 0.9, cu, True)))
+
+    def call(job, stream=None):
+        M, t, tok, acc = job[:4]
+        B.nmdlm_draft_verify(t[0], t[1], M, 7000, t[2], t[3], 0.7, 0.9, tok, acc, cu_rows=t[4], n_seq=3, stream=stream)
+
+    def check():
+        torch.cuda.synchronize()
+        for _, _, tok, acc, _, want in jobs:
+            same4((tok.cpu().numpy(), acc.cpu().numpy(), None, None), want)
+            tok.zero_(), acc.zero_()
+        torch.cuda.synchronize()
+
+    for _ in range(5):
+        for job in jobs:
+            call(job, job[4])
+    check()
+    graphs = []
+    for job in jobs:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call(job)
+    for _ in range(3):
+        for gr, job in zip(graphs, jobs):
+            with torch.cuda.stream(job[4]):
+                gr.replay()
+        check()
+
+
+def test_sample_of_many_rows():
+    rng = np.random.default_rng(17)
+    l, u = K.logits(rng, 65535, 5), rng.random(65535, dtype=np.float32)
+    same(sample(l, 1.0, u), O.token_sample(l, 1.0, u))
+
+
+@pytest.mark.parametrize("V", [1 << 20, 1100003])
+def test_sample_of_a_long_list(V):
+    """2^20 weights: 2^-53 sqrt(2^20) = 1.1e-13 for independent roundings."""
+    rng = np.random.default_rng(18)
+    l, u = K.logits(rng, 3, V), rng.random(3, dtype=np.float32)
+    same(sample(l, 1.0, u), O.token_sample(l, 1.0, u))
+
+
 def test_rejects_foreign_tensors():
     torch, B = need_gpu()
     l, u = torch.zeros(4, 10, device="cuda"), torch.zeros(4, device="cuda")
