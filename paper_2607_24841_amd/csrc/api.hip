@@ -662,6 +662,11 @@ nmdlm_status nmdlm_block_step_masked(const nmdlm_model* md, const nmdlm_mask* ma
   for (int l = 0; bias && l < md->n_layers; ++l) any_bias = any_bias || bias[l];
   if ((rc = mask_ok(mask, any_bias)) != NMDLM_OK) return rc;
   if (!io->x_in && (!mask->q_pos || !aligned(mask->q_pos, 4))) return NMDLM_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)io->tokens, (const void*)io->logits, (const void*)io->pred,
+                        (const void*)io->unmasked_pos, (const void*)io->status})
+    if (!aligned(p, 4)) return NMDLM_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)io->x_in, (const void*)io->y_out, (const void*)io->conf, (const void*)io->stats})
+    if (!aligned(p, 8)) return NMDLM_ERR_INVALID_ARG;
   if (md->cache_cap % 64 != 0 || md->cache_cap < (int64_t)io->C + io->M) return NMDLM_ERR_INVALID_ARG;
   if (md->cache_cap / 64 > INT_MAX) return NMDLM_ERR_UNSUPPORTED;
   if ((rc = layers_ok(md, io->flags)) != NMDLM_OK) return rc;

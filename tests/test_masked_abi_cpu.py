@@ -173,3 +173,13 @@ def test_masked_step_refusals(lib):
     assert f(0, 5) == f(5, 4) == f(5, 0) == 0
     sizes = [f(16, n) for n in range(16, 40000, 97)]
     assert sizes == sorted(sizes)     # does not fall as the keys grow
+
+
+def test_masked_step_refuses_misaligned_buffers(lib):
+    layers = (B.Layer * 1)(B.Layer(FAKE, FAKE, FAKE, FAKE, 200, 200, 200, 200, 200, 200, 200, 4, FAKE, FAKE, FAKE, FAKE))
+    m = B.Model(1, 1024, 16, 4096, 32000, 4, 576, 64, layers, FAKE, FAKE, None, None)
+    mask = B.MaskC(FAKE, FAKE, FAKE, 4)
+    for name, off in [("tokens", 2), ("logits", 2), ("pred", 1), ("unmasked_pos", 2), ("status", 1), ("x_in", 4),
+                      ("y_out", 4), ("conf", 4), ("stats", 4)]:
+        io = B.step_io(16, 512, flags=B.NMDLM_NO_HEAD, **{"tokens": FAKE, name: FAKE + off})
+        assert lib.nmdlm_block_step_masked(C.byref(m), C.byref(mask), None, C.byref(io), FAKE, 1 << 30, None) == INVALID, name
