@@ -345,9 +345,8 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_masked_rows(MaskedArgs a) {
 // Bound by the instructions issued at two waves a SIMD: 266 vector instructions a chunk of
 // 32 rows (key and value bits made bytes, table bytes packed, addresses), 1170 before and
 // behind a tile's chunks.  2 x 1024 rows in blocks 45 us (0.8 POP/s of what the rows see),
-// 2048 causal rows with a bias 66 us, 18 rows x 65 thousand keys 51 and 10 of the join; 48
-// rows x 500 keys, 14 us, fill a fifth of the CUs.  (Sixteen waves a workgroup there:
-// 17.2.)
+// 2048 causal rows with a bias 66 us, 18 rows x 65 thousand keys 51 and 10 of the join.  34
+// rows x 1058 keys, 14 us, fill 48 of 256 CUs (sixteen waves a workgroup there: 17.2).
 // ---------------------------------------------------------------------------
 constexpr int kWideEntries = 384;  // scores -128 .. 255
 constexpr int kBiasPad = 16;
@@ -449,7 +448,8 @@ __global__ __launch_bounds__(64 * NMDLM_MAX_T, QG == 1 ? 4 : 2) void k_masked_ti
     q_lo = wave_min(q_lo);
     q_hi = wave_max(q_hi);
     small_pos = q_lo >= -kSmallPos && q_hi <= kSmallPos;
-    for (int i = HEADS ? lane : tid; i < 2 * D + 2 * kBiasPad; i += HEADS ? 64 : nth)  // entry i: key behind the row by i - D - kBiasPad
+    // entry i: key behind the row by i - D - kBiasPad
+    for (int i = HEADS ? lane : tid; i < 2 * D + 2 * kBiasPad; i += HEADS ? 64 : nth)
       sBias[i] = 8 * a.bias[(size_t)h * (2 * D + 1) + min(max(D + kBiasPad - i, -D), D) + D];
     for (int i = tid; i < kWideEntries; i += nth) {
       const uint32_t v = (uint32_t)a.lut[min(max(i - 128, 0), 255)] ^ 0x80u;
