@@ -143,7 +143,7 @@ __device__ __forceinline__ Place place(const MaskedArgs& a, int wave, int nwaves
 // heads of 128, T = 4, where 92 with four chunks of loads on their way in place of two: they
 // no longer fitted.)  That call takes 57 to 66 us of the kernel and 8 of the join: 268 MB at
 // 4.1 to 4.7 TB/s, where a plain read has 6.3; what is missing is at the chunk's barrier,
-// where all waves wait for the slowest load.  One row of a thousand keys, 5.5 us, is a chain
+// where all waves wait for the slowest load.  One row of 300 keys, 5.5 us, is a chain
 // of trips to memory: arguments, ranges, query, keys, values.
 // ---------------------------------------------------------------------------
 constexpr int kRowWaves = 12;  // of a workgroup at most
