@@ -10,7 +10,6 @@
 //   k_draw         the part in which the running sum passes the drawn number, then the
 //                  id in it; and a request's count and end
 // Every sum that decides is made in the same way by all waves that need it.
-#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -29,12 +28,11 @@ struct PartStat {
 // weights of its ids.
 struct Temper {
   double inv, scale;  // 1 / tau (finite, so that 0 * inv is 0); 32 / (tau ln 2)
-  double reach;       // 690 tau: no exponent below -700 within this of the largest
   bool sharp;         // temperature 0: weights at 1
 };
 static Temper temper(double tau) {
   const double inv = tau == 0.0 ? 1.0 : std::min(1.0 / tau, 1e300);
-  return Temper{inv, inv * 46.16624130844683, 690.0 / inv, tau == 0.0};
+  return Temper{inv, inv * 46.16624130844683, tau == 0.0};
 }
 
 struct VerifyArgs {
@@ -141,13 +139,13 @@ __device__ __forceinline__ bool row_counts(const VerifyArgs& a, int m) {
 // between two ids in one draw of 10^9.  Float64 runs at the rate of float32 here, so
 // it is the instructions that count, 17 a weight.
 struct Dist {
-  float top, cut;     // the largest; below cut an exponent may be below -700
-  double inv, scale, reach;
+  float top;  // the largest
+  double inv, scale;
   double sum;
   bool some, sharp, lift;  // any weight; temperature 0; the largest is +inf
   int first;               // id of the largest
   __device__ __forceinline__ explicit Dist(const Temper& t)
-      : inv(t.inv), scale(t.scale), reach(t.reach), sum(0.0), sharp(t.sharp), first(0) {
+      : inv(t.inv), scale(t.scale), sum(0.0), sharp(t.sharp), first(0) {
     set_top(-INFINITY);
   }
   // with a largest of +inf these logits count as 0, the others as -inf
@@ -155,12 +153,11 @@ struct Dist {
     some = t > -INFINITY;
     lift = t == INFINITY;
     top = lift ? 0.0f : t;
-    cut = fmaxf((float)((double)top - reach), -FLT_MAX);
   }
   __device__ __forceinline__ float seen(float x) const {
     return !lift ? x : x == INFINITY ? 0.0f : -INFINITY;
   }
-  template <bool CLEAN>  // CLEAN: not below cut
+  template <bool CLEAN>  // CLEAN: the exponent is not below the floor
   __device__ __forceinline__ double weight_of(float x, const double* pow) const {
     constexpr double kMagic = 6755399441055744.0;  // 1.5 * 2^52: the sum's low bits are the integer
     const double y = (double)x - (double)top;
@@ -208,7 +205,10 @@ struct Dist {
     for (int k = 0; k < kQuads; ++k)
 #pragma unroll
       for (int e = 0; e < 4; ++e) least = __builtin_elementwise_minimum(least, x[k][e]);
-    if (__builtin_amdgcn_ballot_w64(least >= cut) == ~0ull) each_group<true>(x, pow, use);
+    // the floor's own comparison, made for the least logit: in float64, since a float beside a
+    // large logit may lie many exponents beside what it stands for
+    const double e = ((double)least - (double)top) * inv;
+    if (__builtin_amdgcn_ballot_w64(e >= kExpFloor) == ~0ull) each_group<true>(x, pow, use);
     else each_group<false>(x, pow, use);
   }
   __device__ __forceinline__ void weights(float (&x)[kQuads][4], double (&w)[kQuads][4], const double* pow) const {

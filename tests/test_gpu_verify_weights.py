@@ -1,0 +1,47 @@
+"""Weights of tokens on the GPU where a logit's rounding is many exponents wide: ids equal
+to the oracle's, confidences to the tolerance of the other tests."""
+import numpy as np
+import pytest
+
+from oracle import nmdlm_oracle as O
+from tests.test_gpu_verify import same, same4, sample, verify
+
+pytestmark = pytest.mark.gpu
+
+# the largest logit, floats below it, temperature: exponents of -763, -954, -781, -1024 and
+# -1024, where a float has no room for "700 temperatures below the largest"
+NEAR = [(40.0, 2, 1e-8), (20.0, 1, 2e-9), (20000.0, 4, 1e-5), (2.0 ** 33 + 1024, 1, 1.0), (-2.0 ** 33, 1, 1.0)]
+
+
+def near_equal(rng, M, V, top, steps):
+    """Rows of the largest logit and the one `steps` floats below alone."""
+    low = np.float32(top)
+    for _ in range(steps):
+        low = np.nextafter(low, np.float32(-np.inf))
+    l = np.where(rng.random((M, V)) < 0.5, np.float32(top), low)
+    l[:, 0] = top
+    return l
+
+
+@pytest.mark.parametrize("top, steps, tau", NEAR)
+@pytest.mark.parametrize("V", [3000, 4099])
+def test_sample_among_near_equal_logits(V, top, steps, tau):
+    """Whole parts of ids whose exponents are 0 or below -700."""
+    rng = np.random.default_rng([1, V])
+    l, u = near_equal(rng, 8, V, top, steps), rng.random(8, dtype=np.float32)
+    l[1, 1:] = l[1].min()                 # one id alone
+    l[2, :2048], l[2, 2100] = l[2].min(), top   # parts without a largest one
+    for t in (tau, 0.0):
+        same(sample(l, t, u), O.token_sample(l, t, u))
+
+
+@pytest.mark.parametrize("top, steps, tau", NEAR)
+@pytest.mark.parametrize("chain", [True, False])
+def test_verify_among_near_equal_logits(chain, top, steps, tau):
+    rng = np.random.default_rng([2, steps])
+    V, M = 4099, 12
+    l, ql = near_equal(rng, M, V, top, steps), near_equal(rng, M, V, top, steps)
+    draft, u = rng.integers(0, V, M), rng.random((M, 2), dtype=np.float32)
+    cu = [0, 5, 6, 12]
+    for q, taus in ((ql, (tau, tau)), (None, (tau, tau)), (ql, (1e30 * tau, tau)), (ql, (tau, 0.0))):
+        same4(verify(l, q, draft, u, *taus, cu, chain), O.draft_verify(l, q, draft, u, *taus, cu, chain))
