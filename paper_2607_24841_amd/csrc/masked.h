@@ -53,6 +53,12 @@ struct VerifyCall {
   void* ws;
 };
 size_t verify_ws(int M, int V, bool drafts);
+// The logits to read for row m's draft.  A row without one has none: the caller's may end
+// before it (the row that follows a request's drafts), so the target's are read instead.
+__host__ __device__ inline const float* draft_logits_at(const float* logits, const float* draft_logits, int m,
+                                                        int V, int32_t draft) {
+  return ((uint32_t)draft < (uint32_t)V ? draft_logits : logits) + (size_t)m * V;
+}
 nmdlm_status launch_verify(const VerifyCall& c, hipStream_t st);
 
 }  // namespace nmdlm

@@ -97,6 +97,11 @@ void nmdlm_internal_masked_route(int T, int M, int n_keys, int H, int32_t* out) 
   out[3] = r.heads ? 1 : 0;
 }
 
+// Where the verification reads the draft's logits of row m.
+const float* nmdlm_internal_draft_logits(const float* logits, const float* draft_logits, int m, int V, int32_t draft) {
+  return draft_logits_at(logits, draft_logits, m, V, draft);
+}
+
 // The runs of row block y of M tokens into out[4 i ..]: sequence, first position,
 // tokens, 1 when stored in bytes.  Returns their number.
 int nmdlm_internal_token_runs(int pos0, int seq_len, int Mb, int M, int y, int32_t* out) {

@@ -125,7 +125,8 @@ __device__ __forceinline__ RowAt target_row(const VerifyArgs& a, int m) {
   return RowAt(l, a.V, RowAt::shift_of(l));
 }
 __device__ __forceinline__ RowAt draft_row(const VerifyArgs& a, int m) {  // at the target's ids
-  return RowAt(a.draft_logits + (size_t)m * a.V, a.V, RowAt::shift_of(a.logits + (size_t)m * a.V));
+  return RowAt(draft_logits_at(a.logits, a.draft_logits, m, a.V, a.draft[m]), a.V,
+               RowAt::shift_of(a.logits + (size_t)m * a.V));
 }
 __device__ __forceinline__ bool row_counts(const VerifyArgs& a, int m) {
   return !a.cu || (m >= a.cu[0] && m < a.cu[a.n_seq]);
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(64 * kPartWaves, 5) void k_logit_parts(VerifyArgs a
   };
   auto row_at = [&](int r) { return r >= a.M ? draft_row(a, r - a.M) : target_row(a, r); };
   float next[kQuads][4], x[kQuads][4];
-  if (left > 0) row_at(m).load(next, part);  // wanted or not: asking takes as long
+  if (left > 0) row_at(m).load(next, part);  // whether it counts or not: asking takes as long
   bool here = left > 0 && wanted(m);
   fill_pow(pow);
   __syncthreads();

@@ -4,7 +4,8 @@ import numpy as np
 import pytest
 
 from oracle import nmdlm_oracle as O
-from tests.test_gpu_verify import same, same4, sample, verify
+from tests._gpu import assert_same, need_gpu
+from tests.test_gpu_verify import make, same, same4, sample, verify
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +46,26 @@ def test_verify_among_near_equal_logits(chain, top, steps, tau):
     cu = [0, 5, 6, 12]
     for q, taus in ((ql, (tau, tau)), (None, (tau, tau)), (ql, (1e30 * tau, tau)), (ql, (tau, 0.0))):
         same4(verify(l, q, draft, u, *taus, cu, chain), O.draft_verify(l, q, draft, u, *taus, cu, chain))
+
+
+@pytest.mark.parametrize("V", [300, 32000])
+@pytest.mark.parametrize("n", [1, 8])
+def test_draft_logits_end_with_the_drafts(n, V):
+    """Logits of the drafted rows alone through the C entry: the row behind them has none."""
+    import ctypes as C
+
+    torch, B = need_gpu()
+    l, ql, draft, u, cu = make(n, [n + 1], V, spare=(0, 0))
+    draft[n] = -1
+    want = O.draft_verify(l, ql, draft, u, 0.8, 0.8, cu, True)
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+    t = [dev(l), dev(ql[:n]), dev(draft.astype(np.int32)), dev(u)]
+    tok, acc = torch.zeros(n + 1, dtype=torch.int32, device="cuda"), torch.zeros(n + 1, dtype=torch.uint8, device="cuda")
+    ws = B.workspace(B.nmdlm_draft_verify_workspace_size(n + 1, V))
+    p = lambda x: C.c_void_p(x.data_ptr())  # noqa: E731
+    for _ in range(2):
+        assert B.load().nmdlm_draft_verify(p(t[0]), p(t[1]), n + 1, V, p(t[2]), p(t[3]), 0.8, 0.8, None, 1, 0, p(tok), p(acc),
+                                           None, None, p(ws), ws.numel(), None) == B.NMDLM_OK
+        torch.cuda.synchronize()
+        assert_same(tok.cpu().numpy(), want[0], "tokens")
+        assert_same(acc.cpu().numpy(), want[1], "accepted")
