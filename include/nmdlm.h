@@ -767,9 +767,9 @@ size_t nmdlm_block_step_masked_workspace_size(const nmdlm_model* model, int M, i
 
 /* ------------------------------------------------------------------------
  * nmdlm_token_sample — a token of each row of logits.  With the row's largest
- * logit l_max, temperature tau and w_v = exp((l_v - l_max) / tau) (float64; 0 for
- * exponents below -700 and for NaN, 1 where l_v = l_max), the token is the first
- * v with
+ * logit l_max, temperature tau and w_v = exp((l_v - l_max) / tau) (float64, to
+ * 4.6e-16 + 1.2e-16 |exponent| of itself; 0 for exponents below -700 and for NaN, 1
+ * where l_v = l_max), the token is the first v with
  *     w_0 + ... + w_v > u * sum_j w_j
  * (the last of positive weight when none is); at tau = 0 the first of the
  * largest logits.  conf is w_token / sum_j w_j, at tau = 0 with tau = 1 in the

@@ -69,3 +69,23 @@ def test_draft_logits_end_with_the_drafts(n, V):
         torch.cuda.synchronize()
         assert_same(tok.cpu().numpy(), want[0], "tokens")
         assert_same(acc.cpu().numpy(), want[1], "accepted")
+
+
+@pytest.mark.parametrize("tau", [0.1, 0.8, 1.0, 7.3, 250.0])
+def test_weights_are_exponentials_in_float64(tau):
+    """Two ids, the second drafted and taken (u = 0): its probability is e^x / (1 + e^x), x the
+    exponent.  A weight errs by 4.6e-16 + 1.2e-16 |x|, the sum, the division and float64 of the
+    reference by 2^-53 each.  The reference, in 64 bits of mantissa, adds |x| 2^-63."""
+    M = 4000
+    rng = np.random.default_rng(int(tau * 10))
+    l = np.zeros((M, 2), np.float32)
+    l[:, 0] = rng.normal(size=M) * tau
+    l[:, 1] = l[:, 0] - (tau * np.concatenate([rng.random(M // 2) * 3, np.linspace(0, 680, M - M // 2)])).astype(np.float32)
+    tok, acc, conf, _ = verify(l, None, np.ones(M, int), np.zeros((M, 2), np.float32), tau, tau, [0, M], False)
+    assert (acc == 1).all() and (tok == 1).all()
+    x = (l[:, 1].astype(np.longdouble) - l[:, 0]) / np.longdouble(tau)
+    w = np.exp(x)
+    want = w / (1 + w)
+    bound = 4.6e-16 + 1.2e-16 * np.abs(x) + 3 * 2.0 ** -53 + np.abs(x) * 2.0 ** -63
+    off = np.abs(conf / want - 1)
+    assert (off <= bound).all(), (float((off / bound).max()), float(off.max()))
