@@ -401,6 +401,9 @@ struct Pair {
   // max(p - q, 0) of a part's ids
   __device__ __forceinline__ void left(const RowAt& row, int part, Logits& l, double (&w)[kQuads][4],
                                        const double* pow) const {
+    // each product rounded by itself: of equal distributions nothing is left, and the part's sum
+    // and its weights come out alike in both kernels
+#pragma clang fp contract(off)
     auto &lp = l.p, &lq = l.q;
     double y[kQuads][4];
     if (p.sharp) {

@@ -89,3 +89,18 @@ def test_weights_are_exponentials_in_float64(tau):
     bound = 4.6e-16 + 1.2e-16 * np.abs(x) + 3 * 2.0 ** -53 + np.abs(x) * 2.0 ** -63
     off = np.abs(conf / want - 1)
     assert (off <= bound).all(), (float((off / bound).max()), float(off.max()))
+
+
+@pytest.mark.parametrize("V", [500, 33001])
+def test_nothing_is_left_of_equal_distributions(V):
+    """p is q and the draft an id that both rule out: the token is drawn from p."""
+    rng = np.random.default_rng(V)
+    l, _, draft, u, cu = make(21, [9, 8], V)
+    draft[:] = rng.integers(0, V, len(draft))
+    l[np.arange(len(l)), draft] = -np.inf
+    for tau in (0.0, 0.3, 0.8):
+        got = verify(l, l, draft, u, tau, tau, cu, False)
+        want = O.draft_verify(l, l, draft, u, tau, tau, cu, False)
+        same4(got, want)
+        rows = slice(cu[0], cu[-1])
+        assert_same(got[0][rows], O.token_sample(l[rows], tau, u[rows, 1])[0], "drawn")
