@@ -125,8 +125,9 @@ __device__ __forceinline__ RowAt target_row(const VerifyArgs& a, int m) {
   const float* l = a.logits + (size_t)m * a.V;
   return RowAt(l, a.V, RowAt::shift_of(l));
 }
-__device__ __forceinline__ RowAt draft_row(const VerifyArgs& a, int m) {  // at the target's ids
-  return RowAt(draft_logits_at(a.logits, a.draft_logits, m, a.V, a.draft[m]), a.V,
+// The draft's row (x: its draft) at the target's ids.
+__device__ __forceinline__ RowAt draft_row(const VerifyArgs& a, int m, int x) {
+  return RowAt(draft_logits_at(a.logits, a.draft_logits, m, a.V, x), a.V,
                RowAt::shift_of(a.logits + (size_t)m * a.V));
 }
 __device__ __forceinline__ bool row_counts(const VerifyArgs& a, int m) {
@@ -297,7 +298,7 @@ __global__ __launch_bounds__(64 * kPartWaves, 5) void k_logit_parts(VerifyArgs a
     const int row = of_draft ? r - a.M : r;
     return row_counts(a, row) && !(of_draft && (uint32_t)a.draft[row] >= (uint32_t)a.V);
   };
-  auto row_at = [&](int r) { return r >= a.M ? draft_row(a, r - a.M) : target_row(a, r); };
+  auto row_at = [&](int r) { return r >= a.M ? draft_row(a, r - a.M, a.draft[r - a.M]) : target_row(a, r); };
   float next[kQuads][4], x[kQuads][4];
   if (left > 0) row_at(m).load(next, part);  // whether it counts or not: asking takes as long
   bool here = left > 0 && wanted(m);
@@ -383,9 +384,9 @@ __device__ __forceinline__ Dist row_dist(const PartStat* st, PartStat mine, int 
 // The logits of a part of a row, the target's and the draft's.
 struct Logits {
   float p[kQuads][4], q[kQuads][4];
-  __device__ __forceinline__ void load(const VerifyArgs& a, int m, int part) {
+  __device__ __forceinline__ void load(const VerifyArgs& a, int m, int x, int part) {
     target_row(a, m).load(p, part);
-    if (a.draft_logits) draft_row(a, m).load(q, part);
+    if (a.draft_logits) draft_row(a, m, x).load(q, part);
   }
 };
 
@@ -458,7 +459,7 @@ __global__ __launch_bounds__(64 * kPartWaves) void k_verify_left(VerifyArgs a) {
   const int x = a.draft[m], at = min(max(x, 0), a.V - 1);
   const float u = a.u[2 * m];
   const RowAt row = target_row(a, m);
-  const float px = row.at(at), qx = a.draft_logits ? draft_row(a, m).at(at) : 0.0f;
+  const float px = row.at(at), qx = a.draft_logits ? draft_row(a, m, x).at(at) : 0.0f;
   fill_pow(pow);
   if (!row_counts(a, m)) return;  // uniform
   if ((uint32_t)x >= (uint32_t)a.V) {
@@ -488,7 +489,7 @@ __global__ __launch_bounds__(64 * kPartWaves) void k_verify_left(VerifyArgs a) {
   if (take || !p.some) return;
   for (; part < a.parts; part += step) {
     Logits l;
-    l.load(a, m, part);
+    l.load(a, m, x, part);
     double w[kQuads][4], sum = 0.0;
     d.left(row, part, l, w, pow);
 #pragma unroll
@@ -639,7 +640,7 @@ __global__ __launch_bounds__(64) void k_draw(VerifyArgs a) {
       const Spot s = find_part(a.parts, u, [&](int i) { return i < 64 ? mine_left : left[i]; });
       if (s.total > 0.0) {
         Logits l;
-        l.load(a, m, s.part);
+        l.load(a, m, x, s.part);
         const Pair d(a, m, x, p, mine_q, pow);
         d.left(row, s.part, l, w, pow);
         tok = find_id(s, w, l.p, row);
