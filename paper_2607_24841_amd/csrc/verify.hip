@@ -279,8 +279,8 @@ __device__ __forceinline__ double sum4(const double (&w)[4]) { return (w[0] + w[
 // the waves a wave met the same part of every row, and those of a row's last, partial one
 // took 42 us where half of the others were through in 21: 1000 rows x 32000.)
 //
-// Bound by the float64 instructions, 17 a weight and 430 a part in all, beside the read:
-// 1000 rows x 32000 36 us, 3.5 TB/s (the read without the weights 27 us).  Five waves a SIMD
+// Bound by the float64 instructions, 18 a weight and 480 a part in all, beside the read:
+// 1000 rows x 32000 39 us, 3.3 TB/s (the read without the weights 27 us).  Five waves a SIMD
 // hold what they need in registers; with eight some was spilled (52 us).
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(64 * kPartWaves, 5) void k_logit_parts(VerifyArgs a) {
@@ -445,7 +445,7 @@ struct Pair {
 // k_verify_left: grid (waves of a row / 4, rows).  Each wave decides on its row's draft for
 // itself; the first writes what was decided.  (With the logits of the wave's first part on
 // their way meanwhile, 372 rows took 62 us against 58: most rows do not need them.)  372
-// rows x 32000: 16 us; few rows, 6 us, are a chain of trips to memory.
+// rows x 32000: 17 us; few rows, 6 us, are a chain of trips to memory.
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(64 * kPartWaves) void k_verify_left(VerifyArgs a) {
   __shared__ double pow[32];
@@ -569,7 +569,7 @@ __device__ __forceinline__ Token find_id(const Spot& s, const double (&w)[kQuads
 // k_draw: a wave a row that has no token yet, then one a request for its count.  In a
 // chain a row that follows one without an accepted draft is void.  (A void row's flag
 // is cleared while later rows look: they are void by the earlier row's, which stays.)
-// 4.7 to 8 us: a chain of trips to memory, stats, the part's logits, a token.
+// 5 to 8.4 us: a chain of trips to memory, stats, the part's logits, a token.
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(64) void k_draw(VerifyArgs a) {
   __shared__ double pow[32];
