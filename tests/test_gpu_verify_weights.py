@@ -1,5 +1,7 @@
-"""Weights of tokens on the GPU where a logit's rounding is many exponents wide: ids equal
-to the oracle's, confidences to the tolerance of the other tests."""
+"""Weights of tokens on the GPU: logits whose rounding is many exponents wide, the
+exponentials' accuracy, equal distributions, draft logits that end with the drafts.  Ids
+equal the oracle's, confidences to the tolerance of the other tests where no other is
+derived."""
 import numpy as np
 import pytest
 
